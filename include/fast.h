@@ -18,6 +18,10 @@
  *                             as the ordered sum over its readers     (Sec. 4.2)
  *   fast_edge_attention_bwd_indexed_coef, fast_index_add_scaled_rows  the
  *                             same from per-edge coefficients         (Sec. 4.2, 4.3)
+ *   fast_layer_norm_fwd/bwd   the norm around the attention (Eq. 1's update)
+ *   fast_rotary_fwd/bwd       rotary positions of queries and keys, several axes
+ *   fast_cache_write, fast_cache_gather  cached rows in 8 or 4 bits   (Sec. 4.2)
+ *   fast_edge_attention_fwd_cached   ESM and AGG over K|V rows of such a cache
  *
  * Conventions shared by every entry point
  *   - Memory: every array argument is a DEVICE pointer into HBM owned by the
@@ -523,6 +527,146 @@ fast_status_t fast_index_add_scaled_rows(const int32_t* occ_off, const int32_t* 
                                          fast_dtype_t src_dtype, const float* scal,
                                          const void* src, float* dst, void* ws,
                                          size_t ws_bytes, fast_stream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Layer norm of rows (the norm that a temporal attention layer applies to the
+ * destination's own row plus its aggregated messages, Eq. 1's update).
+ *   h = x + res (x where res is NULL),  mu = mean(h),
+ *   r = 1 / sqrt(mean((h - mu)^2) + eps),  y = (h - mu) r gamma + beta
+ * x, res, y: [n, D] of dtype; gamma, beta: [D] fp32, NULL for ones / zeros.
+ * With res the sum is rounded to dtype before the statistics, so that they
+ * are those of the row that `sum` ([n, D], optional, only with res) stores and the backward
+ * reads.  mean, rstd: [n] fp32, optional (the backward needs both).
+ * Statistics and products are fp32, the mean taken before the squares.
+ * Limits: 1 <= D <= 8192, n < 2^31.  Rows aligned to their element; y may be
+ * x, res or, where sum is NULL, neither.  eps >= 0.
+ * ------------------------------------------------------------------------ */
+fast_status_t fast_layer_norm_fwd(int64_t n, int D, fast_dtype_t dtype, const void* x,
+                                  const void* res, const float* gamma, const float* beta,
+                                  float eps, void* y, void* sum, float* mean, float* rstd,
+                                  fast_stream_t stream);
+
+/* Backward for dy [n, D], with xhat = (h - mu) r and g = dy gamma:
+ *   dx = r (g - mean(g) - xhat mean(g xhat)) + dsum   (the gradient of x and of res)
+ *   dgamma = sum over rows of dy xhat,  dbeta = sum over rows of dy
+ * h: the forward's sum (x where res was NULL); mean, rstd: its outputs; dsum:
+ * NULL, or the gradient [n, D] of dtype that reaches the sum on another path.
+ * dgamma, dbeta: [D] fp32, overwritten (zeros when n = 0), each optional;
+ * added in fp32 over at most 32 rows and in fp64 beyond, in a fixed order
+ * (repeated calls give the same bits).  dx: [n, D] of dtype; it may be dy or dsum.
+ * Workspace, needed for dgamma or dbeta only: fast_layer_norm_bwd_workspace(n, D)
+ * bytes, 8-byte aligned. */
+size_t fast_layer_norm_bwd_workspace(int64_t n, int D);
+fast_status_t fast_layer_norm_bwd(int64_t n, int D, fast_dtype_t dtype, const void* h,
+                                  const float* gamma, const float* mean, const float* rstd,
+                                  const void* dy, const void* dsum, void* dx, float* dgamma,
+                                  float* dbeta, void* ws, size_t ws_bytes, fast_stream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Rotary positions with several axes: instead of time features beside a row
+ * (fast_time_encode), queries and keys are turned by angles that grow with
+ * their positions, so that <turned q, turned k> depends on the difference of
+ * the positions only.  A key row can be turned once, when its event arrives.
+ *   theta[i,p] = pos[i, axis[p]] * omega[p]
+ *   (a, b) -> (a cos theta - b sin theta, a sin theta + b cos theta)
+ * for pairs p < `pairs` of every head of row i: elements (p, pairs + p) of the
+ * head, or (2p, 2p + 1) where `interleaved` is not 0.  A head's elements from
+ * 2 * pairs on are copied.
+ * x, y: rows of [H, dh] of dtype, ldx and ldy elements apart (>= H*dh: the K
+ * half of packed K|V rows has ldx = 2*H*dh).  y may be x with ldy = ldx; any
+ * other overlap of their elements is refused.  pos: [n, axes] fp32 (event
+ * times, ranks, coordinates); axis: [pairs] int32, NULL for all 0, values
+ * outside [0, axes) read the nearest axis; omega: [pairs] fp32.  The angle is
+ * exact in fp64, its sine and cosine are within 2e-7 at any position; a position that
+ * is not finite gives NaN.
+ * Limits: H <= 64, dh <= 256, 2 * pairs <= dh, n < 2^31.
+ * The backward turns dy by -theta (pos and omega are constants); its
+ * arguments are the forward's, with dy in place of x and dx in place of y.
+ * ------------------------------------------------------------------------ */
+fast_status_t fast_rotary_fwd(int64_t n, int H, int dh, fast_dtype_t dtype, const void* x,
+                              int64_t ldx, const float* pos, int axes, const int32_t* axis,
+                              const float* omega, int pairs, int interleaved, void* y,
+                              int64_t ldy, fast_stream_t stream);
+fast_status_t fast_rotary_bwd(int64_t n, int H, int dh, fast_dtype_t dtype, const void* dy,
+                              int64_t lddy, const float* pos, int axes, const int32_t* axis,
+                              const float* omega, int pairs, int interleaved, void* dx,
+                              int64_t lddx, fast_stream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Cached rows in 8 or 4 bits (the cache of Sec. 4.2 holds two to eight times
+ * the rows).  A row is `parts` vectors of `width` elements: one of D for
+ * feature rows, 2H of dh for packed K|V rows.  Every vector is cut into
+ * groups of 32 elements (the last may be shorter); a group has a scale 2^k,
+ * the smallest for which its largest magnitude is at most the format's largest
+ * value, and an element is the nearest code (ties to even) times the scale:
+ *   FAST_MXFP8: e4m3, largest 448, relative error at most 2^-4
+ *   FAST_MXFP4: e2m1, values 0, 0.5, 1, 1.5, 2, 3, 4, 6
+ * with k >= -127.  A group that holds an infinity or a NaN reads back as NaN.
+ * Record (row s of the cache at byte s * fast_cache_row_bytes): the codes of
+ * each vector, padded to 8 (a 4-bit pair's first code in the low half), then
+ * one byte k + 127 per vector and group (255: NaN, codes 0); bytes past
+ * them are neither read nor written.
+ *
+ * Rows are named by ids, as in fast_dedup_gather: slot(x) = slot_map ?
+ * slot_map[x] : x, for x in [0, id_bound); an id outside that range, or a
+ * slot outside [0, cache_rows), has no row.
+ * cache: [cache_rows] records, 16-byte aligned.  ids: [n] int64.
+ * Limits: parts <= 128, width <= 1024, parts * width <= 8192; n, cache_rows < 2^31.
+ *
+ * fast_cache_row_bytes: bytes of a record (a multiple of 16; 0 for sizes
+ *   outside the limits), chosen so that a record touches few 128-byte lines.
+ * fast_cache_write: cache[slot(ids[i])] = row i of src [n, parts, width].  Of
+ *   several i with one slot the last one is kept; `distinct` not 0 promises
+ *   that there are none and saves the search for them (a broken promise leaves
+ *   some mixture of their rows).  Workspace, where distinct is 0:
+ *   fast_cache_write_workspace(n, cache_rows) bytes, 16-byte aligned.
+ * fast_cache_gather: rows[i] = the values of cache[slot(ids[i])], rows
+ *   [n, parts, width] of dtype; a row without a slot is left untouched.
+ * ------------------------------------------------------------------------ */
+typedef enum {
+  FAST_MXFP8 = 0,
+  FAST_MXFP4 = 1,
+  FAST_CACHE_FORMAT_MAX_ENUM = 0x7fffffff /* as FAST_DTYPE_MAX_ENUM */
+} fast_cache_format_t;
+
+size_t fast_cache_row_bytes(int parts, int width, fast_cache_format_t format);
+size_t fast_cache_write_workspace(int64_t n, int64_t cache_rows);
+fast_status_t fast_cache_write(const int64_t* ids, int64_t n, int64_t id_bound,
+                               const int32_t* slot_map, int parts, int width,
+                               fast_dtype_t dtype, const void* src,
+                               fast_cache_format_t format, void* cache, int64_t cache_rows,
+                               int distinct, void* ws, size_t ws_bytes, fast_stream_t stream);
+fast_status_t fast_cache_gather(const int64_t* ids, int64_t n, int64_t id_bound,
+                                const int32_t* slot_map, int parts, int width,
+                                fast_cache_format_t format, const void* cache,
+                                int64_t cache_rows, fast_dtype_t dtype, void* rows,
+                                fast_stream_t stream);
+
+/* ------------------------------------------------------------------------
+ * The fused operator on cached K|V rows (serving: the events' rows are
+ * projected, turned and cached once, and every query reads them).
+ *   edge e reads K|V row slot(ids[e]) of a cache of 2H vectors of dh (K's
+ *   heads, then V's), as fast_cache_gather would return it in fp32; an edge
+ *   without a row is left out of its segment.
+ * Otherwise fast_edge_attention_fwd: out = AGG(ESM(Q, K), V), lse optional; a segment
+ * none of whose edges has a row is empty (out = 0, lse = -inf).
+ * Q, out: [N, H, dh] of dtype; ids: [E] int64 (g->edge_ids, or src_ids where
+ * rows belong to nodes); slot_map, cache: as in fast_cache_write.  Reads
+ * g->dst_offsets.  Segments of any length: long ones are cut into pieces that
+ * a second launch joins in their order (repeated calls give the same bits).
+ * Limits: H <= 64, dh <= 256, H*dh <= 1024.
+ * Workspace: fast_edge_attention_cached_workspace(N, E, H, dh) bytes (never 0 for valid
+ * sizes), 16-byte aligned.
+ * ------------------------------------------------------------------------ */
+size_t fast_edge_attention_cached_workspace(int64_t num_dst, int64_t num_edges, int H, int dh);
+fast_status_t fast_edge_attention_fwd_cached(const fast_tcsr_t* g, int H, int dh,
+                                             fast_dtype_t dtype, const void* Q,
+                                             const int64_t* ids, int64_t id_bound,
+                                             const int32_t* slot_map,
+                                             fast_cache_format_t format, const void* cache,
+                                             int64_t cache_rows, float scale, float neg_slope,
+                                             void* out, float* lse, void* ws, size_t ws_bytes,
+                                             fast_stream_t stream);
 
 #ifdef __cplusplus
 }

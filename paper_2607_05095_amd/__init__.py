@@ -32,6 +32,10 @@ __all__ = [
     "fast_index_add_rows_workspace", "fast_index_add_rows",
     "fast_edge_attention_bwd_indexed_coef",
     "fast_index_add_scaled_rows_workspace", "fast_index_add_scaled_rows",
+    "fast_layer_norm_fwd", "fast_layer_norm_bwd_workspace", "fast_layer_norm_bwd",
+    "fast_rotary_fwd", "fast_rotary_bwd", "MXFP8", "MXFP4", "fast_cache_row_bytes",
+    "fast_cache_write_workspace", "fast_cache_write", "fast_cache_gather",
+    "fast_edge_attention_cached_workspace", "fast_edge_attention_fwd_cached",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -40,6 +44,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("FAST_LIB") or os.path.join(_HERE, "libfast.so")
 
 F32, BF16 = 0, 1
+MXFP8, MXFP4 = 0, 1   # fast_cache_format_t
 NOALLOC_SCRATCH_BYTES = 128 << 20   # FAST_NOALLOC_SCRATCH_BYTES of include/fast.h
 _STATUS = {0: "FAST_OK", 1: "FAST_ERR_INVALID_ARG", 2: "FAST_ERR_UNSUPPORTED",
            3: "FAST_ERR_WORKSPACE", 4: "FAST_ERR_HIP"}
@@ -127,6 +132,22 @@ _SIGS = {
     "fast_index_add_scaled_rows_workspace": (_sz, [_i64, _i64, _i32, _i32]),
     "fast_index_add_scaled_rows": (_i32, [_p, _p, _i64, _i64, _p, _i64, _i32, _i32, _i32, _p, _p,
                                           _p, _p, _sz, _p]),
+    "fast_layer_norm_fwd": (_i32, [_i64, _i32, _i32, _p, _p, _p, _p, _f32, _p, _p, _p, _p, _p]),
+    "fast_layer_norm_bwd_workspace": (_sz, [_i64, _i32]),
+    "fast_layer_norm_bwd": (_i32, [_i64, _i32, _i32, _p, _p, _p, _p, _p, _p, _p, _p, _p, _p, _sz,
+                                   _p]),
+    "fast_rotary_fwd": (_i32, [_i64, _i32, _i32, _i32, _p, _i64, _p, _i32, _p, _p, _i32, _i32, _p,
+                               _i64, _p]),
+    "fast_rotary_bwd": (_i32, [_i64, _i32, _i32, _i32, _p, _i64, _p, _i32, _p, _p, _i32, _i32, _p,
+                               _i64, _p]),
+    "fast_cache_row_bytes": (_sz, [_i32, _i32, _i32]),
+    "fast_cache_write_workspace": (_sz, [_i64, _i64]),
+    "fast_cache_write": (_i32, [_p, _i64, _i64, _p, _i32, _i32, _i32, _p, _i32, _p, _i64, _i32, _p,
+                                _sz, _p]),
+    "fast_cache_gather": (_i32, [_p, _i64, _i64, _p, _i32, _i32, _i32, _p, _i64, _i32, _p, _p]),
+    "fast_edge_attention_cached_workspace": (_sz, [_i64, _i64, _i32, _i32]),
+    "fast_edge_attention_fwd_cached": (_i32, [_G, _i32, _i32, _i32, _p, _p, _i64, _p, _i32, _p,
+                                              _i64, _f32, _f32, _p, _p, _p, _sz, _p]),
 }
 
 _lib = None
@@ -165,6 +186,20 @@ def _stream(stream):
 def _check(st: int):
     if st != 0:
         raise FastError(st, fast_last_error())
+
+
+def _resident(dense=(), strided=()):
+    """Tensors of a call live on the current device, and those without a row
+    stride of their own are contiguous; raises otherwise."""
+    import torch
+    for t in (*dense, *strided):
+        if t is None or isinstance(t, int):
+            continue
+        if not t.is_cuda or t.device.index != torch.cuda.current_device():
+            raise FastError(1, f"tensor on {t.device}, not on the current GPU")
+    for t in dense:
+        if t is not None and not isinstance(t, int) and not t.is_contiguous():
+            raise FastError(1, f"tensor of shape {tuple(t.shape)} is not contiguous")
 
 
 def dtype_of(t) -> int:
@@ -434,3 +469,76 @@ def fast_index_add_scaled_rows(occ_off, occ, n, num_rows, dst_offsets, num_dst, 
                                             _ptr(dst_offsets), num_dst, H, dh, src_dtype,
                                             _ptr(scal), _ptr(src), _ptr(dst), _ptr(ws), ws_bytes,
                                             _stream(stream)))
+
+
+def fast_layer_norm_fwd(n, D, dtype, x, res, gamma, beta, eps, y, sum=None, mean=None, rstd=None,
+                        stream=None):
+    _resident((x, res, gamma, beta, y, sum, mean, rstd))
+    _check(lib().fast_layer_norm_fwd(n, D, dtype, _ptr(x), _ptr(res), _ptr(gamma), _ptr(beta), eps,
+                                     _ptr(y), _ptr(sum), _ptr(mean), _ptr(rstd), _stream(stream)))
+
+
+def fast_layer_norm_bwd_workspace(n: int, D: int) -> int:
+    return lib().fast_layer_norm_bwd_workspace(n, D)
+
+
+def fast_layer_norm_bwd(n, D, dtype, h, gamma, mean, rstd, dy, dsum, dx, dgamma, dbeta, ws,
+                        ws_bytes, stream=None):
+    _resident((h, gamma, mean, rstd, dy, dsum, dx, dgamma, dbeta, ws))
+    _check(lib().fast_layer_norm_bwd(n, D, dtype, _ptr(h), _ptr(gamma), _ptr(mean), _ptr(rstd),
+                                     _ptr(dy), _ptr(dsum), _ptr(dx), _ptr(dgamma), _ptr(dbeta),
+                                     _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def fast_rotary_fwd(n, H, dh, dtype, x, ldx, pos, axes, axis, omega, pairs, interleaved, y, ldy,
+                    stream=None):
+    """x and y may be views whose rows are ldx and ldy elements apart."""
+    _resident((pos, axis, omega), (x, y))
+    _check(lib().fast_rotary_fwd(n, H, dh, dtype, _ptr(x), ldx, _ptr(pos), axes, _ptr(axis),
+                                 _ptr(omega), pairs, int(interleaved), _ptr(y), ldy,
+                                 _stream(stream)))
+
+
+def fast_rotary_bwd(n, H, dh, dtype, dy, lddy, pos, axes, axis, omega, pairs, interleaved, dx, lddx,
+                    stream=None):
+    _resident((pos, axis, omega), (dy, dx))
+    _check(lib().fast_rotary_bwd(n, H, dh, dtype, _ptr(dy), lddy, _ptr(pos), axes, _ptr(axis),
+                                 _ptr(omega), pairs, int(interleaved), _ptr(dx), lddx,
+                                 _stream(stream)))
+
+
+def fast_cache_row_bytes(parts: int, width: int, format: int) -> int:
+    return lib().fast_cache_row_bytes(parts, width, format)
+
+
+def fast_cache_write_workspace(n: int, cache_rows: int) -> int:
+    return lib().fast_cache_write_workspace(n, cache_rows)
+
+
+def fast_cache_write(ids, n, id_bound, slot_map, parts, width, dtype, src, format, cache, cache_rows,
+                     distinct, ws=None, ws_bytes=0, stream=None):
+    _resident((ids, slot_map, src, cache, ws))
+    _check(lib().fast_cache_write(_ptr(ids), n, id_bound, _ptr(slot_map), parts, width, dtype,
+                                  _ptr(src), format, _ptr(cache), cache_rows, int(distinct),
+                                  _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def fast_cache_gather(ids, n, id_bound, slot_map, parts, width, format, cache, cache_rows, dtype,
+                      rows, stream=None):
+    _resident((ids, slot_map, cache, rows))
+    _check(lib().fast_cache_gather(_ptr(ids), n, id_bound, _ptr(slot_map), parts, width, format,
+                                   _ptr(cache), cache_rows, dtype, _ptr(rows), _stream(stream)))
+
+
+def fast_edge_attention_cached_workspace(num_dst: int, num_edges: int, H: int, dh: int) -> int:
+    return lib().fast_edge_attention_cached_workspace(num_dst, num_edges, H, dh)
+
+
+def fast_edge_attention_fwd_cached(g: TCSR, H, dh, dtype, Q, ids, id_bound, slot_map, format, cache,
+                                   cache_rows, scale, neg_slope, out, lse, ws, ws_bytes,
+                                   stream=None):
+    _resident((Q, ids, slot_map, cache, out, lse, ws))
+    _check(lib().fast_edge_attention_fwd_cached(C.byref(g), H, dh, dtype, _ptr(Q), _ptr(ids),
+                                                id_bound, _ptr(slot_map), format, _ptr(cache),
+                                                cache_rows, scale, neg_slope, _ptr(out),
+                                                _ptr(lse), _ptr(ws), ws_bytes, _stream(stream)))

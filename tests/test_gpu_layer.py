@@ -1,0 +1,256 @@
+"""GPU parity of layer norm and rotary positions against their plain 64-bit
+definitions, through the C ABI.  Tolerances are rounding bounds written beside
+each comparison (U = 2^-24, half a step of fp32)."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2607_05095_amd as fast
+from tests import plain64 as p64
+from tests.parity import tdtype, to_dev
+from tests.plain64 import HALF, U
+
+pytestmark = pytest.mark.gpu
+
+DT = {"f32": fast.F32, "bf16": fast.BF16}
+
+
+def rand(shape, dt, seed, offset=0.0, scale=1.0):
+    """A device tensor of the storage type and the values it holds, in 64 bits."""
+    r = np.random.default_rng(seed)
+    t = torch.from_numpy((r.normal(size=shape) * scale + offset).astype(np.float32)).to(tdtype(dt))
+    return t.cuda(), t.double().numpy()
+
+
+def host(t):
+    return t.detach().double().cpu().numpy()
+
+
+def within(x, ref, tol, what):
+    x = host(x)
+    assert x.shape == ref.shape, what
+    bad = ~(np.abs(x - ref) <= tol)
+    assert not bad.any(), (what, int(bad.sum()), bad.size, float(np.abs(x - ref).max()),
+                           [(tuple(i), x[tuple(i)], ref[tuple(i)]) for i in np.argwhere(bad)[:3]])
+
+
+# ------------------------------------------------------------------ layer norm
+def norm_bounds(h, mu, r, gamma, beta, y, dt):
+    """A sum of D fp32 terms takes at most 32 additions in a lane and 10 across lanes:
+    45 U of the terms' mean magnitude, so 45 U M in the mean, M the largest |h| (3 U for
+    rounding h itself); the sum of squares twice the relative error of its terms plus 45 U."""
+    M = np.abs(h).max(1, keepdims=True)
+    xh = np.abs((h - mu[:, None]) * r[:, None])
+    c = 50 * U * M * r[:, None]                  # error of xhat from the mean
+    tol = np.abs(gamma) * (c + xh * (c * c + 30 * U)) + 4 * U * (np.abs(y) + np.abs(beta))
+    return tol + HALF[dt] * np.abs(y)
+
+
+SHAPES = [(1, 1), (3, 1), (7, 2), (5, 3), (4, 7), (33, 8), (600, 100), (9, 64), (257, 172), (31, 129),
+          (5, 500), (3, 1023), (4, 2048), (3, 2049), (2, 4096), (2, 5001), (2, 8192), (1, 8191)]
+
+
+@pytest.mark.parametrize("n,D", SHAPES)
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("res", [False, True])
+def test_layer_norm_fwd(n, D, dt, res):
+    print(f"[layer] norm fwd n={n} D={D} {dt} res={res}", flush=True)
+    x, x64 = rand((n, D), dt, 1, offset=0.5)
+    r, r64 = rand((n, D), dt, 2) if res else (None, 0.0)
+    ga, g64 = rand((D,), "f32", 3)
+    be, b64 = rand((D,), "f32", 4)
+    y = torch.full((n + 1, D), 7.0, dtype=tdtype(dt), device="cuda")
+    h = torch.full((n + 1, D), 7.0, dtype=tdtype(dt), device="cuda") if res else None
+    mean, rstd = torch.zeros(2, n + 1, device="cuda").unbind(0)
+    fast.fast_layer_norm_fwd(n, D, DT[dt], x, r, ga, be, 1e-5, y, h, mean, rstd)
+    h64 = torch.from_numpy(x64 + r64).to(tdtype(dt)).double().numpy()
+    ref, mu, rs = p64.layer_norm(h64, g64, b64, 1e-5)
+    within(y[:n], ref, norm_bounds(h64, mu, rs, g64, b64, ref, dt), "y")
+    M = np.abs(h64).max(1)
+    within(mean[:n], mu, 50 * U * M, "mean")
+    within(rstd[:n], rs, rs * (40 * U + (50 * U * M * rs) ** 2), "rstd")
+    if res:
+        np.testing.assert_array_equal(host(h[:n]), h64)
+        assert (h[n] == 7).all()
+    assert (y[n] == 7).all() and float(mean[n]) == 0 and float(rstd[n]) == 0
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_layer_norm_far_from_zero_and_without_weights(dt):
+    # rows whose mean is 1000 times their spread; ones and zeros for NULL weights; constant rows
+    x, x64 = rand((40, 100), dt, 5, offset=1000.0)
+    x[3] = 2.5
+    x64[3] = 2.5
+    y = torch.empty_like(x)
+    fast.fast_layer_norm_fwd(40, 100, DT[dt], x, None, None, None, 1e-5, y)
+    ref, mu, rs = p64.layer_norm(x64, 1.0, 0.0, 1e-5)
+    within(y, ref, norm_bounds(x64, mu, rs, 1.0, 0.0, ref, dt), "y")
+    assert (host(y)[3] == 0).all()
+    # in place
+    z = x.clone()
+    fast.fast_layer_norm_fwd(40, 100, DT[dt], z, None, None, None, 1e-5, z)
+    assert torch.equal(z, y)
+
+
+def test_layer_norm_nonfinite_rows_stay_in_their_row():
+    x, x64 = rand((64, 36), "f32", 6)
+    x[5, 7] = float("inf")
+    x[9, 0] = float("nan")
+    y = torch.empty_like(x)
+    fast.fast_layer_norm_fwd(64, 36, fast.F32, x, None, None, None, 1e-5, y)
+    nan = torch.isnan(y).any(1).cpu().numpy()
+    assert nan[5] and nan[9] and nan.sum() == 2
+
+
+@pytest.mark.parametrize("n,D", SHAPES + [(20000, 36), (70001, 4), (9000, 2), (3000, 500)])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("dsum", [False, True])
+def test_layer_norm_bwd(n, D, dt, dsum):
+    print(f"[layer] norm bwd n={n} D={D} {dt} dsum={dsum}", flush=True)
+    h, h64 = rand((n, D), dt, 7, offset=0.3)
+    dy, dy64 = rand((n, D), dt, 8)
+    ds, ds64 = rand((n, D), dt, 9) if dsum else (None, None)
+    ga, g64 = rand((D,), "f32", 10)
+    _, mu, rs = p64.layer_norm(h64, g64, 0.0, 1e-2)
+    mean, rstd = to_dev(mu.astype(np.float32)), to_dev(rs.astype(np.float32))
+    mu, rs = host(mean), host(rstd)               # the inputs, as rounded
+    dx = torch.full((n + 1, D), 7.0, dtype=tdtype(dt), device="cuda")
+    dg, db = torch.full((2, D + 1), 7.0, device="cuda").unbind(0)
+    wsb = fast.fast_layer_norm_bwd_workspace(n, D)
+    ws = torch.empty(wsb + 64, dtype=torch.uint8, device="cuda").fill_(0xAB)
+    fast.fast_layer_norm_bwd(n, D, DT[dt], h, ga, mean, rstd, dy, ds, dx, dg, db, ws, wsb)
+    rx, rg, rb = p64.layer_norm_bwd(h64, g64, mu, rs, dy64, ds64)
+    xh = np.abs((h64 - mu[:, None]) * rs[:, None])
+    Mr = (np.abs(h64).max(1) + np.abs(mu))[:, None] * rs[:, None]
+    g = np.abs(dy64 * g64)
+    m1, m2 = g.mean(1, keepdims=True), (g * xh).mean(1, keepdims=True)
+    tol = U * rs[:, None] * 60 * (g + m1 + (xh + Mr) * (m2 + m1 * Mr)) + 2 * U * np.abs(rx)
+    tol = tol + (U * np.abs(ds64) if dsum else 0) + HALF[dt] * np.abs(rx)
+    within(dx[:n], rx, tol, "dx")
+    # a term carries 4 U Mr |dy| from xhat; at most 32 of them are added in fp32
+    within(dg[:D], rg, U * (40 * np.abs(dy64 * xh).sum(0) + 4 * (np.abs(dy64) * Mr).sum(0)) + U * np.abs(rg), "dgamma")
+    within(db[:D], rb, U * 33 * np.abs(dy64).sum(0) + U * np.abs(rb), "dbeta")
+    assert (dx[n] == 7).all() and float(dg[D]) == 7 and float(db[D]) == 7 and (ws[wsb:] == 0xAB).all()
+    # one gradient only, none, and dx in dy's place give the same bits
+    dg2, dx2 = torch.empty(D, device="cuda"), dy.clone()
+    fast.fast_layer_norm_bwd(n, D, DT[dt], h, ga, mean, rstd, dx2, ds, dx2, dg2, None, ws, wsb)
+    assert torch.equal(dg2, dg[:D]) and torch.equal(dx2, dx[:n])
+    fast.fast_layer_norm_bwd(n, D, DT[dt], h, ga, mean, rstd, dy, ds, dx2, None, None, None, 0)
+    assert torch.equal(dx2, dx[:n])
+
+
+def test_layer_norm_bwd_without_rows_zeroes_the_weight_gradients():
+    dg, db = torch.full((2, 12), 7.0, device="cuda").unbind(0)
+    wsb = fast.fast_layer_norm_bwd_workspace(0, 12)
+    ws = torch.empty(wsb, dtype=torch.uint8, device="cuda")
+    fast.fast_layer_norm_bwd(0, 12, fast.F32, None, None, None, None, None, None, None, dg, db, ws, wsb)
+    assert (dg == 0).all() and (db == 0).all()
+
+
+# ------------------------------------------------------------------ rotary
+ROT = [  # n, H, dh, pairs, axes
+    (1, 1, 2, 1, 1), (3, 1, 3, 1, 2), (600, 2, 50, 25, 1), (65, 2, 50, 24, 3), (77, 4, 32, 16, 1),
+    (130, 8, 128, 64, 3), (5, 3, 7, 2, 2), (64, 1, 256, 128, 4), (33, 5, 43, 21, 1), (9, 64, 16, 8, 2),
+    (257, 2, 20, 0, 1)]
+
+
+@pytest.mark.parametrize("n,H,dh,pairs,axes", ROT)
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_rotary(n, H, dh, pairs, axes, inter, dt):
+    print(f"[layer] rotary n={n} H={H} dh={dh} pairs={pairs} axes={axes} inter={inter} {dt}", flush=True)
+    r = np.random.default_rng(n + dh)
+    x, x64 = rand((n, H, dh), dt, 11)
+    pos = (r.uniform(-1, 1, (n, axes)) * 10.0 ** r.uniform(0, 7, (n, axes))).astype(np.float32)
+    ax = r.integers(0, axes, max(pairs, 1)).astype(np.int32)[:pairs]
+    om = (10.0 ** r.uniform(-6, 0.3, max(pairs, 1))).astype(np.float32)[:pairs]
+    F = H * dh
+    dpos, dax, dom = to_dev(pos), to_dev(ax), to_dev(om)
+
+    def bound(ref, sign):
+        # sine and cosine within 2e-7, two products and a sum in fp32
+        turned = np.abs(p64.rotary(np.abs(x64), np.zeros_like(pos, np.float64), ax, om, pairs, inter))
+        a = np.arange(pairs) * (2 if inter else 1)
+        b = a + (1 if inter else pairs)
+        both = turned.copy()
+        both[..., a] = both[..., b] = turned[..., a] + turned[..., b]
+        t = both * (2e-7 + 3 * U)
+        t[..., 2 * pairs:] = 0
+        return t + HALF[dt] * np.abs(ref) * (dt == "bf16")
+
+    for sign, f in ((1.0, fast.fast_rotary_fwd), (-1.0, fast.fast_rotary_bwd)):
+        ref = p64.rotary(x64, pos.astype(np.float64), ax, om.astype(np.float64), pairs, inter, sign)
+        y = torch.full((n + 1, H, dh), 7.0, dtype=tdtype(dt), device="cuda")
+        f(n, H, dh, DT[dt], x, F, dpos, axes, dax, dom, pairs, inter, y, F)
+        within(y[:n], ref, bound(ref, sign), "y")
+        assert (y[n] == 7).all()
+        # the K half of packed rows, in place; V stays as it was
+        kv = torch.full((n, 2, H, dh), 3.0, dtype=tdtype(dt), device="cuda")
+        kv[:, 0] = x
+        f(n, H, dh, DT[dt], kv, 2 * F, dpos, axes, dax, dom, pairs, inter, kv, 2 * F)
+        assert torch.equal(kv[:, 0], y[:n]) and (kv[:, 1] == 3).all()
+        # from the K half into the V half
+        kv[:, 0] = x
+        f(n, H, dh, DT[dt], kv, 2 * F, dpos, axes, dax, dom, pairs, inter, kv[:, 1], 2 * F)
+        assert torch.equal(kv[:, 0], x) and torch.equal(kv[:, 1], y[:n])
+
+
+def test_rotary_axis_out_of_range_null_axis_and_infinite_position():
+    x, x64 = rand((4, 1, 8), "f32", 12)
+    pos = to_dev(np.array([[1.0, 2.0], [3.0, 4.0], [np.inf, 1.0], [0.0, 0.0]], np.float32))
+    om = to_dev(np.array([1.0, 0.5, 2.0, 0.0], np.float32))
+    y, z, w = torch.empty(3, 4, 1, 8, device="cuda").unbind(0)
+    fast.fast_rotary_fwd(4, 1, 8, 0, x, 8, pos, 2, to_dev(np.array([-5, 9, 0, 1], np.int32)), om, 4, 0, y, 8)
+    fast.fast_rotary_fwd(4, 1, 8, 0, x, 8, pos, 2, to_dev(np.array([0, 1, 0, 1], np.int32)), om, 4, 0, z, 8)
+    assert torch.equal(y.nan_to_num(9), z.nan_to_num(9))
+    fast.fast_rotary_fwd(4, 1, 8, 0, x, 8, pos[:, :1].contiguous(), 1, None, om, 4, 0, z, 8)
+    fast.fast_rotary_fwd(4, 1, 8, 0, x, 8, pos, 2, to_dev(np.zeros(4, np.int32)), om, 4, 0, w, 8)
+    assert torch.equal(z.nan_to_num(9), w.nan_to_num(9))
+    assert torch.isnan(z[2, 0, 0]) and not torch.isnan(z[[0, 1, 3]]).any() and torch.equal(z[3], x[3])
+
+
+# ------------------------------------------------------------------ streams, graphs, several at once
+def test_norm_and_rotary_on_another_stream_and_in_a_graph():
+    n, D, H, dh = 3000, 100, 2, 50
+    x, _ = rand((n, D), "f32", 13)
+    dy, _ = rand((n, D), "f32", 14)
+    ga, _ = rand((D,), "f32", 15)
+    pos = torch.rand(n, 1, device="cuda") * 1000
+    om = torch.rand(25, device="cuda")
+    wsb = fast.fast_layer_norm_bwd_workspace(n, D)
+
+    def buffers():
+        b = dict(y=torch.zeros(n, D, device="cuda"), z=torch.zeros(n, H, dh, device="cuda"),
+                 dx=torch.zeros(n, D, device="cuda"), mean=torch.zeros(n, device="cuda"),
+                 rstd=torch.zeros(n, device="cuda"), dg=torch.zeros(D, device="cuda"),
+                 db=torch.zeros(D, device="cuda"), ws=torch.zeros(wsb, dtype=torch.uint8, device="cuda"))
+        return b
+
+    def step(b, stream=None):
+        fast.fast_layer_norm_fwd(n, D, 0, x, None, ga, None, 1e-5, b["y"], None, b["mean"], b["rstd"], stream)
+        fast.fast_rotary_fwd(n, H, dh, 0, b["y"], D, pos, 1, None, om, 25, 1, b["z"], D, stream)
+        fast.fast_layer_norm_bwd(n, D, 0, x, ga, b["mean"], b["rstd"], dy, None, b["dx"], b["dg"], b["db"],
+                                 b["ws"], wsb, stream)
+
+    want = buffers()
+    step(want)
+    torch.cuda.synchronize()
+    names = ("y", "z", "dx", "dg", "db")
+    got = buffers()
+    st = torch.cuda.Stream()
+    st.wait_stream(torch.cuda.current_stream())
+    step(got, st)
+    st.synchronize()
+    assert all(torch.equal(got[k], want[k]) for k in names)
+    cap = buffers()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(cap)
+    for k in range(3):
+        for b in cap.values():
+            b.zero_()
+        step(got)                                  # eager work between the replays
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(cap[m], want[m]) for m in names), k
