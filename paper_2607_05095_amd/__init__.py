@@ -192,10 +192,13 @@ def _resident(dense=(), strided=()):
     """Tensors of a call live on the current device, and those without a row
     stride of their own are contiguous; raises otherwise."""
     import torch
+    dev = None
     for t in (*dense, *strided):
         if t is None or isinstance(t, int):
             continue
-        if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        if dev is None and t.is_cuda:
+            dev = torch.cuda.current_device()
+        if t.get_device() != dev:
             raise FastError(1, f"tensor on {t.device}, not on the current GPU")
     for t in dense:
         if t is not None and not isinstance(t, int) and not t.is_contiguous():

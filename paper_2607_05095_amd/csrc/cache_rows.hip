@@ -80,7 +80,7 @@ __global__ void __launch_bounds__(CR_THREADS) k_cache_write(CacheArgs a) {
     o = __float_as_uint(dpp_quad_xor2(__uint_as_float(m)));
     m = m > o ? m : o;
     const uint32_t sb = mx_scale_byte<FMT>(__uint_as_float(m));
-    MxPiece<FMT> p;
+    MxPiece<FMT, 8> p;
     if (sb == 255u) p.zero();
     else p.pack(mx_scale(sb), x);
     uint8_t* rec = a.cache + slot * a.rec.stride;
@@ -102,7 +102,7 @@ __global__ void __launch_bounds__(CR_THREADS) k_cache_gather(CacheArgs a) {
     const int64_t slot = mx_slot(a.ids[i], a.id_bound, a.slot_map, a.cache_rows);
     if (slot < 0) continue;
     const uint8_t* rec = a.cache_in + slot * a.rec.stride;
-    MxPiece<FMT> p;
+    MxPiece<FMT, 8> p;
     p.load(rec + part * a.rec.code_bytes + c * PB);
     const uint32_t sb = rec[a.rec.scale_off + part * a.rec.groups + (c >> 2)];
     float x[8];
