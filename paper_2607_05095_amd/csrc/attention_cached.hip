@@ -13,12 +13,18 @@
 // owns one, its 64 / L groups of lanes take the edges in turn, and their
 // results are joined by lane exchanges at the end.
 //
-// Segments longer than `cap` edges (a power of two) are cut at the multiples of cap in
-// the block's edge order.  A workgroup per cell between two multiples looks up the
-// long segment that comes in from the left and the one that goes out to
-// the right with a 64-way search of the offsets, and leaves at once where there is
-// none.  Its waves split the piece, join in LDS and write (maximum, sum,
-// accumulators) to the workspace; a second launch joins a segment's pieces in order.
+// Segments longer than `cap` edges (a power of two) are left to a second launch, which
+// cuts them at the multiples of cap in the block's edge order.  Every multiple belongs
+// to one segment, whose lanes note in the first launch whether it is a long one.  A
+// workgroup of the second launch takes the piece between two multiples of the long
+// segment that comes in from the left, then of the one that goes out to the
+// right: its waves split the piece, join in LDS and write (maximum, sum,
+// accumulators) to the workspace.  A third launch joins a segment's pieces in their
+// order.  (Joining in the workgroup that finishes a segment's last piece needs an
+// agent-wide fence per piece, which writes the L2 back: 72 us against 20 for
+// four histories of 100,003 edges.  Looking for the long segments with a search of the
+// offsets, in the first launch, cost 30 us of 190 in registers and waves for a
+// block of 264,000 short segments.)
 #include "attention.h"
 #include "mx.h"
 #include "rows.h"
@@ -28,6 +34,8 @@ namespace fast {
 constexpr int CA_THREADS = 256, CA_WAVES = CA_THREADS / 64;
 constexpr int CA_ROWS = 4;           // records in flight per lane
 constexpr int CA_AHEAD = 2;          // places that a lane looks up at once
+constexpr int CA_SHIFT = 8, CA_SHIFT_MAX = 10;   // cap = 256 .. 1024
+constexpr int CA_CELLS = 1024;       // workgroups of the second launch, at most: 4 per CU (a power of two)
 
 struct CaArgs {
   int64_t N, E;
@@ -35,8 +43,8 @@ struct CaArgs {
   int H, dh;
   int lph, L;                        // lanes per head, per record (powers of two up to 64)
   int shift;                         // cap = 1 << shift
-  int64_t cells, cell_blocks;        // cells of cap edges (0 where no segment can be long), their workgroups
-  int cells_per_block;               // 1 or CA_WAVES: cells b, b + cell_blocks, ...
+  int64_t cells;                     // cells between multiples of cap, 0 where no segment can be long
+  int64_t rounds;                    // cells per workgroup of the other launches: b, b + CA_CELLS, ...
   const int64_t* ids;
   int64_t id_bound;
   const int32_t* slot_map;
@@ -48,27 +56,12 @@ struct CaArgs {
   void* out;
   float* lse;
   float* part;                       // [2 per cell][H][dh + 2]
-  int32_t* starts;                   // [cells] the long segment that starts in a cell, or -1
+  int32_t* mark;                     // [min(cells, CA_CELLS)][rounds]: cell m's at ca_mark_at(m): the long segment that holds edge m cap, or -1
 };
 
 __device__ __forceinline__ void ca_segment(const CaArgs& a, int64_t v, int64_t& s, int64_t& t) {
   s = clamp64(a.off[v], 0, a.E);
   t = clamp64(a.off[v + 1], s, a.E);
-}
-
-// Last v with off[v] <= x (off[0] is taken as 0): every round the lanes try 64
-// equally spaced offsets.
-__device__ __forceinline__ int64_t ca_find(const CaArgs& a, int64_t x) {
-  const int lane = threadIdx.x & 63;
-  int64_t lo = 0, hi = a.N;
-  while (hi - lo > 1) {
-    const int64_t step = (hi - lo + 63) >> 6, i = lo + lane * step;
-    const bool le = lane == 0 || (i < hi && a.off[i] <= x);
-    const int last = 63 - __builtin_clzll(__ballot(le));
-    lo += last * step;
-    hi = hi < lo + step ? hi : lo + step;
-  }
-  return lo;
 }
 
 __device__ __forceinline__ float ca_pow2(float x, float m) {   // 2^(x - m), 0 for x = -inf
@@ -118,31 +111,43 @@ __device__ __forceinline__ void ca_init(const CaArgs& a, int64_t v, CaLane<VE>& 
 // rec[] is the record's byte in a cache of less than 4 GiB, so that an address is a
 // base that all lanes share plus 32 bits, or (BIG) its slot.
 constexpr uint32_t CA_NONE = 0xffffffffu;
+
+// The codes in flight.  They are zeroed once, for the lanes that hold none; a record
+// that is not there leaves its place as it was, and nothing uses it.
+template <int FMT, int VE>
+struct CaCodes {
+  MxPiece<FMT, VE> k[CA_ROWS], v[CA_ROWS];
+  uint32_t ks[CA_ROWS], vs[CA_ROWS];
+  __device__ void zero() {
+#pragma unroll
+    for (int i = 0; i < CA_ROWS; ++i) {
+      k[i].zero();
+      v[i].zero();
+      ks[i] = vs[i] = 127u;
+    }
+  }
+};
 template <int FMT, int VE, int LPH, bool BIG>
-__device__ __forceinline__ void ca_fold(const CaArgs& a, const uint32_t (&rec)[CA_ROWS], CaLane<VE>& c) {
-  MxPiece<FMT, VE> kc[CA_ROWS], vc[CA_ROWS];
-  uint32_t kb[CA_ROWS], vb[CA_ROWS];
+__device__ __forceinline__ void ca_fold(const CaArgs& a, const uint32_t (&rec)[CA_ROWS], CaLane<VE>& c,
+                                        CaCodes<FMT, VE>& r) {
   const uint8_t* kbase = a.cache;
   const uint8_t* vbase = a.cache + a.H * a.rec.code_bytes;
   const uint8_t* sbase = a.cache + a.H * a.rec.groups;
 #pragma unroll
   for (int i = 0; i < CA_ROWS; ++i) {
-    kc[i].zero();
-    vc[i].zero();
-    kb[i] = vb[i] = 127u;
     if (rec[i] != CA_NONE && c.mine) {
       if constexpr (BIG) {
         const uint64_t o = uint64_t(rec[i]) * uint32_t(a.rec.stride);
-        kc[i].load(kbase + (o + c.code));
-        vc[i].load(vbase + (o + c.code));
-        kb[i] = kbase[o + c.scale];
-        vb[i] = sbase[o + c.scale];
+        r.k[i].load(kbase + (o + c.code));
+        r.v[i].load(vbase + (o + c.code));
+        r.ks[i] = kbase[o + c.scale];
+        r.vs[i] = sbase[o + c.scale];
       } else {
         const uint32_t o = rec[i] + c.code, s = rec[i] + c.scale;
-        kc[i].load(kbase + o);
-        vc[i].load(vbase + o);
-        kb[i] = kbase[s];
-        vb[i] = sbase[s];
+        r.k[i].load(kbase + o);
+        r.v[i].load(vbase + o);
+        r.ks[i] = kbase[s];
+        r.vs[i] = sbase[s];
       }
     }
   }
@@ -150,15 +155,15 @@ __device__ __forceinline__ void ca_fold(const CaArgs& a, const uint32_t (&rec)[C
 #pragma unroll
   for (int i = 0; i < CA_ROWS; ++i) {
     t[i] = -INFINITY;
-    if (i > 0 && !__any(rec[i] != CA_NONE)) continue;    // no lane has a record here
-    float k[VE], d = 0.f;
-    kc[i].unpack(mx_scale(kb[i]), k);
+    if (rec[i] != CA_NONE) {           // all lanes of a record alike
+      float k[VE], d = 0.f;
+      r.k[i].unpack(mx_scale(r.ks[i]), k);
 #pragma unroll
-    for (int j = 0; j < VE; ++j) d = fmaf(c.q[j], k[j], d);
-    if constexpr (LPH > 0) d = group_sum_ct<LPH>(d);
-    else d = group_sum(d, a.lph);
-    d *= d > 0.f ? 1.f : a.slope;
-    t[i] = rec[i] != CA_NONE ? d : -INFINITY;
+      for (int j = 0; j < VE; ++j) d = fmaf(c.q[j], k[j], d);
+      if constexpr (LPH > 0) d = group_sum_ct<LPH>(d);
+      else d = group_sum(d, a.lph);
+      t[i] = d * (d > 0.f ? 1.f : a.slope);
+    }
     mn = fmaxf(mn, t[i]);
   }
   const float corr = ca_pow2(c.mx, mn), ref = mn == -INFINITY ? 0.f : mn;
@@ -168,13 +173,14 @@ __device__ __forceinline__ void ca_fold(const CaArgs& a, const uint32_t (&rec)[C
   for (int j = 0; j < VE; ++j) c.acc[j] *= corr;
 #pragma unroll
   for (int i = 0; i < CA_ROWS; ++i) {
-    if (i > 0 && !__any(rec[i] != CA_NONE)) continue;
-    const float w = __builtin_amdgcn_exp2f(t[i] - ref);
-    float x[VE];
-    vc[i].unpack(mx_scale(vb[i]), x);
-    c.Z += w;
+    if (rec[i] != CA_NONE) {
+      const float w = __builtin_amdgcn_exp2f(t[i] - ref);
+      float x[VE];
+      r.v[i].unpack(mx_scale(r.vs[i]), x);
+      c.Z += w;
 #pragma unroll
-    for (int j = 0; j < VE; ++j) c.acc[j] = fmaf(w, x[j], c.acc[j]);
+      for (int j = 0; j < VE; ++j) c.acc[j] = fmaf(w, x[j], c.acc[j]);
+    }
   }
 }
 
@@ -192,6 +198,8 @@ __device__ __forceinline__ uint32_t ca_rec(const CaArgs& a, int64_t e, int64_t e
 template <int FMT, int VE, int LPH, bool BIG>
 __device__ __forceinline__ void ca_wave(const CaArgs& a, int64_t e0, int64_t e1, CaLane<VE>& c) {
   const int lane = threadIdx.x & 63, L = a.L, GR = 64 / L, gi = lane / L;
+  CaCodes<FMT, VE> codes;
+  codes.zero();
   for (int64_t base = e0; base < e1; base += 64) {
     const uint32_t my = ca_rec<BIG>(a, base + lane, e1);
     const int n = int(e1 - base < 64 ? e1 - base : 64);
@@ -203,7 +211,7 @@ __device__ __forceinline__ void ca_wave(const CaArgs& a, int64_t e0, int64_t e1,
         const uint32_t o = __shfl(my, r & 63);
         rec[i] = r < 64 ? o : CA_NONE;
       }
-      ca_fold<FMT, VE, LPH, BIG>(a, rec, c);
+      ca_fold<FMT, VE, LPH, BIG>(a, rec, c, codes);
     }
   }
   for (int o = L; o < 64; o *= 2) {
@@ -269,69 +277,45 @@ __device__ __forceinline__ void ca_piece(const CaArgs& a, int64_t v, int64_t e0,
   __syncthreads();                     // before the next piece of this workgroup
 }
 
-struct CaFound {
-  int64_t v, e0, e1, slot;             // slot < 0: no piece
-};
+// Where the mark of cell m is: the cells of a workgroup lie side by side.
+__device__ __forceinline__ int64_t ca_mark_at(const CaArgs& a, int64_t m) {
+  return (m & (CA_CELLS - 1)) * a.rounds + m / CA_CELLS;
+}
+
+// What the other launches read: for every multiple of cap inside segment v, whether
+// it is long.  The `n` lanes of the segment share the work.
+__device__ __forceinline__ void ca_mark(const CaArgs& a, int64_t v, int64_t s, int64_t t, int lane, int n) {
+  if (s == t || blockIdx.y != 0) return;
+  const int64_t cap = int64_t(1) << a.shift;
+  const int64_t first = (s + cap - 1) >> a.shift, last = (t - 1) >> a.shift;
+  for (int64_t m = first + lane; m <= last; m += n) a.mark[ca_mark_at(a, m)] = t - s > cap ? int32_t(v) : -1;
+}
 
 // WAVE: a wave per segment, else L lanes per segment.
 template <typename T, int FMT, int VE, int LPH, bool BIG, bool WAVE>
 __global__ void __launch_bounds__(CA_THREADS) k_attn_cached(CaArgs a) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t cap = int64_t(1) << a.shift;
-  if (int64_t(blockIdx.x) < a.cell_blocks) {
-    __shared__ float s_acc[CA_WAVES][VE + 2][64];
-    __shared__ CaFound s_found[2 * CA_WAVES];
-    // each wave looks into one of this workgroup's cells
-    const int64_t m = blockIdx.x + wave * a.cell_blocks, x = m << a.shift, y = x + cap;
-    const bool look = wave < a.cells_per_block && m < a.cells;
-    CaFound l = {0, 0, 0, -1}, r = l;
-    if (look) {
-      int64_t s, t, start = -1;
-      l.v = ca_find(a, x);             // comes in from the left, or starts at x
-      ca_segment(a, l.v, s, t);
-      if (s <= x && x < t && t - s > cap) {
-        l = {l.v, x, t < y ? t : y, s == x ? 2 * m + 1 : 2 * m};
-        if (s == x) start = l.v;
-      }
-      if (y < a.E) {
-        r.v = ca_find(a, y);           // goes out to the right
-        ca_segment(a, r.v, s, t);
-        if (x < s && s < y && y < t && t - s > cap) {
-          r = {r.v, s, y, 2 * m + 1};
-          start = r.v;
-        }
-      }
-      if (lane == 0 && blockIdx.y == 0) a.starts[m] = int32_t(start);
-    }
-    if (lane == 0) {
-      s_found[2 * wave] = l;
-      s_found[2 * wave + 1] = r;
-    }
-    __syncthreads();
-    for (int k = 0; k < 2 * a.cells_per_block; ++k) {
-      const CaFound f = s_found[k];
-      if (f.slot >= 0) ca_piece<T, FMT, VE, LPH, BIG>(a, f.v, f.e0, f.e1, f.slot, s_acc);
-    }
-    return;
-  }
-  const int64_t block = int64_t(blockIdx.x) - a.cell_blocks;
   CaLane<VE> c;
   int64_t s, t;
   if constexpr (WAVE) {
-    const int64_t v = block * CA_WAVES + wave;
+    const int64_t v = int64_t(blockIdx.x) * CA_WAVES + wave;
     if (v >= a.N) return;
     ca_segment(a, v, s, t);
-    if (t - s > cap) return;           // in pieces
+    if (a.cells > 0) ca_mark(a, v, s, t, lane, 64);
+    if (t - s > int64_t(1) << a.shift) return;   // in pieces
     ca_init<T, FMT, VE, LPH>(a, v, c);
     ca_wave<FMT, VE, LPH, BIG>(a, s, t, c);
     if (lane < a.L) ca_store<T, VE>(a, v, c);
   } else {
     const int L = a.L, gl = lane & (L - 1), g0 = lane - gl;
-    const int64_t v = block * (CA_THREADS / L) + threadIdx.x / L;
+    const int64_t v = int64_t(blockIdx.x) * (CA_THREADS / L) + threadIdx.x / L;
     if (v >= a.N) return;
     ca_segment(a, v, s, t);
-    if (t - s > cap) return;
+    if (a.cells > 0) ca_mark(a, v, s, t, gl, L);
+    if (t - s > int64_t(1) << a.shift) return;
     ca_init<T, FMT, VE, LPH>(a, v, c);
+    CaCodes<FMT, VE> codes;
+    codes.zero();
     for (int64_t base = s; base < t; base += CA_AHEAD * L) {   // CA_AHEAD places per lane at a time
       uint32_t my[CA_AHEAD];
 #pragma unroll
@@ -346,7 +330,7 @@ __global__ void __launch_bounds__(CA_THREADS) k_attn_cached(CaArgs a) {
             const uint32_t o = __shfl(my[k], g0 + ((r0 + i) & (L - 1)));
             rec[i] = r0 + i < n ? o : CA_NONE;
           }
-          ca_fold<FMT, VE, LPH, BIG>(a, rec, c);
+          ca_fold<FMT, VE, LPH, BIG>(a, rec, c, codes);
         }
       }
     }
@@ -354,75 +338,127 @@ __global__ void __launch_bounds__(CA_THREADS) k_attn_cached(CaArgs a) {
   }
 }
 
-// Joins the pieces of the long segments that start in cells b, b + gridDim.x, ...,
-// head blockIdx.y.  Threads over a segment's pieces find the maximum; then,
-// CJ_THREADS pieces at a time, one thread per piece forms its weight, and threads
-// (element, every slices-th piece) add the weighted accumulators.
-constexpr int CJ_THREADS = 256;
+// Joins the n pieces of segment v, which starts in cell m, for head h.  Threads over
+// the pieces find the maximum; then, CA_THREADS pieces at a time, one thread
+// per piece forms its weight, and threads (element, every slices-th piece) add
+// the weighted accumulators.
 template <typename T>
-__global__ void __launch_bounds__(CJ_THREADS) k_attn_cached_join(CaArgs a) {
-  __shared__ float s_red[2][CJ_THREADS / 64];
-  __shared__ float s_w[CJ_THREADS];
-  __shared__ float s_acc[CJ_THREADS];
-  const int h = blockIdx.y, H = a.H, dh = a.dh;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+__device__ __forceinline__ void ca_join(const CaArgs& a, int64_t v, int64_t m, int64_t n, int h) {
+  __shared__ float s_red[2][CA_WAVES];
+  __shared__ float s_w[CA_THREADS];
+  __shared__ float s_sum[CA_THREADS];
+  const int H = a.H, dh = a.dh, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int cols = 1;                        // the elements of a head, padded to a power of two
   while (cols < dh) cols *= 2;
-  const int slices = CJ_THREADS / cols, col = threadIdx.x & (cols - 1), sl = threadIdx.x / cols;
-  for (int64_t m = blockIdx.x; m < a.cells; m += gridDim.x) {
-    const int64_t v = a.starts[m];
-    if (v < 0) continue;
-    int64_t s, t;
-    ca_segment(a, v, s, t);
-    const int64_t n = ((t - 1) >> a.shift) - m + 1;    // pieces; the first is slot 2m + 1, then 2(m + k)
-    const int64_t step = int64_t(H) * (dh + 2);
-    const float* first = a.part + (2 * m + 1) * step + h * (dh + 2);
-    const float* rest = a.part + 2 * m * step + h * (dh + 2);
-    auto piece = [&](int64_t k) { return k == 0 ? first : rest + 2 * k * step; };
-    float mx = -INFINITY;
-    for (int64_t k = threadIdx.x; k < n; k += CJ_THREADS) mx = fmaxf(mx, piece(k)[0]);
-    for (int o = 1; o < 64; o *= 2) mx = fmaxf(mx, __shfl_xor(mx, o));
-    if (lane == 0) s_red[0][wave] = mx;
-    __syncthreads();
-    for (int w = 0; w < CJ_THREADS / 64; ++w) mx = fmaxf(mx, s_red[0][w]);
-    float Z = 0.f, acc = 0.f;
-    for (int64_t k0 = 0; k0 < n; k0 += CJ_THREADS) {
-      const int c = int(n - k0 < CJ_THREADS ? n - k0 : CJ_THREADS);
-      if (int(threadIdx.x) < c) {
-        const float* p = piece(k0 + threadIdx.x);
-        const float w = ca_pow2(p[0], mx);
-        s_w[threadIdx.x] = w;
-        Z = fmaf(p[1], w, Z);
-      }
-      __syncthreads();
-      if (col < dh) {
-#pragma unroll 8
-        for (int k = sl; k < c; k += slices) acc = fmaf(piece(k0 + k)[2 + col], s_w[k], acc);
-      }
-      __syncthreads();                 // before the next weights
+  const int slices = CA_THREADS / cols, col = threadIdx.x & (cols - 1), sl = threadIdx.x / cols;
+  const int64_t step = int64_t(H) * (dh + 2);
+  const float* first = a.part + (2 * m + 1) * step + h * (dh + 2);   // slot 2m + 1, then 2(m + k)
+  const float* rest = a.part + 2 * m * step + h * (dh + 2);
+  auto piece = [&](int64_t k) { return k == 0 ? first : rest + 2 * k * step; };
+  float mx = -INFINITY;
+  for (int64_t k = threadIdx.x; k < n; k += CA_THREADS) mx = fmaxf(mx, piece(k)[0]);
+  for (int o = 1; o < 64; o *= 2) mx = fmaxf(mx, __shfl_xor(mx, o));
+  if (lane == 0) s_red[0][wave] = mx;
+  __syncthreads();
+  for (int w = 0; w < CA_WAVES; ++w) mx = fmaxf(mx, s_red[0][w]);
+  float Z = 0.f, acc = 0.f;
+  for (int64_t k0 = 0; k0 < n; k0 += CA_THREADS) {
+    const int c = int(n - k0 < CA_THREADS ? n - k0 : CA_THREADS);
+    if (int(threadIdx.x) < c) {
+      const float* p = piece(k0 + threadIdx.x);
+      const float w = ca_pow2(p[0], mx);
+      s_w[threadIdx.x] = w;
+      Z = fmaf(p[1], w, Z);
     }
-    Z = group_sum(Z, 64);
-    if (lane == 0) s_red[1][wave] = Z;
-    s_acc[threadIdx.x] = acc;
     __syncthreads();
-    Z = 0.f;
-    for (int w = 0; w < CJ_THREADS / 64; ++w) Z += s_red[1][w];
-    const bool some = !(Z == 0.f);
-    if (sl == 0 && col < dh) {
-      for (int k = 1; k < slices; ++k) acc += s_acc[k * cols + col];
-      const float o = some ? acc / Z : 0.f;
-      VecIO<T, 1>::store(static_cast<T*>(a.out) + (v * H + h) * dh + col, &o);
+    if (col < dh) {
+#pragma unroll 16
+      for (int k = sl; k < c; k += slices) acc = fmaf(piece(k0 + k)[2 + col], s_w[k], acc);
     }
-    if (a.lse && threadIdx.x == 0) a.lse[v * H + h] = some ? (mx + log2f(Z)) * LN2 : -INFINITY;
-    __syncthreads();                   // before the next segment's sums
+    __syncthreads();                   // before the next weights
+  }
+  Z = group_sum(Z, 64);
+  if (lane == 0) s_red[1][wave] = Z;
+  s_sum[threadIdx.x] = acc;
+  __syncthreads();
+  Z = 0.f;
+  for (int w = 0; w < CA_WAVES; ++w) Z += s_red[1][w];
+  const bool some = !(Z == 0.f);
+  if (sl == 0 && col < dh) {
+    for (int k = 1; k < slices; ++k) acc += s_sum[k * cols + col];
+    const float o = some ? acc / Z : 0.f;
+    VecIO<T, 1>::store(static_cast<T*>(a.out) + (v * H + h) * dh + col, &o);
+  }
+  if (a.lse && threadIdx.x == 0) a.lse[v * H + h] = some ? (mx + log2f(Z)) * LN2 : -INFINITY;
+  __syncthreads();                     // before the next head's sums
+}
+
+// The marks of cells b + i CA_CELLS, and of the cells behind them, for i in [base, base + 64): a
+// lane each, one round trip for all.  Returns the lanes that have one.
+__device__ __forceinline__ uint64_t ca_marks(const CaArgs& a, int64_t base, int32_t& here, int32_t& next) {
+  const int64_t i = base + (threadIdx.x & 63), m = blockIdx.x + i * CA_CELLS;
+  here = i < a.rounds && m < a.cells ? a.mark[ca_mark_at(a, m)] : -1;
+  next = i < a.rounds && m + 1 < a.cells ? a.mark[ca_mark_at(a, m + 1)] : -1;
+  // marks of malformed offsets may be anything
+  if (here >= a.N) here = -1;
+  if (next >= a.N) next = -1;
+  return __ballot(here >= 0 || next >= 0);
+}
+
+// The pieces of long segments in cells b, b + CA_CELLS, ... (so that a long history is
+// spread over the workgroups).
+template <typename T, int FMT, int VE, int LPH, bool BIG>
+__global__ void __launch_bounds__(CA_THREADS) k_attn_cached_long(CaArgs a) {
+  __shared__ float s_acc[CA_WAVES][VE + 2][64];
+  const int64_t cap = int64_t(1) << a.shift;
+  for (int64_t base = 0; base < a.rounds; base += 64) {
+    int32_t here, next;
+    for (uint64_t set = ca_marks(a, base, here, next); set; set &= set - 1) {   // the same in every wave
+      const int i = __builtin_ctzll(set);
+      const int64_t x = (blockIdx.x + (base + i) * CA_CELLS) << a.shift, y = x + cap;
+      int32_t seg[2] = {__builtin_amdgcn_readlane(here, i), __builtin_amdgcn_readlane(next, i)};
+      for (int k = 0; k < 2; ++k) {
+        const int32_t v = seg[k];
+        if (v < 0 || (k == 1 && v == seg[0])) continue;
+        int64_t s, t;
+        ca_segment(a, v, s, t);
+        const int64_t e0 = s > x ? s : x, e1 = t < y ? t : y;
+        if (t - s > cap && e0 < e1)
+          ca_piece<T, FMT, VE, LPH, BIG>(a, v, e0, e1, 2 * (x >> a.shift) + (s >= x ? 1 : 0), s_acc);
+      }
+    }
   }
 }
 
-// Piece length of long segments: a workgroup's 4 waves take 64 edges each, and more
-// where there are pieces enough to fill the chip.
-static int ca_shift(int64_t E) {
-  int s = 8;
-  while (s < 10 && (E >> (s + 1)) >= 8192) ++s;
+// Joins the long segments that start in cells b, b + CA_CELLS, ..., head blockIdx.y: those
+// that hold the next cell's first edge.
+template <typename T>
+__global__ void __launch_bounds__(CA_THREADS) k_attn_cached_join(CaArgs a) {
+  for (int64_t base = 0; base < a.rounds; base += 64) {
+    int32_t here, next;
+    for (uint64_t set = ca_marks(a, base, here, next); set; set &= set - 1) {
+      const int i = __builtin_ctzll(set);
+      const int64_t m = blockIdx.x + (base + i) * CA_CELLS;
+      const int32_t v = __builtin_amdgcn_readlane(next, i);
+      if (v < 0) continue;
+      int64_t s, t;
+      ca_segment(a, v, s, t);
+      if (t - s > (int64_t(1) << a.shift) && s >> a.shift == m)
+        ca_join<T>(a, v, m, ((t - 1) >> a.shift) - m + 1, blockIdx.y);
+    }
+  }
+}
+
+// A wave per segment where they are few, or long; else L lanes each.
+static bool ca_wave_each(int64_t N, int64_t E, int L) {
+  return N <= 4096 || E / N >= 2 * CA_ROWS * (64 / L);
+}
+
+// Piece length: a workgroup's 4 waves take 64 edges each; more where a wave owns a segment
+// (a few lanes would be long over 1024 edges) and there are pieces enough.
+static int ca_shift(int64_t E, bool wave) {
+  int s = CA_SHIFT;
+  while (wave && s < CA_SHIFT_MAX && (E >> (s + 1)) >= 2 * CA_CELLS) ++s;
   return s;
 }
 
@@ -432,10 +468,18 @@ static int pow2_at_least(int x) {
   return p;
 }
 
-template <typename T, int FMT, bool WAVE>
-static void launch_ca(const CaArgs& a, int ve, bool big, dim3 grid, hipStream_t st) {
-#define FAST_CA(V, N, B) \
-  hipLaunchKernelGGL((k_attn_cached<T, FMT, V, N, B, WAVE>), grid, dim3(CA_THREADS), 0, st, a)
+template <typename T, int FMT>
+static void launch_ca(const CaArgs& a, int ve, bool big, bool wave, dim3 grid, dim3 long_grid,
+                      hipStream_t st) {
+#define FAST_CA(V, N, B)                                                                             \
+  do {                                                                                               \
+    if (wave)                                                                                        \
+      hipLaunchKernelGGL((k_attn_cached<T, FMT, V, N, B, true>), grid, dim3(CA_THREADS), 0, st, a);  \
+    else                                                                                             \
+      hipLaunchKernelGGL((k_attn_cached<T, FMT, V, N, B, false>), grid, dim3(CA_THREADS), 0, st, a); \
+    if (a.cells > 0)                                                                                 \
+      hipLaunchKernelGGL((k_attn_cached_long<T, FMT, V, N, B>), long_grid, dim3(CA_THREADS), 0, st, a); \
+  } while (0)
   if (ve == 8) FAST_CA(8, 0, true);
   else if (big) FAST_CA(16, 0, true);
   else if (a.lph == 2) FAST_CA(16, 2, false);
@@ -445,12 +489,12 @@ static void launch_ca(const CaArgs& a, int ve, bool big, dim3 grid, hipStream_t 
 #undef FAST_CA
 }
 
-static int64_t ca_cells(int64_t E) {
-  const int s = ca_shift(E);
-  return E > (int64_t(1) << s) ? ((E - 1) >> s) + 1 : 0;
+// Cells of cap edges; none where no segment can be long.
+static int64_t ca_cells(int64_t E, int shift) {
+  return E > (int64_t(1) << shift) ? ((E - 1) >> shift) + 1 : 0;
 }
-static size_t ca_part_bytes(int64_t E, int H, int dh) {
-  return align_up(size_t(2 * ca_cells(E)) * H * (dh + 2) * sizeof(float), 16);
+static size_t ca_part_bytes(int64_t cells, int H, int dh) {
+  return align_up(size_t(2 * cells) * H * (dh + 2) * sizeof(float), 16);
 }
 
 }  // namespace fast
@@ -462,7 +506,9 @@ extern "C" size_t fast_edge_attention_cached_workspace(int64_t num_dst, int64_t 
   if (num_dst < 0 || num_edges < 0 || num_edges >= (int64_t(1) << 31) || H <= 0 || dh <= 0 || H > 64 ||
       dh > 256 || H * dh > 1024)
     return 0;
-  return ca_part_bytes(num_edges, H, dh) + align_up(size_t(ca_cells(num_edges) + 1) * sizeof(int32_t), 16);
+  // never 0; partial results, then a mark per cell (the shortest pieces have the most)
+  const int64_t cells = ca_cells(num_edges, CA_SHIFT);
+  return ca_part_bytes(cells, H, dh) + align_up(size_t(cells + CA_CELLS) * sizeof(int32_t), 16);
 }
 
 extern "C" fast_status_t fast_edge_attention_fwd_cached(
@@ -503,12 +549,6 @@ extern "C" fast_status_t fast_edge_attention_fwd_cached(
   a.off = g->dst_offsets;
   a.H = H;
   a.dh = dh;
-  a.shift = ca_shift(E);
-  a.cells = ca_cells(E);
-  // Cells are looked at CA_WAVES to a workgroup where there are many, so that the
-  // looking costs little; a workgroup each where they may be all the work.
-  a.cells_per_block = a.cells > 2048 ? CA_WAVES : 1;
-  a.cell_blocks = (a.cells + a.cells_per_block - 1) / a.cells_per_block;
   a.ids = ids;
   a.id_bound = id_bound;
   a.slot_map = slot_map;
@@ -521,7 +561,6 @@ extern "C" fast_status_t fast_edge_attention_fwd_cached(
   a.out = out;
   a.lse = lse;
   a.part = static_cast<float*>(ws);
-  a.starts = reinterpret_cast<int32_t*>(static_cast<char*>(ws) + ca_part_bytes(E, H, dh));
   // 16 codes a lane (fewer instructions per record) where every lane's codes lie in
   // one group: a head's last piece may start 8 codes early, which crosses a
   // group's border where 1 to 8 elements are left past one.
@@ -531,28 +570,30 @@ extern "C" fast_status_t fast_edge_attention_fwd_cached(
   if (hpw > 64 / a.lph) hpw = 64 / a.lph;
   a.L = a.lph * hpw;
   const bool big = a.rec.stride * cache_rows >= (int64_t(1) << 32);
-  // Few segments, or long ones: a wave each.
-  const bool wave = N <= 4096 || E / N >= 2 * CA_ROWS * (64 / a.L);
+  const bool wave = ca_wave_each(N, E, a.L);
+  a.shift = ca_shift(E, wave);
+  a.cells = ca_cells(E, a.shift);
+  a.rounds = (a.cells + CA_CELLS - 1) / CA_CELLS;
+  a.mark = reinterpret_cast<int32_t*>(static_cast<char*>(ws) + ca_part_bytes(a.cells, H, dh));
   const int64_t per = wave ? CA_WAVES : CA_THREADS / a.L;
-  const dim3 grid(uint32_t(a.cell_blocks + (N + per - 1) / per), uint32_t((H + hpw - 1) / hpw));
+  const uint32_t heads = uint32_t((H + hpw - 1) / hpw);
+  const dim3 grid(uint32_t((N + per - 1) / per), heads);
+  const uint32_t cells = uint32_t(a.cells < CA_CELLS ? a.cells : CA_CELLS);
+  const dim3 long_grid(cells, heads);
   hipStream_t st = static_cast<hipStream_t>(stream);
-#define FAST_CAL(T, F)                            \
-  do {                                            \
-    if (wave) launch_ca<T, F, true>(a, ve, big, grid, st);  \
-    else launch_ca<T, F, false>(a, ve, big, grid, st); \
-  } while (0)
   if (dtype == FAST_F32) {
-    if (format == FAST_MXFP8) FAST_CAL(float, FAST_MXFP8);
-    else FAST_CAL(float, FAST_MXFP4);
+    if (format == FAST_MXFP8) launch_ca<float, FAST_MXFP8>(a, ve, big, wave, grid, long_grid, st);
+    else launch_ca<float, FAST_MXFP4>(a, ve, big, wave, grid, long_grid, st);
   } else {
-    if (format == FAST_MXFP8) FAST_CAL(uint16_t, FAST_MXFP8);
-    else FAST_CAL(uint16_t, FAST_MXFP4);
+    if (format == FAST_MXFP8) launch_ca<uint16_t, FAST_MXFP8>(a, ve, big, wave, grid, long_grid, st);
+    else launch_ca<uint16_t, FAST_MXFP4>(a, ve, big, wave, grid, long_grid, st);
   }
-#undef FAST_CAL
   if (a.cells > 0) {
-    const dim3 jg(uint32_t(a.cells > 2048 ? (a.cells + 15) / 16 : a.cells), uint32_t(H));
-    if (dtype == FAST_F32) hipLaunchKernelGGL((k_attn_cached_join<float>), jg, dim3(CJ_THREADS), 0, st, a);
-    else hipLaunchKernelGGL((k_attn_cached_join<uint16_t>), jg, dim3(CJ_THREADS), 0, st, a);
+    const dim3 join_grid(cells, uint32_t(H));
+    if (dtype == FAST_F32)
+      hipLaunchKernelGGL((k_attn_cached_join<float>), join_grid, dim3(CA_THREADS), 0, st, a);
+    else
+      hipLaunchKernelGGL((k_attn_cached_join<uint16_t>), join_grid, dim3(CA_THREADS), 0, st, a);
   }
   return check_launch(fn);
 }
