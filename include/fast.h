@@ -538,8 +538,8 @@ fast_status_t fast_index_add_scaled_rows(const int32_t* occ_off, const int32_t* 
  * are those of the row that `sum` ([n, D], optional, only with res) stores and the backward
  * reads.  mean, rstd: [n] fp32, optional (the backward needs both).
  * Statistics and products are fp32, the mean taken before the squares.
- * Limits: 1 <= D <= 8192, n < 2^31.  Rows aligned to their element; y may be
- * x, res or, where sum is NULL, neither.  eps >= 0.
+ * Limits: 1 <= D <= 8192, n < 2^31.  Rows aligned to their element; y and sum
+ * may each be x or res, not both the same.  eps >= 0.
  * ------------------------------------------------------------------------ */
 fast_status_t fast_layer_norm_fwd(int64_t n, int D, fast_dtype_t dtype, const void* x,
                                   const void* res, const float* gamma, const float* beta,
@@ -552,8 +552,8 @@ fast_status_t fast_layer_norm_fwd(int64_t n, int D, fast_dtype_t dtype, const vo
  * h: the forward's sum (x where res was NULL); mean, rstd: its outputs; dsum:
  * NULL, or the gradient [n, D] of dtype that reaches the sum on another path.
  * dgamma, dbeta: [D] fp32, overwritten (zeros when n = 0), each optional;
- * added in fp32 over at most 32 rows and in fp64 beyond, in a fixed order
- * (repeated calls give the same bits).  dx: [n, D] of dtype; it may be dy or dsum.
+ * added in fp32 over at most 32 rows and in fp64 beyond (a workgroup's sum
+ * rounded to fp32 in between), in a fixed order: repeated calls give the same bits.  dx: [n, D] of dtype; it may be dy or dsum.
  * Workspace, needed for dgamma or dbeta only: fast_layer_norm_bwd_workspace(n, D)
  * bytes, 8-byte aligned. */
 size_t fast_layer_norm_bwd_workspace(int64_t n, int D);

@@ -20,21 +20,33 @@
 
 namespace fast {
 
-constexpr int LN_THREADS = 256;
-constexpr int LN_MAX_P = 8;      // chunks of a row per lane, at most
+constexpr int LN_THREADS = 256;  // of a workgroup that holds several groups
+constexpr int LN_MAX_G = 1024;   // lanes of a group, at most
+constexpr int LN_ELEMS = 16;     // elements of a row per lane, at most
+constexpr int64_t LN_BLOCKS = 1024;   // workgroups of the backward, about
 constexpr int LN_ROWS = 32;      // rows that a lane adds up in fp32, at most
-constexpr int64_t LN_MAX_D = int64_t(LN_THREADS) * LN_MAX_P * 4;   // 8192
+constexpr int64_t LN_MAX_D = 8192;
 
-// Sum over the G lanes of a group; G = LN_THREADS: over the workgroup.
-__device__ __forceinline__ float row_sum(float x, int G, float* s_red) {
-  if (G <= 64) return group_sum(x, G);
+// Sums over the G lanes of a group; G > 64: over the workgroup, through
+// one of two LDS buffers in turn, so that one barrier per sum is enough (a
+// wave that writes a buffer again has passed the barrier behind its last readers).
+struct LnSum {
+  float2* buf;
+  int turn;
+};
+__device__ __forceinline__ float2 row_sums(float x, float y, int G, LnSum& s) {
+  if (G <= 64) return make_float2(group_sum(x, G), group_sum(y, G));
   x = group_sum(x, 64);
-  __syncthreads();                       // the last sum's readers are done
-  if ((threadIdx.x & 63) == 0) s_red[threadIdx.x >> 6] = x;
+  y = group_sum(y, 64);
+  float2* b = s.buf + s.turn * (LN_MAX_G / 64);
+  s.turn ^= 1;
+  if ((threadIdx.x & 63) == 0) b[threadIdx.x >> 6] = make_float2(x, y);
   __syncthreads();
-  float t = 0.f;
-#pragma unroll
-  for (int w = 0; w < LN_THREADS / 64; ++w) t += s_red[w];
+  float2 t = make_float2(0.f, 0.f);
+  for (int w = 0; w < G / 64; ++w) {
+    t.x += b[w].x;
+    t.y += b[w].y;
+  }
   return t;
 }
 
@@ -52,24 +64,75 @@ struct LnArgs {
   float* rstd;
 };
 
-template <typename T, int P>
-__global__ void __launch_bounds__(LN_THREADS) k_ln_fwd(LnArgs a) {
+// A lane's chunk p of a row.  Of a row that is no multiple of 16 bytes (TAIL) the last chunk
+// starts early enough to end with it: its first `skip` elements are the
+// neighbour's, and count once; loading the rest of a row one by one took 1.5 times as
+// long (200,000 x 172 bf16).  Rows of less than 16 bytes are one partial chunk.
+template <int VE, bool TAIL>
+struct LnChunk {
+  int first, n, skip;                // elements [first, first + n), n <= 0: none
+  __device__ LnChunk(int c, int D) {
+    first = c * VE;
+    n = D - first;
+    skip = 0;
+    if constexpr (TAIL) {
+      if (n > 0 && n < VE && D >= VE) {
+        skip = VE - n;
+        first = D - VE;
+        n = VE;
+      }
+    } else if (n > VE) {
+      n = VE;
+    }
+  }
+  __device__ bool own(int j) const { return TAIL ? j >= skip && j < n : n > 0; }
+};
+template <typename T, bool TAIL, bool NT>
+__device__ __forceinline__ void ln_load(const T* row, const LnChunk<CHUNK<T>, TAIL>& c, float* x) {
+  if (TAIL || c.n > 0) {
+    load_chunk<T, NT>(row + c.first, c.n, x);
+  } else {
+#pragma unroll
+    for (int j = 0; j < CHUNK<T>; ++j) x[j] = 0.f;
+  }
+}
+template <typename T, bool TAIL, bool NT>
+__device__ __forceinline__ void ln_store(T* row, const LnChunk<CHUNK<T>, TAIL>& c, const float* x) {
+  if (c.n > 0) store_chunk<T, NT>(row + c.first, c.n, x);
+}
+// The chunk's columns of an fp32 vector, `fill` where it is NULL.
+template <int VE, bool TAIL>
+__device__ __forceinline__ void ln_cols(const float* v, float fill, const LnChunk<VE, TAIL>& c, float* x) {
+#pragma unroll
+  for (int j = 0; j < VE; j += 4) {
+    if (v) {
+      load_chunk(v + c.first + j, c.n - j, x + j);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) x[j + k] = fill;
+    }
+  }
+}
+
+template <typename T, int P, bool TAIL, bool NT>
+__global__ void __launch_bounds__(LN_MAX_G) k_ln_fwd(LnArgs a) {
   constexpr int VE = CHUNK<T>;
-  __shared__ float s_red[LN_THREADS / 64];
+  typedef LnChunk<VE, TAIL> Chunk;
+  __shared__ float2 s_red[2 * (LN_MAX_G / 64)];
+  LnSum red = {s_red, 0};
   const int G = a.G, lane = threadIdx.x & (G - 1), sub = threadIdx.x / G;
-  const int64_t row = int64_t(blockIdx.x) * (LN_THREADS / G) + sub;
+  const int64_t row = int64_t(blockIdx.x) * (int(blockDim.x) / G) + sub;
   if (row >= a.n) return;               // whole groups; a workgroup-wide row always exists
   const int D = a.D;
-  const T* x = static_cast<const T*>(a.x) + row * D;
-  float h[P][VE];
-  float s = 0.f;
+  float h[P][VE], g[P][VE], b[P][VE];
 #pragma unroll
-  for (int p = 0; p < P; ++p) load_chunk(x + (lane + p * G) * VE, D - (lane + p * G) * VE, h[p]);
+  for (int p = 0; p < P; ++p)
+    ln_load<T, TAIL, NT>(static_cast<const T*>(a.x) + row * D, Chunk(lane + p * G, D), h[p]);
   if (a.res) {
-    const T* r = static_cast<const T*>(a.res) + row * D;
     float t[P][VE];
 #pragma unroll
-    for (int p = 0; p < P; ++p) load_chunk(r + (lane + p * G) * VE, D - (lane + p * G) * VE, t[p]);
+    for (int p = 0; p < P; ++p)
+      ln_load<T, TAIL, NT>(static_cast<const T*>(a.res) + row * D, Chunk(lane + p * G, D), t[p]);
 #pragma unroll
     for (int p = 0; p < P; ++p)
 #pragma unroll
@@ -78,52 +141,52 @@ __global__ void __launch_bounds__(LN_THREADS) k_ln_fwd(LnArgs a) {
         // the statistics are those of the stored row, which the backward reads
         if constexpr (sizeof(T) == 2) h[p][j] = __uint_as_float(bf16_rne(h[p][j]) << 16);
       }
-    if (a.sum) {
-      T* o = static_cast<T*>(a.sum) + row * D;
-#pragma unroll
-      for (int p = 0; p < P; ++p) store_chunk(o + (lane + p * G) * VE, D - (lane + p * G) * VE, h[p]);
-    }
   }
 #pragma unroll
-  for (int p = 0; p < P; ++p)
+  for (int p = 0; p < P; ++p) {
+    ln_cols(a.gamma, 1.f, Chunk(lane + p * G, D), g[p]);
+    ln_cols(a.beta, 0.f, Chunk(lane + p * G, D), b[p]);
+  }
+  float s = 0.f;
 #pragma unroll
-    for (int j = 0; j < VE; ++j) s += h[p][j];
-  const float mean = row_sum(s, G, s_red) / float(D);
+  for (int p = 0; p < P; ++p) {
+    const Chunk c(lane + p * G, D);
+#pragma unroll
+    for (int j = 0; j < VE; ++j) s += !TAIL || c.own(j) ? h[p][j] : 0.f;   // zeros past the row
+  }
+  const float mean = row_sums(s, 0.f, G, red).x / float(D);
+  // the row has been read by every lane: sum and y may take the place of x or res
+  if (a.sum) {
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+      ln_store<T, TAIL, NT>(static_cast<T*>(a.sum) + row * D, Chunk(lane + p * G, D), h[p]);
+  }
   float q = 0.f;
 #pragma unroll
-  for (int p = 0; p < P; ++p)
+  for (int p = 0; p < P; ++p) {
+    const Chunk c(lane + p * G, D);
 #pragma unroll
     for (int j = 0; j < VE; ++j) {
-      const float c = (lane + p * G) * VE + j < D ? h[p][j] - mean : 0.f;
-      q = fmaf(c, c, q);
+      const float d = c.own(j) ? h[p][j] - mean : 0.f;
+      q = fmaf(d, d, q);
     }
-  const float rstd = 1.f / sqrtf(row_sum(q, G, s_red) / float(D) + a.eps);
+  }
+  const float rstd = 1.f / sqrtf(row_sums(q, 0.f, G, red).x / float(D) + a.eps);
   if (lane == 0) {
     if (a.mean) a.mean[row] = mean;
     if (a.rstd) a.rstd[row] = rstd;
   }
-  T* y = static_cast<T*>(a.y) + row * D;
 #pragma unroll
   for (int p = 0; p < P; ++p) {
-    const int c0 = (lane + p * G) * VE;
-    float g[VE], b[VE];
 #pragma unroll
-    for (int j = 0; j < VE; j += 4) {
-      if (a.gamma) load_chunk(a.gamma + c0 + j, D - c0 - j, g + j);
-      else for (int k = 0; k < 4; ++k) g[j + k] = 1.f;
-      if (a.beta) load_chunk(a.beta + c0 + j, D - c0 - j, b + j);
-      else for (int k = 0; k < 4; ++k) b[j + k] = 0.f;
-    }
-#pragma unroll
-    for (int j = 0; j < VE; ++j) g[j] = fmaf((h[p][j] - mean) * rstd, g[j], b[j]);
-    store_chunk(y + c0, D - c0, g);
+    for (int j = 0; j < VE; ++j) g[p][j] = fmaf((h[p][j] - mean) * rstd, g[p][j], b[p][j]);
+    ln_store<T, TAIL, NT>(static_cast<T*>(a.y) + row * D, Chunk(lane + p * G, D), g[p]);
   }
 }
 
 struct LnBwdArgs {
   int64_t n;
   int D, G;
-  int64_t rows;        // rows per workgroup
   const void* h;
   const float* gamma;
   const float* mean;
@@ -131,71 +194,76 @@ struct LnBwdArgs {
   const void* dy;
   const void* dsum;
   void* dx;
-  double* part;        // [workgroups][2][D], or NULL: dx only
+  float* part;         // [workgroups][2][D], or NULL: dx only
 };
 
-template <typename T, int P>
-__global__ void __launch_bounds__(LN_THREADS) k_ln_bwd(LnBwdArgs a) {
+template <typename T, int P, bool TAIL, bool NT>
+__global__ void __launch_bounds__(LN_MAX_G) k_ln_bwd(LnBwdArgs a) {
   constexpr int VE = CHUNK<T>;
-  __shared__ float s_red[LN_THREADS / 64];
+  typedef LnChunk<VE, TAIL> Chunk;
+  __shared__ float2 s_red[2 * (LN_MAX_G / 64)];
+  LnSum red = {s_red, 0};
   extern __shared__ double s_col[];     // [D] where the workgroup holds several groups
-  const int G = a.G, lane = threadIdx.x & (G - 1), sub = threadIdx.x / G, groups = LN_THREADS / G;
+  const int G = a.G, lane = threadIdx.x & (G - 1), sub = threadIdx.x / G, groups = blockDim.x / G;
   const int D = a.D;
-  const int64_t r0 = int64_t(blockIdx.x) * a.rows;
-  const int64_t r1 = r0 + a.rows < a.n ? r0 + a.rows : a.n;
+  // rows b, b + workgroups, ... (in units of a workgroup's groups), so that the chip reads
+  // one stretch of memory at a time: 281 -> 272 us against a stretch per workgroup
+  // (40,000 x 2048 fp32)
+  const int64_t r0 = int64_t(blockIdx.x) * groups, step = int64_t(gridDim.x) * groups;
   float ga[P][VE], dg[P][VE], db[P][VE];
 #pragma unroll
   for (int p = 0; p < P; ++p) {
-    const int c0 = (lane + p * G) * VE;
-#pragma unroll
-    for (int j = 0; j < VE; j += 4) {
-      if (a.gamma) load_chunk(a.gamma + c0 + j, D - c0 - j, ga[p] + j);
-      else for (int k = 0; k < 4; ++k) ga[p][j + k] = 1.f;
-    }
+    ln_cols(a.gamma, 1.f, Chunk(lane + p * G, D), ga[p]);
 #pragma unroll
     for (int j = 0; j < VE; ++j) dg[p][j] = db[p][j] = 0.f;
   }
   const float inv = 1.f / float(D);
-  for (int64_t row = r0 + sub; row < r1; row += groups) {
-    const T* hp = static_cast<const T*>(a.h) + row * D;
-    const T* yp = static_cast<const T*>(a.dy) + row * D;
-    float xh[P][VE], dy[P][VE];
+  for (int64_t row = r0 + sub; row < a.n; row += step) {
+    const float mean = a.mean[row], rstd = a.rstd[row];
+    float xh[P][VE], dy[P][VE], d[P][VE];
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-      const int c0 = (lane + p * G) * VE;
-      load_chunk(hp + c0, D - c0, xh[p]);
-      load_chunk(yp + c0, D - c0, dy[p]);     // 0 past the row's end: those columns add nothing
+      const Chunk c(lane + p * G, D);
+      ln_load<T, TAIL, NT>(static_cast<const T*>(a.h) + row * D, c, xh[p]);
+      ln_load<T, TAIL, NT>(static_cast<const T*>(a.dy) + row * D, c, dy[p]);   // zeros past the row
     }
-    const float mean = a.mean[row], rstd = a.rstd[row];
+    if (a.dsum) {
+#pragma unroll
+      for (int p = 0; p < P; ++p)
+        ln_load<T, TAIL, NT>(static_cast<const T*>(a.dsum) + row * D, Chunk(lane + p * G, D), d[p]);
+    } else {
+#pragma unroll
+      for (int p = 0; p < P; ++p)
+#pragma unroll
+        for (int j = 0; j < VE; ++j) d[p][j] = 0.f;
+    }
     float s1 = 0.f, s2 = 0.f;
 #pragma unroll
-    for (int p = 0; p < P; ++p)
+    for (int p = 0; p < P; ++p) {
+      const Chunk c(lane + p * G, D);
 #pragma unroll
       for (int j = 0; j < VE; ++j) {
         xh[p][j] = (xh[p][j] - mean) * rstd;
         dg[p][j] = fmaf(dy[p][j], xh[p][j], dg[p][j]);
         db[p][j] += dy[p][j];
         dy[p][j] *= ga[p][j];
-        s1 += dy[p][j];
-        s2 = fmaf(dy[p][j], xh[p][j], s2);
+        const float g = !TAIL || c.own(j) ? dy[p][j] : 0.f;
+        s1 += g;
+        s2 = fmaf(g, xh[p][j], s2);
       }
-    s1 = row_sum(s1, G, s_red) * inv;
-    s2 = row_sum(s2, G, s_red) * inv;
-    T* o = static_cast<T*>(a.dx) + row * D;
+    }
+    const float2 st = row_sums(s1, s2, G, red);
+    s1 = st.x * inv;
+    s2 = st.y * inv;
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-      const int c0 = (lane + p * G) * VE;
-      float d[VE];
-      if (a.dsum) load_chunk(static_cast<const T*>(a.dsum) + row * D + c0, D - c0, d);
-      else
-        for (int j = 0; j < VE; ++j) d[j] = 0.f;
 #pragma unroll
-      for (int j = 0; j < VE; ++j) d[j] = fmaf(rstd, dy[p][j] - s1 - xh[p][j] * s2, d[j]);
-      store_chunk(o + c0, D - c0, d);
+      for (int j = 0; j < VE; ++j) d[p][j] = fmaf(rstd, dy[p][j] - s1 - xh[p][j] * s2, d[p][j]);
+      ln_store<T, TAIL, NT>(static_cast<T*>(a.dx) + row * D, Chunk(lane + p * G, D), d[p]);
     }
   }
   if (!a.part) return;
-  double* out = a.part + int64_t(blockIdx.x) * 2 * D;
+  float* out = a.part + int64_t(blockIdx.x) * 2 * D;
   const int wave = threadIdx.x >> 6;
   for (int which = 0; which < 2; ++which) {
     double c[P][VE];
@@ -208,98 +276,135 @@ __global__ void __launch_bounds__(LN_THREADS) k_ln_bwd(LnBwdArgs a) {
       }
     if (groups == 1) {                   // the lanes of the workgroup own different columns
 #pragma unroll
-      for (int p = 0; p < P; ++p)
+      for (int p = 0; p < P; ++p) {
+        const Chunk k(lane + p * G, D);
 #pragma unroll
         for (int j = 0; j < VE; ++j)
-          if ((lane + p * G) * VE + j < D) out[which * D + (lane + p * G) * VE + j] = c[p][j];
+          if (k.own(j)) out[which * D + k.first + j] = float(c[p][j]);
+      }
       continue;
     }
-    for (int k = 0; k < LN_THREADS / 64; ++k) {   // the waves in order
-      if (wave == k && (threadIdx.x & 63) < G) {
+    for (int w = 0; w < LN_THREADS / 64; ++w) {   // the waves in order (several groups: LN_THREADS threads)
+      if (wave == w && (threadIdx.x & 63) < G) {
 #pragma unroll
-        for (int p = 0; p < P; ++p)
+        for (int p = 0; p < P; ++p) {
+          const Chunk k(lane + p * G, D);
 #pragma unroll
-          for (int j = 0; j < VE; ++j) {
-            const int col = (lane + p * G) * VE + j;
-            if (col < D) s_col[col] = (k ? s_col[col] : 0.0) + c[p][j];
-          }
+          for (int j = 0; j < VE; ++j)
+            if (k.own(j)) s_col[k.first + j] = (w ? s_col[k.first + j] : 0.0) + c[p][j];
+        }
       }
       __syncthreads();
     }
-    for (int col = threadIdx.x; col < D; col += LN_THREADS) out[which * D + col] = s_col[col];
+    for (int col = threadIdx.x; col < D; col += LN_THREADS) out[which * D + col] = float(s_col[col]);
     __syncthreads();                     // read before the next sums overwrite it
   }
 }
 
-// dgamma and dbeta from the partial rows, added in their order: LN_SUM_ROWS
-// threads per column take every LN_SUM_ROWS-th row, then one adds theirs.
-constexpr int LN_SUM_COLS = 16;
-constexpr int LN_SUM_ROWS = LN_THREADS / LN_SUM_COLS;
-__global__ void __launch_bounds__(LN_THREADS) k_ln_bwd_sum(const double* __restrict__ part, int64_t nb,
-                                                           int D, float* __restrict__ dgamma,
-                                                           float* __restrict__ dbeta) {
-  __shared__ double s[LN_SUM_ROWS][LN_SUM_COLS];
-  const int col = threadIdx.x % LN_SUM_COLS, r = threadIdx.x / LN_SUM_COLS;
-  const int c = blockIdx.x * LN_SUM_COLS + col;      // of 2 D columns
+// dgamma and dbeta from the partial rows, added in fp64 in a fixed order: LNS_ROWS
+// threads per column take every LNS_ROWS-th row, then one adds theirs.
+constexpr int LNS_THREADS = 1024, LNS_COLS = 16, LNS_ROWS = LNS_THREADS / LNS_COLS;
+__global__ void __launch_bounds__(LNS_THREADS) k_ln_bwd_sum(const float* __restrict__ part, int64_t nb,
+                                                            int D, float* __restrict__ dgamma,
+                                                            float* __restrict__ dbeta) {
+  __shared__ double s[LNS_ROWS][LNS_COLS];
+  const int col = threadIdx.x % LNS_COLS, r = threadIdx.x / LNS_COLS;
+  const int c = blockIdx.x * LNS_COLS + col;         // of 2 D columns
   double t = 0.0;
-  if (c < 2 * D)
-    for (int64_t b = r; b < nb; b += LN_SUM_ROWS) t += part[b * 2 * D + c];
+  if (c < 2 * D) {
+#pragma unroll 8
+    for (int64_t b = r; b < nb; b += LNS_ROWS) t += part[b * 2 * D + c];
+  }
   s[r][col] = t;
   __syncthreads();
+  for (int h = LNS_ROWS / 2; h > 0; h /= 2) {
+    if (r < h) s[r][col] += s[r + h][col];
+    __syncthreads();
+  }
   if (r == 0 && c < 2 * D) {
-    for (int k = 1; k < LN_SUM_ROWS; ++k) t += s[k][col];
     float* o = c < D ? dgamma : dbeta;
-    if (o) o[c < D ? c : c - D] = float(t);
+    if (o) o[c < D ? c : c - D] = float(s[0][col]);
   }
 }
 
 struct LnPlan {
   int G, P;            // lanes per row, chunks per lane
-  int64_t rows, nb;    // backward: rows per workgroup, workgroups
+  int threads;         // per workgroup: one group of more than a wave, or several
+  int64_t nb;          // backward: workgroups
 };
 
-// The narrowest group that holds a row with the fewest idle chunk slots; a
-// workgroup for rows past what a wave's registers hold.
+// The group with the fewest idle chunk slots that holds a row in at most LN_ELEMS
+// elements a lane, and the fewest of those.  Fewer registers keep more rows in flight: 40,000
+// rows of 2048 fp32, backward 444 us with a wave per row (32 elements a lane), 281 with
+// 256 lanes (8); 200,000 rows of 172 bf16, 8 lanes of 24 elements 136, 32 of 8 78.
 static LnPlan ln_plan(int64_t n, int D, int ve) {
   LnPlan L = {};
   const int C = (D + ve - 1) / ve;
   int best = 1 << 30;
-  const int ps[] = {1, 2, 3, 4, 6, 8};
-  for (int G = 1; G <= 64; G *= 2)
-    for (int P : ps)
+  for (int G = 1; G <= LN_MAX_G; G *= 2)
+    for (int P = 1; P <= LN_ELEMS / ve; ++P)
       if (G * P >= C && (G * P < best || (G * P == best && P < L.P))) {
         best = G * P;
         L.G = G;
         L.P = P;
       }
-  if (best == 1 << 30) {
-    L.G = LN_THREADS;
-    for (int P : ps)
-      if (LN_THREADS * P >= C) {
-        L.P = P;
-        break;
-      }
-  }
-  const int64_t groups = LN_THREADS / L.G;
-  // about 2048 workgroups (8 per CU), each with at most LN_ROWS rows per group
-  int64_t per = (n + 2048 * groups - 1) / (2048 * groups);
+  L.threads = L.G > 64 ? L.G : LN_THREADS;
+  // 4 workgroups per CU (2 / 4 / 8: 23 / 19 / 26 us for 66,000 rows of 128 bf16, the
+  // partial rows' sums included: 27 / 23 / 31), and at most LN_ROWS rows per group
+  const int64_t groups = L.threads / L.G;
+  int64_t per = (n + LN_BLOCKS * groups - 1) / (LN_BLOCKS * groups);
   per = per < 1 ? 1 : (per > LN_ROWS ? LN_ROWS : per);
-  L.rows = per * groups;
-  L.nb = (n + L.rows - 1) / L.rows;
+  L.nb = (n + per * groups - 1) / (per * groups);
   return L;
 }
 
-template <typename T>
-static void launch_ln_fwd(const LnArgs& a, int P, uint32_t grid, hipStream_t st) {
-#define FAST_LN(p) case p: hipLaunchKernelGGL((k_ln_fwd<T, p>), dim3(grid), dim3(LN_THREADS), 0, st, a); break
-  switch (P) { FAST_LN(1); FAST_LN(2); FAST_LN(3); FAST_LN(4); FAST_LN(6); FAST_LN(8); }
+// Stream rows that cover whole cache lines when a pass moves more than the 256 MB
+// last-level cache holds: 40,000 x 2048 fp32, forward 223 -> 217 us, backward 272 ->
+// 247; 66,000 x 128 bf16 (135 MB for both directions) 14.8 -> 14.7, 20.0 -> 21.9.
+static bool ln_stream(int64_t n, int D, size_t es, int arrays, const void* const* rows, int count) {
+  if ((D * es) % CACHE_LINE != 0 || n * int64_t(D * es) * arrays <= (int64_t(256) << 20)) return false;
+  for (int k = 0; k < count; ++k)
+    if (!aligned(rows[k], CACHE_LINE)) return false;
+  return true;
+}
+
+template <typename T, bool TAIL, bool NT>
+static void launch_ln(const LnArgs& a, const LnPlan& L, uint32_t grid, size_t, hipStream_t st) {
+  static_assert(LN_ELEMS == 16, "chunks per lane: 1 to 4 of fp32, 1 or 2 of bf16");
+#define FAST_LN(p) hipLaunchKernelGGL((k_ln_fwd<T, p, TAIL, NT>), dim3(grid), dim3(L.threads), 0, st, a)
+  if (L.P == 1) FAST_LN(1);
+  else if (L.P == 2) FAST_LN(2);
+  else if constexpr (sizeof(T) == 4) {
+    if (L.P == 3) FAST_LN(3);
+    else FAST_LN(4);
+  }
 #undef FAST_LN
 }
-template <typename T>
-static void launch_ln_bwd(const LnBwdArgs& a, int P, uint32_t grid, size_t lds, hipStream_t st) {
-#define FAST_LN(p) case p: hipLaunchKernelGGL((k_ln_bwd<T, p>), dim3(grid), dim3(LN_THREADS), lds, st, a); break
-  switch (P) { FAST_LN(1); FAST_LN(2); FAST_LN(3); FAST_LN(4); FAST_LN(6); FAST_LN(8); }
+template <typename T, bool TAIL, bool NT>
+static void launch_ln(const LnBwdArgs& a, const LnPlan& L, uint32_t grid, size_t lds, hipStream_t st) {
+#define FAST_LN(p) hipLaunchKernelGGL((k_ln_bwd<T, p, TAIL, NT>), dim3(grid), dim3(L.threads), lds, st, a)
+  if (L.P == 1) FAST_LN(1);
+  else if (L.P == 2) FAST_LN(2);
+  else if constexpr (sizeof(T) == 4) {
+    if (L.P == 3) FAST_LN(3);
+    else FAST_LN(4);
+  }
 #undef FAST_LN
+}
+// Streamed rows cover whole cache lines, so they have no tail.
+template <typename Args>
+static void launch_ln(const Args& a, const LnPlan& L, uint32_t grid, size_t lds, fast_dtype_t dtype, bool nt,
+                      hipStream_t st) {
+  const bool tail = a.D % (dtype == FAST_F32 ? CHUNK<float> : CHUNK<uint16_t>) != 0;
+  if (dtype == FAST_F32) {
+    if (nt) launch_ln<float, false, true>(a, L, grid, lds, st);
+    else if (tail) launch_ln<float, true, false>(a, L, grid, lds, st);
+    else launch_ln<float, false, false>(a, L, grid, lds, st);
+  } else {
+    if (nt) launch_ln<uint16_t, false, true>(a, L, grid, lds, st);
+    else if (tail) launch_ln<uint16_t, true, false>(a, L, grid, lds, st);
+    else launch_ln<uint16_t, false, false>(a, L, grid, lds, st);
+  }
 }
 
 static fast_status_t ln_check(const char* fn, int64_t n, int D, fast_dtype_t dtype) {
@@ -333,11 +438,12 @@ extern "C" fast_status_t fast_layer_norm_fwd(int64_t n, int D, fast_dtype_t dtyp
     return fail(FAST_ERR_UNSUPPORTED, "%s: gamma/beta/mean/rstd not 4-byte aligned", fn);
   const LnPlan L = ln_plan(n, D, 16 / int(es));
   const LnArgs a = {n, D, L.G, x, res, gamma, beta, eps, y, sum, mean, rstd};
-  const int64_t per = LN_THREADS / L.G;
+  const int64_t per = L.threads / L.G;
   const uint32_t grid = uint32_t((n + per - 1) / per);
   hipStream_t st = static_cast<hipStream_t>(stream);
-  if (dtype == FAST_F32) launch_ln_fwd<float>(a, L.P, grid, st);
-  else launch_ln_fwd<uint16_t>(a, L.P, grid, st);
+  const void* rows[] = {x, res, y, sum};
+  const bool nt = ln_stream(n, D, es, 2 + (res != nullptr) + (sum != nullptr), rows, 4);
+  launch_ln(a, L, grid, 0, dtype, nt, st);
   return check_launch(fn);
 }
 
@@ -345,7 +451,7 @@ extern "C" size_t fast_layer_norm_bwd_workspace(int64_t n, int D) {
   if (n < 0 || n >= (int64_t(1) << 31) || D <= 0 || D > LN_MAX_D) return 0;
   const LnPlan a = ln_plan(n, D, 4), b = ln_plan(n, D, 8);
   const int64_t nb = a.nb > b.nb ? a.nb : b.nb;
-  return size_t(nb > 0 ? nb : 1) * 2 * D * sizeof(double);
+  return size_t(nb > 0 ? nb : 1) * 2 * D * sizeof(float);
 }
 
 extern "C" fast_status_t fast_layer_norm_bwd(int64_t n, int D, fast_dtype_t dtype, const void* h,
@@ -375,14 +481,15 @@ extern "C" fast_status_t fast_layer_norm_bwd(int64_t n, int D, fast_dtype_t dtyp
   const LnPlan L = ln_plan(n, D, 16 / int(es));
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (n > 0) {
-    const LnBwdArgs a = {n, D, L.G, L.rows, h, gamma, mean, rstd, dy, dsum, dx,
-                         sums ? static_cast<double*>(ws) : nullptr};
-    const size_t lds = sums && L.G < LN_THREADS ? size_t(D) * sizeof(double) : 0;
-    if (dtype == FAST_F32) launch_ln_bwd<float>(a, L.P, uint32_t(L.nb), lds, st);
-    else launch_ln_bwd<uint16_t>(a, L.P, uint32_t(L.nb), lds, st);
+    const LnBwdArgs a = {n, D, L.G, h, gamma, mean, rstd, dy, dsum, dx,
+                         sums ? static_cast<float*>(ws) : nullptr};
+    const size_t lds = sums && L.G < L.threads ? size_t(D) * sizeof(double) : 0;
+    const void* rows[] = {h, dy, dsum, dx};
+    const bool nt = ln_stream(n, D, es, 3 + (dsum != nullptr), rows, 4);
+    launch_ln(a, L, uint32_t(L.nb), lds, dtype, nt, st);
   }
   if (sums)
-    hipLaunchKernelGGL(k_ln_bwd_sum, dim3((2 * D + LN_SUM_COLS - 1) / LN_SUM_COLS), dim3(LN_THREADS), 0, st,
-                       static_cast<const double*>(ws), n > 0 ? L.nb : 0, D, dgamma, dbeta);
+    hipLaunchKernelGGL(k_ln_bwd_sum, dim3((2 * D + LNS_COLS - 1) / LNS_COLS), dim3(LNS_THREADS), 0, st,
+                       static_cast<const float*>(ws), n > 0 ? L.nb : 0, D, dgamma, dbeta);
   return check_launch(fn);
 }

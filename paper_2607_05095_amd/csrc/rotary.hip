@@ -7,7 +7,7 @@
 //
 // Bound by HBM: each element is read and written once.  The angles belong to a
 // row, not to its heads: a workgroup first forms the sines and cosines of its
-// rows in LDS, then streams the rows in pieces of 16 bytes.
+// rows in LDS while the rows' pieces of 16 bytes are on their way to its registers.
 //
 // Positions may be event times far from zero, where an fp32 angle has no correct
 // digit left: the product of the two fp32 factors is exact in fp64, it is reduced
@@ -18,8 +18,11 @@
 namespace fast {
 
 constexpr int ROT_THREADS = 256;
-constexpr int ROT_LDS_PAIRS = 2048;     // (cos, sin) pairs per workgroup: 16 KB
-constexpr int ROT_MAX_ROWS = 64;
+// Pieces per thread: 2 where a piece is 16 bytes, 1 where it is 16 of either half
+// (528,000 rows of 2 x 50 fp32: 102 / 115 us with 2 / 1, by halves 108 / 101).
+template <bool INTER> constexpr int ROT_UNROLL = INTER ? 2 : 1;
+constexpr int ROT_PAIRS = 1024;         // (cos, sin) pairs per workgroup
+constexpr int ROT_LDS_PAIRS = ROT_PAIRS + 8;
 
 struct RotArgs {
   int64_t n, ldx, ldy;
@@ -36,68 +39,100 @@ struct RotArgs {
   float sign;
 };
 
-template <typename T, bool INTER>
+// (cos, sin) of a position times a frequency: the angle in quarter turns, its nearest whole number
+// and the rest g, |g| <= 1/2, then the Taylor sums of sin and cos(g pi/2) through g^9 and
+// g^10 (the next terms are below 2e-9); 1.5e-7 in all with their fp32 roundings.
+__device__ __forceinline__ float2 rot_turn(float pos, float omega, float sign) {
+  const double quarters = double(pos) * double(omega) * 0.6366197723675814;   // 2 / pi; the first product is exact
+  const double q = rint(quarters);
+  const float g = float(quarters - q);               // NaN of an infinite angle
+  const int k = int(__builtin_amdgcn_fract(q * 0.25) * 4.0);   // q mod 4
+  const float t = g * g;
+  float s = fmaf(t, 1.604411847e-4f, -4.681754135e-3f);
+  s = fmaf(s, t, 7.969262624e-2f);
+  s = fmaf(s, t, -6.459640975e-1f);
+  s = fmaf(s, t, 1.570796327f) * g;
+  float c = fmaf(t, -2.520204237e-5f, 9.192602748e-4f);
+  c = fmaf(c, t, -2.086348077e-2f);
+  c = fmaf(c, t, 2.536695079e-1f);
+  c = fmaf(c, t, -1.233700550f);
+  c = fmaf(c, t, 1.f);
+  const float s1 = (k & 1) ? c : s, c1 = (k & 1) ? s : c;
+  return make_float2((k == 1 || k == 2) ? -c1 : c1, (k >= 2 ? -s1 : s1) * sign);
+}
+
+// A piece of a head: 16 bytes of it, or (pairs (p, pairs + p)) 16 bytes of either half.
+template <int VE, bool INTER>
+struct RotPiece {
+  int64_t x, y;                         // element offsets of the head's first element
+  int e, n, cs;                         // first element, elements left, first pair's place in LDS
+  bool rot;
+  float a[VE], b[INTER ? 1 : VE];
+};
+
+template <typename T, bool INTER, bool NT>
 __global__ void __launch_bounds__(ROT_THREADS) k_rotary(RotArgs a) {
-  constexpr int VE = CHUNK<T>;
+  constexpr int VE = CHUNK<T>, UN = ROT_UNROLL<INTER>;
   __shared__ float2 s_cs[ROT_LDS_PAIRS];
   const int64_t row0 = int64_t(blockIdx.x) * a.rows;
   const int rows = int(a.n - row0 < a.rows ? a.n - row0 : a.rows);
-  const int P = a.pairs;
+  const int P = a.pairs, total = rows * a.upr;
+  const T* x = static_cast<const T*>(a.x);
+  T* y = static_cast<T*>(a.y);
+  // the rows' loads are in flight while the angles are formed
+  RotPiece<VE, INTER> w[UN];
+#pragma unroll
+  for (int k = 0; k < UN; ++k) {
+    const int t = threadIdx.x + (blockIdx.y * UN + k) * ROT_THREADS;
+    if (t < total) {
+      const int r = int(div_small(t, a.mag_upr)), u = t - r * a.upr;
+      const int h = int(div_small(u, a.mag_units)), c = u - h * a.units;
+      RotPiece<VE, INTER>& q = w[k];
+      q.x = (row0 + r) * a.ldx + h * a.dh;
+      q.y = (row0 + r) * a.ldy + h * a.dh;
+      q.rot = c < a.crot;
+      q.e = q.rot ? c * VE : 2 * P + (c - a.crot) * VE;        // past the pairs: copied
+      q.n = (q.rot ? (INTER ? 2 * P : P) : a.dh) - q.e;
+      q.cs = r * P + (INTER ? q.e / 2 : q.e);
+      load_chunk(x + q.x + q.e, q.n, q.a);
+      if constexpr (!INTER)
+        if (q.rot) load_chunk(x + q.x + P + q.e, q.n, q.b);
+    }
+  }
   for (int t = threadIdx.x; t < rows * P; t += ROT_THREADS) {
     const int r = int(div_small(t, a.mag_pairs)), p = t - r * P;
     int ax = a.axis ? a.axis[p] : 0;
     ax = ax < 0 ? 0 : (ax < a.axes ? ax : a.axes - 1);
-    const double th = double(a.pos[(row0 + r) * a.axes + ax]) * double(a.omega[p]);   // exact
-    const double rev = th * 0.15915494309189535;       // 1 / (2 pi)
-    const double q = rint(rev * 4.0);
-    const float f = float(rev - q * 0.25);             // |f| <= 1/8; NaN of an infinite angle
-    float s, c;
-    sincospif(2.f * f, &s, &c);
-    const int k = int(q - 4.0 * floor(q * 0.25));      // quarter turns, 0..3
-    const float s1 = (k & 1) ? c : s, c1 = (k & 1) ? s : c;
-    s_cs[t] = make_float2((k == 1 || k == 2) ? -c1 : c1, (k >= 2 ? -s1 : s1) * a.sign);
+    s_cs[t] = rot_turn(a.pos[(row0 + r) * a.axes + ax], a.omega[p], a.sign);
   }
   __syncthreads();
-  const T* x = static_cast<const T*>(a.x);
-  T* y = static_cast<T*>(a.y);
-  for (int t = threadIdx.x; t < rows * a.upr; t += ROT_THREADS) {
-    const int r = int(div_small(t, a.mag_upr)), u = t - r * a.upr;
-    const int h = int(div_small(u, a.mag_units)), c = u - h * a.units;
-    const T* xp = x + (row0 + r) * a.ldx + h * a.dh;
-    T* yp = y + (row0 + r) * a.ldy + h * a.dh;
-    if (c >= a.crot) {                                  // past the pairs: copied
-      const int e = 2 * P + (c - a.crot) * VE;
-      float v[VE];
-      load_chunk(xp + e, a.dh - e, v);
-      store_chunk(yp + e, a.dh - e, v);
-    } else if constexpr (INTER) {                       // pairs (2p, 2p + 1)
-      const int e = c * VE;
-      float v[VE];
-      load_chunk(xp + e, 2 * P - e, v);
 #pragma unroll
-      for (int j = 0; j < VE / 2; ++j) {
-        const int p = e / 2 + j < P ? e / 2 + j : P - 1;
-        const float2 cs = s_cs[r * P + p];
-        const float va = v[2 * j], vb = v[2 * j + 1];
-        v[2 * j] = fmaf(va, cs.x, -(vb * cs.y));
-        v[2 * j + 1] = fmaf(va, cs.y, vb * cs.x);
-      }
-      store_chunk(yp + e, 2 * P - e, v);
-    } else {                                            // pairs (p, pairs + p)
-      const int e = c * VE;
-      float va[VE], vb[VE];
-      load_chunk(xp + e, P - e, va);
-      load_chunk(xp + P + e, P - e, vb);
+  for (int k = 0; k < UN; ++k) {
+    if (int(threadIdx.x + (blockIdx.y * UN + k) * ROT_THREADS) < total) {
+      RotPiece<VE, INTER>& q = w[k];
+      if (q.rot) {
+        // s_cs is read past the head's last pair where the piece is partial: within the
+        // array (ROT_LDS_PAIRS has CHUNK places more than pairs in use), and not used
+        if constexpr (INTER) {
 #pragma unroll
-      for (int j = 0; j < VE; ++j) {
-        const int p = e + j < P ? e + j : P - 1;
-        const float2 cs = s_cs[r * P + p];
-        const float t0 = va[j];
-        va[j] = fmaf(t0, cs.x, -(vb[j] * cs.y));
-        vb[j] = fmaf(t0, cs.y, vb[j] * cs.x);
+          for (int j = 0; j < VE / 2; ++j) {
+            const float2 cs = s_cs[q.cs + j];
+            const float va = q.a[2 * j], vb = q.a[2 * j + 1];
+            q.a[2 * j] = fmaf(va, cs.x, -(vb * cs.y));
+            q.a[2 * j + 1] = fmaf(va, cs.y, vb * cs.x);
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < VE; ++j) {
+            const float2 cs = s_cs[q.cs + j];
+            const float va = q.a[j];
+            q.a[j] = fmaf(va, cs.x, -(q.b[j] * cs.y));
+            q.b[j] = fmaf(va, cs.y, q.b[j] * cs.x);
+          }
+          store_chunk(y + q.y + P + q.e, q.n, q.b);
+        }
       }
-      store_chunk(yp + e, P - e, va);
-      store_chunk(yp + P + e, P - e, vb);
+      store_chunk<T, NT>(y + q.y + q.e, q.n, q.a);
     }
   }
 }
@@ -158,8 +193,11 @@ static fast_status_t rotary(const char* fn, int64_t n, int H, int dh, fast_dtype
   a.units = a.crot + (in_place ? 0 : (dh - 2 * pairs + ve - 1) / ve);
   if (a.units == 0) return ok();
   a.upr = a.units * H;
-  int rows = pairs > 0 ? ROT_LDS_PAIRS / pairs : ROT_MAX_ROWS;
-  a.rows = rows < ROT_MAX_ROWS ? rows : ROT_MAX_ROWS;
+  // whole rows, the kernel's pieces per thread; a row of more pieces is shared by workgroups
+  // (blockIdx.y), each forming its angles
+  const int tile = (interleaved ? ROT_UNROLL<true> : ROT_UNROLL<false>) * ROT_THREADS;
+  a.rows = a.upr < tile ? tile / a.upr : 1;
+  if (pairs > 0 && a.rows > ROT_PAIRS / pairs) a.rows = ROT_PAIRS / pairs;
   a.mag_pairs = div_magic(pairs > 0 ? pairs : 1);
   a.mag_upr = div_magic(a.upr);
   a.mag_units = div_magic(a.units);
@@ -169,15 +207,22 @@ static fast_status_t rotary(const char* fn, int64_t n, int H, int dh, fast_dtype
   a.axis = axis;
   a.omega = omega;
   a.sign = sign;
-  const uint32_t grid = uint32_t((n + a.rows - 1) / a.rows);
+  const dim3 grid(uint32_t((n + a.rows - 1) / a.rows), uint32_t((a.rows * a.upr + tile - 1) / tile));
   hipStream_t st = static_cast<hipStream_t>(stream);
-#define FAST_ROT(T, I) hipLaunchKernelGGL((k_rotary<T, I>), dim3(grid), dim3(ROT_THREADS), 0, st, a)
+  // Rows of whole cache lines that go out in one stream (pairs side by side) bypass the
+  // cache when rows and results are more than its last level holds: 1,000,000 rows
+  // of 4 x 32 bf16, 102 -> 76 us; pairs by halves 105 -> 114, so they do not.
+  const bool nt = interleaved && ldy * es % CACHE_LINE == 0 && F == ldy && aligned(y, CACHE_LINE) &&
+                  2 * n * F * es > (int64_t(256) << 20);
+#define FAST_ROT(T, I, N) hipLaunchKernelGGL((k_rotary<T, I, N>), grid, dim3(ROT_THREADS), 0, st, a)
   if (dtype == FAST_F32) {
-    if (interleaved) FAST_ROT(float, true);
-    else FAST_ROT(float, false);
+    if (nt) FAST_ROT(float, true, true);
+    else if (interleaved) FAST_ROT(float, true, false);
+    else FAST_ROT(float, false, false);
   } else {
-    if (interleaved) FAST_ROT(uint16_t, true);
-    else FAST_ROT(uint16_t, false);
+    if (nt) FAST_ROT(uint16_t, true, true);
+    else if (interleaved) FAST_ROT(uint16_t, true, false);
+    else FAST_ROT(uint16_t, false, false);
   }
 #undef FAST_ROT
   return check_launch(fn);
