@@ -73,7 +73,7 @@ __device__ __forceinline__ int64_t mx_slot(int64_t id, int64_t id_bound,
 // (0 is read as 2^-127, 255 as not a number).
 __device__ __forceinline__ float mx_scale(uint32_t b) { return __uint_as_float(b << 23); }
 
-// A piece of 8 or 16 codes of one group, and its values.  Pieces of 16 may start
+// A piece of 4, 8 or 16 codes of one group, and its values.  Pieces of 16 may start
 // at a multiple of 8 codes.
 typedef uint32_t u32x4_8 __attribute__((ext_vector_type(4), aligned(8)));
 typedef uint32_t u32x2_4 __attribute__((ext_vector_type(2), aligned(4)));
@@ -84,14 +84,17 @@ template <int N> struct MxPiece<FAST_MXFP8, N> {
     if constexpr (N == 16) {
       const u32x4_8 t = *reinterpret_cast<const u32x4_8*>(p);
       w[0] = t.x; w[1] = t.y; w[2] = t.z; w[3] = t.w;
-    } else {
+    } else if constexpr (N == 8) {
       const uint2 t = *reinterpret_cast<const uint2*>(p);
       w[0] = t.x; w[1] = t.y;
+    } else {
+      w[0] = *reinterpret_cast<const uint32_t*>(p);
     }
   }
   __device__ void store(uint8_t* p) const {
-    static_assert(N == 8, "pieces are written 8 codes at a time");
-    *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+    static_assert(N <= 8, "pieces are written 4 or 8 codes at a time");
+    if constexpr (N == 8) *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+    else *reinterpret_cast<uint32_t*>(p) = w[0];
   }
   __device__ void zero() {
 #pragma unroll
@@ -118,43 +121,52 @@ template <int N> struct MxPiece<FAST_MXFP8, N> {
   }
 };
 template <int N> struct MxPiece<FAST_MXFP4, N> {
-  uint32_t w[N / 8];
+  static constexpr int W = N >= 8 ? N / 8 : 1, PAIRS = N >= 8 ? 4 : 2;   // words, pairs in each
+  uint32_t w[W];
   __device__ void load(const uint8_t* p) {
     if constexpr (N == 16) {
       const u32x2_4 t = *reinterpret_cast<const u32x2_4*>(p);
       w[0] = t.x; w[1] = t.y;
-    } else {
+    } else if constexpr (N == 8) {
       w[0] = *reinterpret_cast<const uint32_t*>(p);
+    } else {
+      w[0] = *reinterpret_cast<const uint16_t*>(p);
     }
   }
   __device__ void store(uint8_t* p) const {
-    static_assert(N == 8, "pieces are written 8 codes at a time");
-    *reinterpret_cast<uint32_t*>(p) = w[0];
+    static_assert(N <= 8, "pieces are written 4 or 8 codes at a time");
+    if constexpr (N == 8) *reinterpret_cast<uint32_t*>(p) = w[0];
+    else *reinterpret_cast<uint16_t*>(p) = uint16_t(w[0]);
   }
   __device__ void zero() {
 #pragma unroll
-    for (int k = 0; k < N / 8; ++k) w[k] = 0u;
+    for (int k = 0; k < W; ++k) w[k] = 0u;
   }
   __device__ void unpack(float scale, float* x) const {
 #pragma unroll
-    for (int k = 0; k < N / 8; ++k) {
+    for (int k = 0; k < W; ++k) {
       const f32x2_t a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[k], scale, 0);
       const f32x2_t b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[k], scale, 1);
-      const f32x2_t c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[k], scale, 2);
-      const f32x2_t d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[k], scale, 3);
-      x[8 * k] = a.x; x[8 * k + 1] = a.y; x[8 * k + 2] = b.x; x[8 * k + 3] = b.y;
-      x[8 * k + 4] = c.x; x[8 * k + 5] = c.y; x[8 * k + 6] = d.x; x[8 * k + 7] = d.y;
+      float* o = x + 8 * k;
+      o[0] = a.x; o[1] = a.y; o[2] = b.x; o[3] = b.y;
+      if constexpr (PAIRS == 4) {
+        const f32x2_t c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[k], scale, 2);
+        const f32x2_t d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[k], scale, 3);
+        o[4] = c.x; o[5] = c.y; o[6] = d.x; o[7] = d.y;
+      }
     }
   }
   // round to nearest, ties to even; |x| <= 6 scale
   __device__ void pack(float scale, const float* x) {
 #pragma unroll
-    for (int k = 0; k < N / 8; ++k) {
+    for (int k = 0; k < W; ++k) {
       uint32_t t = 0;
       t = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(t, x[8 * k], x[8 * k + 1], scale, 0);
       t = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(t, x[8 * k + 2], x[8 * k + 3], scale, 1);
-      t = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(t, x[8 * k + 4], x[8 * k + 5], scale, 2);
-      t = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(t, x[8 * k + 6], x[8 * k + 7], scale, 3);
+      if constexpr (PAIRS == 4) {
+        t = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(t, x[8 * k + 4], x[8 * k + 5], scale, 2);
+        t = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(t, x[8 * k + 6], x[8 * k + 7], scale, 3);
+      }
       w[k] = t;
     }
   }
