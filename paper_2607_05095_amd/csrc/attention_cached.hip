@@ -338,65 +338,78 @@ __global__ void __launch_bounds__(CA_THREADS) k_attn_cached(CaArgs a) {
   }
 }
 
-// Joins the n pieces of segment v, which starts in cell m, for head h.  Threads over
-// the pieces find the maximum; then, CA_THREADS pieces at a time, one thread
-// per piece forms its weight, and threads (element, every slices-th piece) add
-// the weighted accumulators.
+// Joins the n pieces of segment v, which starts in cell m, for head h.  A chunk of pieces at a
+// time: a thread loads its element of CJ_AHEAD of them, and (another role of the
+// same threads) a piece's maximum and sum, all in flight together; the weights go
+// through LDS.
+constexpr int CJ_THREADS = 512, CJ_AHEAD = 8;
 template <typename T>
 __device__ __forceinline__ void ca_join(const CaArgs& a, int64_t v, int64_t m, int64_t n, int h) {
-  __shared__ float s_red[2][CA_WAVES];
-  __shared__ float s_w[CA_THREADS];
-  __shared__ float s_sum[CA_THREADS];
-  const int H = a.H, dh = a.dh, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  __shared__ float s_w[CJ_THREADS], s_sum[CJ_THREADS], s_red[2][CJ_THREADS / 64];
+  const int H = a.H, dh = a.dh, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   int cols = 1;                        // the elements of a head, padded to a power of two
   while (cols < dh) cols *= 2;
-  const int slices = CA_THREADS / cols, col = threadIdx.x & (cols - 1), sl = threadIdx.x / cols;
+  const int slices = CJ_THREADS / cols, col = tid & (cols - 1), sl = tid / cols;
+  const int chunk = CJ_AHEAD * slices < CJ_THREADS ? CJ_AHEAD * slices : CJ_THREADS;
   const int64_t step = int64_t(H) * (dh + 2);
   const float* first = a.part + (2 * m + 1) * step + h * (dh + 2);   // slot 2m + 1, then 2(m + k)
   const float* rest = a.part + 2 * m * step + h * (dh + 2);
-  auto piece = [&](int64_t k) { return k == 0 ? first : rest + 2 * k * step; };
-  float mx = -INFINITY;
-  for (int64_t k = threadIdx.x; k < n; k += CA_THREADS) mx = fmaxf(mx, piece(k)[0]);
-  for (int o = 1; o < 64; o *= 2) mx = fmaxf(mx, __shfl_xor(mx, o));
-  if (lane == 0) s_red[0][wave] = mx;
-  __syncthreads();
-  for (int w = 0; w < CA_WAVES; ++w) mx = fmaxf(mx, s_red[0][w]);
-  float Z = 0.f, acc = 0.f;
-  for (int64_t k0 = 0; k0 < n; k0 += CA_THREADS) {
-    const int c = int(n - k0 < CA_THREADS ? n - k0 : CA_THREADS);
-    if (int(threadIdx.x) < c) {
-      const float* p = piece(k0 + threadIdx.x);
-      const float w = ca_pow2(p[0], mx);
-      s_w[threadIdx.x] = w;
-      Z = fmaf(p[1], w, Z);
+  const int64_t ahead = 2 * step * slices;
+  float mx = -INFINITY, Z = 0.f, acc = 0.f;
+  for (int64_t k0 = 0; k0 < n; k0 += chunk) {
+    const int c = int(n - k0 < chunk ? n - k0 : chunk);
+    float pa[CJ_AHEAD], pm = -INFINITY, pz = 0.f;
+    const float* q = rest + 2 * (k0 + sl) * step + 2 + col;
+#pragma unroll
+    for (int i = 0; i < CJ_AHEAD; ++i, q += ahead) {
+      pa[i] = 0.f;
+      if (sl + i * slices < c && col < dh) pa[i] = *(i == 0 && k0 + sl == 0 ? first + 2 + col : q);
     }
+    if (tid < c) {
+      const float* p = k0 + tid == 0 ? first : rest + 2 * (k0 + tid) * step;
+      pm = p[0];
+      pz = p[1];
+    }
+    float mn = pm;
+    for (int o = 1; o < 64; o *= 2) mn = fmaxf(mn, __shfl_xor(mn, o));
+    if (lane == 0) s_red[0][wave] = mn;
     __syncthreads();
-    if (col < dh) {
-#pragma unroll 16
-      for (int k = sl; k < c; k += slices) acc = fmaf(piece(k0 + k)[2 + col], s_w[k], acc);
+    mn = mx;
+    for (int w = 0; w < CJ_THREADS / 64; ++w) mn = fmaxf(mn, s_red[0][w]);
+    const float corr = ca_pow2(mx, mn), weight = ca_pow2(pm, mn);
+    mx = mn;
+    Z = fmaf(pz, weight, Z * corr);
+    s_w[tid] = weight;
+    __syncthreads();
+    acc *= corr;
+#pragma unroll
+    for (int i = 0; i < CJ_AHEAD; ++i) {
+      const int k = sl + i * slices;
+      if (k < c) acc = fmaf(pa[i], s_w[k], acc);
     }
     __syncthreads();                   // before the next weights
   }
   Z = group_sum(Z, 64);
   if (lane == 0) s_red[1][wave] = Z;
-  s_sum[threadIdx.x] = acc;
+  s_sum[tid] = acc;
   __syncthreads();
   Z = 0.f;
-  for (int w = 0; w < CA_WAVES; ++w) Z += s_red[1][w];
+  for (int w = 0; w < CJ_THREADS / 64; ++w) Z += s_red[1][w];
   const bool some = !(Z == 0.f);
   if (sl == 0 && col < dh) {
     for (int k = 1; k < slices; ++k) acc += s_sum[k * cols + col];
     const float o = some ? acc / Z : 0.f;
     VecIO<T, 1>::store(static_cast<T*>(a.out) + (v * H + h) * dh + col, &o);
   }
-  if (a.lse && threadIdx.x == 0) a.lse[v * H + h] = some ? (mx + log2f(Z)) * LN2 : -INFINITY;
-  __syncthreads();                     // before the next head's sums
+  if (a.lse && tid == 0) a.lse[v * H + h] = some ? (mx + log2f(Z)) * LN2 : -INFINITY;
+  __syncthreads();                     // before the next segment's sums
 }
 
 // The marks of cells b + i CA_CELLS, and of the cells behind them, for i in [base, base + 64): a
 // lane each, one round trip for all.  Returns the lanes that have one.
-__device__ __forceinline__ uint64_t ca_marks(const CaArgs& a, int64_t base, int32_t& here, int32_t& next) {
-  const int64_t i = base + (threadIdx.x & 63), m = blockIdx.x + i * CA_CELLS;
+__device__ __forceinline__ uint64_t ca_marks(const CaArgs& a, int64_t b, int64_t base, int32_t& here,
+                                             int32_t& next) {
+  const int64_t i = base + (threadIdx.x & 63), m = b + i * CA_CELLS;
   here = i < a.rounds && m < a.cells ? a.mark[ca_mark_at(a, m)] : -1;
   next = i < a.rounds && m + 1 < a.cells ? a.mark[ca_mark_at(a, m + 1)] : -1;
   // marks of malformed offsets may be anything
@@ -413,7 +426,7 @@ __global__ void __launch_bounds__(CA_THREADS) k_attn_cached_long(CaArgs a) {
   const int64_t cap = int64_t(1) << a.shift;
   for (int64_t base = 0; base < a.rounds; base += 64) {
     int32_t here, next;
-    for (uint64_t set = ca_marks(a, base, here, next); set; set &= set - 1) {   // the same in every wave
+    for (uint64_t set = ca_marks(a, blockIdx.x, base, here, next); set; set &= set - 1) {   // the same in every wave
       const int i = __builtin_ctzll(set);
       const int64_t x = (blockIdx.x + (base + i) * CA_CELLS) << a.shift, y = x + cap;
       int32_t seg[2] = {__builtin_amdgcn_readlane(here, i), __builtin_amdgcn_readlane(next, i)};
@@ -430,23 +443,65 @@ __global__ void __launch_bounds__(CA_THREADS) k_attn_cached_long(CaArgs a) {
   }
 }
 
-// Joins the long segments that start in cells b, b + CA_CELLS, ..., head blockIdx.y: those
-// that hold the next cell's first edge.
+// Joins the long segments that start in cells b, b + CA_CELLS, ... for b = blockIdx.x, blockIdx.x +
+// gridDim.x, ..., head blockIdx.y: those that hold the next cell's first edge.
 template <typename T>
-__global__ void __launch_bounds__(CA_THREADS) k_attn_cached_join(CaArgs a) {
-  for (int64_t base = 0; base < a.rounds; base += 64) {
-    int32_t here, next;
-    for (uint64_t set = ca_marks(a, base, here, next); set; set &= set - 1) {
-      const int i = __builtin_ctzll(set);
-      const int64_t m = blockIdx.x + (base + i) * CA_CELLS;
-      const int32_t v = __builtin_amdgcn_readlane(next, i);
-      if (v < 0) continue;
-      int64_t s, t;
-      ca_segment(a, v, s, t);
-      if (t - s > (int64_t(1) << a.shift) && s >> a.shift == m)
-        ca_join<T>(a, v, m, ((t - 1) >> a.shift) - m + 1, blockIdx.y);
+__global__ void __launch_bounds__(CJ_THREADS) k_attn_cached_join(CaArgs a) {
+  for (int64_t b = blockIdx.x; b < CA_CELLS && b < a.cells; b += gridDim.x) {
+    for (int64_t base = 0; base < a.rounds; base += 64) {
+      int32_t here, next;
+      for (uint64_t set = ca_marks(a, b, base, here, next); set; set &= set - 1) {
+        const int i = __builtin_ctzll(set);
+        const int64_t m = b + (base + i) * CA_CELLS;
+        const int32_t v = __builtin_amdgcn_readlane(next, i);
+        if (v < 0) continue;
+        int64_t s, t;
+        ca_segment(a, v, s, t);
+        if (t - s > (int64_t(1) << a.shift) && s >> a.shift == m)
+          ca_join<T>(a, v, m, ((t - 1) >> a.shift) - m + 1, blockIdx.y);
+      }
     }
   }
+}
+
+// Fewer than 64 segments: every wave holds all offsets, so that pieces and whole segments go
+// in one launch, without marks.  Workgroups [0, cells) take the pieces of their cell, the
+// others a wave per short segment.
+constexpr int CA_FEW = 64;
+template <typename T, int FMT, int VE, int LPH, bool BIG>
+__global__ void __launch_bounds__(CA_THREADS) k_attn_cached_few(CaArgs a) {
+  __shared__ float s_acc[CA_WAVES][VE + 2][64];
+  const int lane = threadIdx.x & 63;
+  const int64_t cap = int64_t(1) << a.shift, m = blockIdx.x;
+  if (m < a.cells) {
+    const int64_t x = m << a.shift, y = x + cap;
+    const int o = lane <= a.N ? int(clamp64(a.off[lane], 0, a.E)) : int(a.E);
+    int e = __shfl_down(o, 1);
+    e = e > o ? e : o;
+    const bool mine = lane < a.N && e - o > cap && o < y && e > x;
+    for (uint64_t set = __ballot(mine); set; set &= set - 1) {
+      const int v = __builtin_ctzll(set);
+      const int64_t s = __builtin_amdgcn_readlane(o, v), t = __builtin_amdgcn_readlane(e, v);
+      ca_piece<T, FMT, VE, LPH, BIG>(a, v, s > x ? s : x, t < y ? t : y, 2 * m + (s >= x ? 1 : 0), s_acc);
+    }
+    return;
+  }
+  const int64_t v = (m - a.cells) * CA_WAVES + (threadIdx.x >> 6);
+  if (v >= a.N) return;
+  int64_t s, t;
+  ca_segment(a, v, s, t);
+  if (t - s > cap) return;
+  CaLane<VE> c;
+  ca_init<T, FMT, VE, LPH>(a, v, c);
+  ca_wave<FMT, VE, LPH, BIG>(a, s, t, c);
+  if (lane < a.L) ca_store<T, VE>(a, v, c);
+}
+template <typename T>
+__global__ void __launch_bounds__(CJ_THREADS) k_attn_cached_few_join(CaArgs a) {
+  int64_t s, t;
+  ca_segment(a, blockIdx.x, s, t);
+  if (t - s > int64_t(1) << a.shift)
+    ca_join<T>(a, blockIdx.x, s >> a.shift, ((t - 1) >> a.shift) - (s >> a.shift) + 1, blockIdx.y);
 }
 
 // A wave per segment where they are few, or long; else L lanes each.
@@ -468,17 +523,23 @@ static int pow2_at_least(int x) {
   return p;
 }
 
+// FEW: fewer than CA_FEW segments, at least one of which may be long.
+enum CaMode { CA_GROUP, CA_WAVE, CA_FEW_MODE };
 template <typename T, int FMT>
-static void launch_ca(const CaArgs& a, int ve, bool big, bool wave, dim3 grid, dim3 long_grid,
+static void launch_ca(const CaArgs& a, int ve, bool big, CaMode mode, dim3 grid, dim3 long_grid,
                       hipStream_t st) {
-#define FAST_CA(V, N, B)                                                                             \
-  do {                                                                                               \
-    if (wave)                                                                                        \
-      hipLaunchKernelGGL((k_attn_cached<T, FMT, V, N, B, true>), grid, dim3(CA_THREADS), 0, st, a);  \
-    else                                                                                             \
-      hipLaunchKernelGGL((k_attn_cached<T, FMT, V, N, B, false>), grid, dim3(CA_THREADS), 0, st, a); \
-    if (a.cells > 0)                                                                                 \
-      hipLaunchKernelGGL((k_attn_cached_long<T, FMT, V, N, B>), long_grid, dim3(CA_THREADS), 0, st, a); \
+#define FAST_CA(V, N, B)                                                                                 \
+  do {                                                                                                   \
+    if (mode == CA_FEW_MODE) {                                                                           \
+      hipLaunchKernelGGL((k_attn_cached_few<T, FMT, V, N, B>), grid, dim3(CA_THREADS), 0, st, a);        \
+      break;                                                                                             \
+    }                                                                                                    \
+    if (mode == CA_WAVE)                                                                                 \
+      hipLaunchKernelGGL((k_attn_cached<T, FMT, V, N, B, true>), grid, dim3(CA_THREADS), 0, st, a);      \
+    else                                                                                                 \
+      hipLaunchKernelGGL((k_attn_cached<T, FMT, V, N, B, false>), grid, dim3(CA_THREADS), 0, st, a);     \
+    if (a.cells > 0)                                                                                     \
+      hipLaunchKernelGGL((k_attn_cached_long<T, FMT, V, N, B>), long_grid, dim3(CA_THREADS), 0, st, a);  \
   } while (0)
   if (ve == 8) FAST_CA(8, 0, true);
   else if (big) FAST_CA(16, 0, true);
@@ -577,23 +638,32 @@ extern "C" fast_status_t fast_edge_attention_fwd_cached(
   a.mark = reinterpret_cast<int32_t*>(static_cast<char*>(ws) + ca_part_bytes(a.cells, H, dh));
   const int64_t per = wave ? CA_WAVES : CA_THREADS / a.L;
   const uint32_t heads = uint32_t((H + hpw - 1) / hpw);
-  const dim3 grid(uint32_t((N + per - 1) / per), heads);
+  const bool few = N < CA_FEW && a.cells > 0;
+  const CaMode mode = few ? CA_FEW_MODE : wave ? CA_WAVE : CA_GROUP;
+  const dim3 grid(uint32_t((few ? a.cells : 0) + (N + per - 1) / per), heads);
   const uint32_t cells = uint32_t(a.cells < CA_CELLS ? a.cells : CA_CELLS);
   const dim3 long_grid(cells, heads);
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (dtype == FAST_F32) {
-    if (format == FAST_MXFP8) launch_ca<float, FAST_MXFP8>(a, ve, big, wave, grid, long_grid, st);
-    else launch_ca<float, FAST_MXFP4>(a, ve, big, wave, grid, long_grid, st);
+    if (format == FAST_MXFP8) launch_ca<float, FAST_MXFP8>(a, ve, big, mode, grid, long_grid, st);
+    else launch_ca<float, FAST_MXFP4>(a, ve, big, mode, grid, long_grid, st);
   } else {
-    if (format == FAST_MXFP8) launch_ca<uint16_t, FAST_MXFP8>(a, ve, big, wave, grid, long_grid, st);
-    else launch_ca<uint16_t, FAST_MXFP4>(a, ve, big, wave, grid, long_grid, st);
+    if (format == FAST_MXFP8) launch_ca<uint16_t, FAST_MXFP8>(a, ve, big, mode, grid, long_grid, st);
+    else launch_ca<uint16_t, FAST_MXFP4>(a, ve, big, mode, grid, long_grid, st);
   }
-  if (a.cells > 0) {
-    const dim3 join_grid(cells, uint32_t(H));
+  if (few) {
+    const dim3 join_grid = dim3(uint32_t(N), uint32_t(H));
     if (dtype == FAST_F32)
-      hipLaunchKernelGGL((k_attn_cached_join<float>), join_grid, dim3(CA_THREADS), 0, st, a);
+      hipLaunchKernelGGL((k_attn_cached_few_join<float>), join_grid, dim3(CJ_THREADS), 0, st, a);
     else
-      hipLaunchKernelGGL((k_attn_cached_join<uint16_t>), join_grid, dim3(CA_THREADS), 0, st, a);
+      hipLaunchKernelGGL((k_attn_cached_few_join<uint16_t>), join_grid, dim3(CJ_THREADS), 0, st, a);
+  } else if (a.cells > 0) {
+    const uint32_t lists = 512 / uint32_t(H);        // about 512 workgroups in all
+    const dim3 join_grid(cells < lists ? cells : lists, uint32_t(H));
+    if (dtype == FAST_F32)
+      hipLaunchKernelGGL((k_attn_cached_join<float>), join_grid, dim3(CJ_THREADS), 0, st, a);
+    else
+      hipLaunchKernelGGL((k_attn_cached_join<uint16_t>), join_grid, dim3(CJ_THREADS), 0, st, a);
   }
   return check_launch(fn);
 }
