@@ -538,7 +538,8 @@ fast_status_t fast_index_add_scaled_rows(const int32_t* occ_off, const int32_t* 
  * are those of the row that `sum` ([n, D], optional, only with res) stores and the backward
  * reads.  mean, rstd: [n] fp32, optional (the backward needs both).
  * Statistics and products are fp32, the mean taken before the squares.
- * Limits: 1 <= D <= 8192, n < 2^31.  Rows aligned to their element; y and sum
+ * Limits: 1 <= D <= 8192, n < 2^31, and (as for the operators below) fewer than
+ * 2^32 threads: rows of some 1.7e10 elements.  Rows aligned to their element; y and sum
  * may each be x or res, not both the same.  eps >= 0.
  * ------------------------------------------------------------------------ */
 fast_status_t fast_layer_norm_fwd(int64_t n, int D, fast_dtype_t dtype, const void* x,

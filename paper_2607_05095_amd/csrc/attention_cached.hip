@@ -642,6 +642,7 @@ extern "C" fast_status_t fast_edge_attention_fwd_cached(
   const CaMode mode = few ? CA_FEW_MODE : wave ? CA_WAVE : CA_GROUP;
   const dim3 grid(uint32_t((few ? a.cells : 0) + (N + per - 1) / per), heads);
   const uint32_t cells = uint32_t(a.cells < CA_CELLS ? a.cells : CA_CELLS);
+  if (!grid_fits(grid.x, CA_THREADS)) return fail(FAST_ERR_UNSUPPORTED, "%s: 2^32 threads or more", fn);
   const dim3 long_grid(cells, heads);
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (dtype == FAST_F32) {

@@ -242,6 +242,8 @@ extern "C" fast_status_t fast_cache_write(const int64_t* ids, int64_t n, int64_t
     if (!aligned(ws, 16)) return fail(FAST_ERR_UNSUPPORTED, "%s: workspace not 16-byte aligned", fn);
   }
   CacheArgs a = cache_args(ids, n, id_bound, slot_map, parts, width, format, cache_rows, dtype, true);
+  const dim3 grid = cache_grid(a);
+  if (!grid_fits(grid.x, CR_THREADS)) return fail(FAST_ERR_UNSUPPORTED, "%s: 2^32 threads or more", fn);
   a.src = src;
   a.cache = static_cast<uint8_t*>(cache);
   hipStream_t st = static_cast<hipStream_t>(stream);
@@ -252,7 +254,6 @@ extern "C" fast_status_t fast_cache_write(const int64_t* ids, int64_t n, int64_t
     hipLaunchKernelGGL(k_cache_claim, dim3(g), dim3(CR_THREADS), 0, st, a, 0);
     hipLaunchKernelGGL(k_cache_claim, dim3(g), dim3(CR_THREADS), 0, st, a, 1);
   }
-  const dim3 grid = cache_grid(a);
 #define FAST_CW(T, F) hipLaunchKernelGGL((k_cache_write<T, F>), grid, dim3(CR_THREADS), 0, st, a)
   if (dtype == FAST_F32) {
     if (format == FAST_MXFP8) FAST_CW(float, FAST_MXFP8);
@@ -279,6 +280,7 @@ extern "C" fast_status_t fast_cache_gather(const int64_t* ids, int64_t n, int64_
   a.dst = rows;
   a.cache_in = static_cast<const uint8_t*>(cache);
   const dim3 grid = cache_grid(a);
+  if (!grid_fits(grid.x, CR_THREADS)) return fail(FAST_ERR_UNSUPPORTED, "%s: 2^32 threads or more", fn);
   hipStream_t st = static_cast<hipStream_t>(stream);
   // Rows that would fill a good part of the 256 MB last-level cache are streamed past it:
   // 1.3 M rows of 172 fp32 from 8 bits 280 -> 208 us; write and read of 300,000 rows of

@@ -237,6 +237,14 @@ __global__ void __launch_bounds__(LN_MAX_G) k_ln_bwd(LnBwdArgs a) {
 #pragma unroll
         for (int j = 0; j < VE; ++j) d[p][j] = 0.f;
     }
+    // dx may take dsum's place, and a last chunk reads elements that another wave writes: they
+    // have arrived before the barrier in row_sums lets that wave go on
+    if constexpr (TAIL) {
+#pragma unroll
+      for (int p = 0; p < P; ++p)
+#pragma unroll
+        for (int j = 0; j < VE; ++j) asm volatile("" : "+v"(d[p][j]));
+    }
     float s1 = 0.f, s2 = 0.f;
 #pragma unroll
     for (int p = 0; p < P; ++p) {
@@ -440,6 +448,7 @@ extern "C" fast_status_t fast_layer_norm_fwd(int64_t n, int D, fast_dtype_t dtyp
   const LnArgs a = {n, D, L.G, x, res, gamma, beta, eps, y, sum, mean, rstd};
   const int64_t per = L.threads / L.G;
   const uint32_t grid = uint32_t((n + per - 1) / per);
+  if (!grid_fits(grid, L.threads)) return fail(FAST_ERR_UNSUPPORTED, "%s: 2^32 threads or more", fn);
   hipStream_t st = static_cast<hipStream_t>(stream);
   const void* rows[] = {x, res, y, sum};
   const bool nt = ln_stream(n, D, es, 2 + (res != nullptr) + (sum != nullptr), rows, 4);
@@ -479,6 +488,7 @@ extern "C" fast_status_t fast_layer_norm_bwd(int64_t n, int D, fast_dtype_t dtyp
   }
   if (n == 0 && !sums) return ok();
   const LnPlan L = ln_plan(n, D, 16 / int(es));
+  if (!grid_fits(L.nb, L.threads)) return fail(FAST_ERR_UNSUPPORTED, "%s: 2^32 threads or more", fn);
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (n > 0) {
     const LnBwdArgs a = {n, D, L.G, h, gamma, mean, rstd, dy, dsum, dx,

@@ -208,6 +208,7 @@ static fast_status_t rotary(const char* fn, int64_t n, int H, int dh, fast_dtype
   a.omega = omega;
   a.sign = sign;
   const dim3 grid(uint32_t((n + a.rows - 1) / a.rows), uint32_t((a.rows * a.upr + tile - 1) / tile));
+  if (!grid_fits(grid.x, ROT_THREADS)) return fail(FAST_ERR_UNSUPPORTED, "%s: 2^32 threads or more", fn);
   hipStream_t st = static_cast<hipStream_t>(stream);
   // Rows of whole cache lines that go out in one stream (pairs side by side) bypass the
   // cache when rows and results are more than its last level holds: 1,000,000 rows

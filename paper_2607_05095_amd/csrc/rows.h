@@ -106,6 +106,9 @@ __device__ __forceinline__ void store_chunk(T* __restrict__ p, int n, const floa
   store_chunk_of<NT>(p, n, x);
 }
 
+// A launch has fewer than 2^32 threads along an axis.
+inline bool grid_fits(int64_t blocks, int64_t threads) { return blocks * threads < (int64_t(1) << 32); }
+
 // t / d for t * d < 2^32 with the multiplier of div_magic(d): one high product.
 inline uint32_t div_magic(uint32_t d) {
   return d <= 1 ? 0u : uint32_t(((uint64_t(1) << 32) + d - 1) / d);

@@ -150,6 +150,17 @@ def test_cache_past_four_gib():
                                         1.0, 0.2, res, None, ws, wsb)
     mean = want[:, 2:].mean(0)                     # a zero query weighs every edge alike
     assert (np.abs(host(res)[0] - mean) <= 20 * U * np.abs(want[:, 2:]).max(0)).all()
+    # many segments of one edge each return that edge's value
+    N = 5000
+    pick = np.arange(N) % len(ids)
+    Q = torch.randn(N, 2, 50, device="cuda")
+    res = torch.empty(N, 2, 50, device="cuda")
+    g = fast.tcsr(torch.arange(N + 1, dtype=torch.int32, device="cuda"), N)
+    wsb = fast.fast_edge_attention_cached_workspace(N, N, 2, 50)
+    ws = torch.empty(wsb, dtype=torch.uint8, device="cuda")
+    fast.fast_edge_attention_fwd_cached(g, 2, 50, fast.F32, Q, to_dev(ids[pick]), rows, None, fast.MXFP8, cache, rows,
+                                        1.0, 0.2, res, None, ws, wsb)
+    np.testing.assert_array_equal(host(res), want[pick, 2:])
     del cache
 
 
@@ -229,6 +240,19 @@ def test_cached_attention_shapes(H, dh, fmt, dt):
 def test_cached_attention_lengths(counts, dt):
     print(f"[cache] attention lengths N={len(counts)} E={sum(counts)} {dt}", flush=True)
     b = Block(counts, 2, 50, 8, dt, seed=len(counts))
+    b.check(*b.run())
+
+
+@pytest.mark.parametrize("H,dh", [(1, 1), (1, 8), (3, 7), (2, 50), (8, 128), (2, 256), (64, 16), (20, 50), (1, 100),
+                                  (5, 43), (4, 40)])
+@pytest.mark.parametrize("fmt", [8, 4])
+def test_cached_attention_many_segments(H, dh, fmt):
+    """More segments than a wave each is chosen for: a few lanes per segment, empty and long ones among them."""
+    print(f"[cache] attention many segments H={H} dh={dh} fmt={fmt}", flush=True)
+    r = np.random.default_rng(dh)
+    counts = r.integers(0, 6, 4500)
+    counts[[7, 900, 901, 4499]] = [300, 70, 257, 1100]
+    b = Block(counts, H, dh, fmt, "f32" if H % 2 else "bf16", seed=dh + H)
     b.check(*b.run())
 
 

@@ -72,6 +72,9 @@ def test_layer_norm_fwd(n, D, dt, res):
     if res:
         np.testing.assert_array_equal(host(h[:n]), h64)
         assert (h[n] == 7).all()
+        x2, r2 = x.clone(), r.clone()             # the sum in x's place, y in res's
+        fast.fast_layer_norm_fwd(n, D, DT[dt], x2, r2, ga, be, 1e-5, r2, x2)
+        assert torch.equal(x2, h[:n]) and torch.equal(r2, y[:n])
     assert (y[n] == 7).all() and float(mean[n]) == 0 and float(rstd[n]) == 0
 
 
@@ -137,6 +140,10 @@ def test_layer_norm_bwd(n, D, dt, dsum):
     assert torch.equal(dg2, dg[:D]) and torch.equal(dx2, dx[:n])
     fast.fast_layer_norm_bwd(n, D, DT[dt], h, ga, mean, rstd, dy, ds, dx2, None, None, None, 0)
     assert torch.equal(dx2, dx[:n])
+    if dsum:                                      # dx in dsum's place
+        dx3 = ds.clone()
+        fast.fast_layer_norm_bwd(n, D, DT[dt], h, ga, mean, rstd, dy, dx3, dx3, None, None, None, 0)
+        assert torch.equal(dx3, dx[:n])
 
 
 def test_layer_norm_bwd_without_rows_zeroes_the_weight_gradients():

@@ -50,6 +50,18 @@ def test_layer_norm_bwd_refusals(kw, status):
     assert call("fast_layer_norm_bwd", NORM_B, kw) == status
 
 
+def test_launches_past_the_thread_limit_are_refused():
+    """Sizes whose launch would need 2^32 threads: refused before anything is enqueued."""
+    assert call("fast_layer_norm_fwd", NORM, dict(n=BIG - 1, D=500)) == UNSUPPORTED
+    assert call("fast_rotary_fwd", ROT, dict(n=BIG - 1, H=8, dh=16, ldx=256, ldy=256, pairs=8, x=FAKE,
+                                             y=FAKE + 4 * 128)) == UNSUPPORTED
+    assert call("fast_cache_write", CW, dict(n=BIG - 1, parts=8, width=32, distinct=1)) == UNSUPPORTED
+    assert call("fast_cache_gather", CG, dict(n=BIG - 1, parts=8, width=32)) == UNSUPPORTED
+    a = dict(ATT, dh=256, Q=FAKE, ws=FAKE, wsb=1 << 40)
+    a["g"] = ctypes.byref(fast.TCSR(BIG - 1, 10, FAKE, None, None, None, None))
+    assert fast.lib().fast_edge_attention_fwd_cached(*a.values()) == UNSUPPORTED
+
+
 def test_layer_norm_workspace():
     assert fast.fast_layer_norm_bwd_workspace(0, 8) > 0
     assert fast.fast_layer_norm_bwd_workspace(-1, 8) == 0
