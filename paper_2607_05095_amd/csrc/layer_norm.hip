@@ -203,7 +203,7 @@ __global__ void __launch_bounds__(LN_MAX_G) k_ln_bwd(LnBwdArgs a) {
   typedef LnChunk<VE, TAIL> Chunk;
   __shared__ float2 s_red[2 * (LN_MAX_G / 64)];
   LnSum red = {s_red, 0};
-  extern __shared__ double s_col[];     // [D] where the workgroup holds several groups
+  extern __shared__ float s_col[];      // [groups][2][D] where the workgroup holds several groups
   const int G = a.G, lane = threadIdx.x & (G - 1), sub = threadIdx.x / G, groups = blockDim.x / G;
   const int D = a.D;
   // rows b, b + workgroups, ... (in units of a workgroup's groups), so that the chip reads
@@ -272,40 +272,35 @@ __global__ void __launch_bounds__(LN_MAX_G) k_ln_bwd(LnBwdArgs a) {
   }
   if (!a.part) return;
   float* out = a.part + int64_t(blockIdx.x) * 2 * D;
-  const int wave = threadIdx.x >> 6;
-  for (int which = 0; which < 2; ++which) {
-    double c[P][VE];
+  if (groups == 1) {                     // the lanes of the workgroup own different columns
 #pragma unroll
-    for (int p = 0; p < P; ++p)
+    for (int p = 0; p < P; ++p) {
+      const Chunk k(lane + p * G, D);
 #pragma unroll
-      for (int j = 0; j < VE; ++j) {
-        c[p][j] = which ? db[p][j] : dg[p][j];
-        for (int o = G; o < 64; o *= 2) c[p][j] += __shfl_xor(c[p][j], o);   // the groups of a wave
-      }
-    if (groups == 1) {                   // the lanes of the workgroup own different columns
-#pragma unroll
-      for (int p = 0; p < P; ++p) {
-        const Chunk k(lane + p * G, D);
-#pragma unroll
-        for (int j = 0; j < VE; ++j)
-          if (k.own(j)) out[which * D + k.first + j] = float(c[p][j]);
-      }
-      continue;
-    }
-    for (int w = 0; w < LN_THREADS / 64; ++w) {   // the waves in order (several groups: LN_THREADS threads)
-      if (wave == w && (threadIdx.x & 63) < G) {
-#pragma unroll
-        for (int p = 0; p < P; ++p) {
-          const Chunk k(lane + p * G, D);
-#pragma unroll
-          for (int j = 0; j < VE; ++j)
-            if (k.own(j)) s_col[k.first + j] = (w ? s_col[k.first + j] : 0.0) + c[p][j];
+      for (int j = 0; j < VE; ++j)
+        if (k.own(j)) {
+          out[k.first + j] = dg[p][j];
+          out[D + k.first + j] = db[p][j];
         }
-      }
-      __syncthreads();
     }
-    for (int col = threadIdx.x; col < D; col += LN_THREADS) out[which * D + col] = float(s_col[col]);
-    __syncthreads();                     // read before the next sums overwrite it
+    return;
+  }
+#pragma unroll
+  for (int p = 0; p < P; ++p) {
+    const Chunk k(lane + p * G, D);
+#pragma unroll
+    for (int j = 0; j < VE; ++j)
+      if (k.own(j)) {
+        s_col[2 * sub * D + k.first + j] = dg[p][j];
+        s_col[(2 * sub + 1) * D + k.first + j] = db[p][j];
+      }
+  }
+  __syncthreads();
+  for (int col = threadIdx.x; col < 2 * D; col += LN_THREADS) {   // the groups in order
+    double t = 0.0;
+#pragma unroll 8
+    for (int k = 0; k < groups; ++k) t += s_col[2 * k * D + col];
+    out[col] = float(t);
   }
 }
 
@@ -357,8 +352,8 @@ static LnPlan ln_plan(int64_t n, int D, int ve) {
         L.P = P;
       }
   L.threads = L.G > 64 ? L.G : LN_THREADS;
-  // 4 workgroups per CU (2 / 4 / 8: 23 / 19 / 26 us for 66,000 rows of 128 bf16, the
-  // partial rows' sums included: 27 / 23 / 31), and at most LN_ROWS rows per group
+  // 4 workgroups per CU (4 / 6 / 8 / 16: 15.2 / 17.7 / 17.7 / 19.0 us for 66,000 rows of 128
+  // bf16, and 4.0 to 5.6 for the partial rows' sums), and at most LN_ROWS rows per group
   const int64_t groups = L.threads / L.G;
   int64_t per = (n + LN_BLOCKS * groups - 1) / (LN_BLOCKS * groups);
   per = per < 1 ? 1 : (per > LN_ROWS ? LN_ROWS : per);
@@ -493,7 +488,8 @@ extern "C" fast_status_t fast_layer_norm_bwd(int64_t n, int D, fast_dtype_t dtyp
   if (n > 0) {
     const LnBwdArgs a = {n, D, L.G, h, gamma, mean, rstd, dy, dsum, dx,
                          sums ? static_cast<float*>(ws) : nullptr};
-    const size_t lds = sums && L.G < L.threads ? size_t(D) * sizeof(double) : 0;
+    // at most 32 KB: a lane owns at most LN_ELEMS columns
+    const size_t lds = sums && L.G < L.threads ? size_t(L.threads / L.G) * 2 * D * sizeof(float) : 0;
     const void* rows[] = {h, dy, dsum, dx};
     const bool nt = ln_stream(n, D, es, 3 + (dsum != nullptr), rows, 4);
     launch_ln(a, L, uint32_t(L.nb), lds, dtype, nt, st);
