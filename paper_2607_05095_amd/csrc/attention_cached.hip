@@ -34,7 +34,8 @@ namespace fast {
 constexpr int CA_THREADS = 256, CA_WAVES = CA_THREADS / 64;
 constexpr int CA_ROWS = 4;           // records in flight per lane
 constexpr int CA_AHEAD = 2;          // places that a lane looks up at once
-constexpr int CA_SHIFT = 8, CA_SHIFT_MAX = 10;   // cap = 256 .. 1024
+constexpr int CA_SHIFT = 8, CA_SHIFT_MAX = 11;   // cap = 256 .. 2048 (4096: see ca_plan)
+constexpr int CA_BLOCKS = 2048;      // segments that get a workgroup each, at most: 8 per CU
 constexpr int CA_CELLS = 1024;       // workgroups of the second launch, at most: 4 per CU (a power of two)
 
 struct CaArgs {
@@ -239,7 +240,7 @@ __device__ __forceinline__ void ca_store(const CaArgs& a, int64_t v, CaLane<VE>&
   if (a.lse && c.l == 0) a.lse[v * a.H + c.h] = some ? (c.mx + log2f(c.Z)) * LN2 : -INFINITY;
 }
 
-// Edges [e0, e1) of segment v by a workgroup, into partial result `slot`.
+// Edges [e0, e1) of segment v by a workgroup, into partial result `slot` (-1: they are the segment).
 template <typename T, int FMT, int VE, int LPH, bool BIG>
 __device__ __forceinline__ void ca_piece(const CaArgs& a, int64_t v, int64_t e0, int64_t e1, int64_t slot,
                                          float (*s_acc)[VE + 2][64]) {
@@ -265,14 +266,20 @@ __device__ __forceinline__ void ca_piece(const CaArgs& a, int64_t v, int64_t e0,
 #pragma unroll
       for (int j = 0; j < VE; ++j) c.acc[j] = fmaf(s_acc[w][j][lane], k, c.acc[j]);
     }
-    float* p = a.part + (slot * a.H + c.h) * (a.dh + 2);
-    if (c.l == 0) {
-      p[0] = mx;
-      p[1] = Z;
-    }
+    if (slot < 0) {
+      c.mx = mx;
+      c.Z = Z;
+      ca_store<T, VE>(a, v, c);
+    } else {
+      float* p = a.part + (slot * a.H + c.h) * (a.dh + 2);
+      if (c.l == 0) {
+        p[0] = mx;
+        p[1] = Z;
+      }
 #pragma unroll
-    for (int j = 0; j < VE; ++j)
-      if (c.first + j >= c.own && c.first + j < a.dh) p[2 + c.first + j] = c.acc[j];
+      for (int j = 0; j < VE; ++j)
+        if (c.first + j >= c.own && c.first + j < a.dh) p[2 + c.first + j] = c.acc[j];
+    }
   }
   __syncthreads();                     // before the next piece of this workgroup
 }
@@ -291,18 +298,27 @@ __device__ __forceinline__ void ca_mark(const CaArgs& a, int64_t v, int64_t s, i
   for (int64_t m = first + lane; m <= last; m += n) a.mark[ca_mark_at(a, m)] = t - s > cap ? int32_t(v) : -1;
 }
 
-// WAVE: a wave per segment, else L lanes per segment.
-template <typename T, int FMT, int VE, int LPH, bool BIG, bool WAVE>
+// Who owns a segment: L lanes, a wave, or a workgroup.
+enum CaOwner { CA_GROUP, CA_WAVE, CA_BLOCK };
+template <typename T, int FMT, int VE, int LPH, bool BIG, CaOwner OWNER>
 __global__ void __launch_bounds__(CA_THREADS) k_attn_cached(CaArgs a) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t cap = int64_t(1) << a.shift;
   CaLane<VE> c;
   int64_t s, t;
-  if constexpr (WAVE) {
+  if constexpr (OWNER == CA_BLOCK) {
+    __shared__ float s_acc[CA_WAVES][VE + 2][64];
+    const int64_t v = blockIdx.x;
+    ca_segment(a, v, s, t);
+    if (a.cells > 0) ca_mark(a, v, s, t, threadIdx.x, CA_THREADS);
+    if (t - s > cap) return;           // in pieces
+    ca_piece<T, FMT, VE, LPH, BIG>(a, v, s, t, -1, s_acc);
+  } else if constexpr (OWNER == CA_WAVE) {
     const int64_t v = int64_t(blockIdx.x) * CA_WAVES + wave;
     if (v >= a.N) return;
     ca_segment(a, v, s, t);
     if (a.cells > 0) ca_mark(a, v, s, t, lane, 64);
-    if (t - s > int64_t(1) << a.shift) return;   // in pieces
+    if (t - s > cap) return;
     ca_init<T, FMT, VE, LPH>(a, v, c);
     ca_wave<FMT, VE, LPH, BIG>(a, s, t, c);
     if (lane < a.L) ca_store<T, VE>(a, v, c);
@@ -312,7 +328,7 @@ __global__ void __launch_bounds__(CA_THREADS) k_attn_cached(CaArgs a) {
     if (v >= a.N) return;
     ca_segment(a, v, s, t);
     if (a.cells > 0) ca_mark(a, v, s, t, gl, L);
-    if (t - s > int64_t(1) << a.shift) return;
+    if (t - s > cap) return;
     ca_init<T, FMT, VE, LPH>(a, v, c);
     CaCodes<FMT, VE> codes;
     codes.zero();
@@ -466,7 +482,7 @@ __global__ void __launch_bounds__(CJ_THREADS) k_attn_cached_join(CaArgs a) {
 
 // Fewer than 64 segments: every wave holds all offsets, so that pieces and whole segments go
 // in one launch, without marks.  Workgroups [0, cells) take the pieces of their cell, the
-// others a wave per short segment.
+// others a short segment each.
 constexpr int CA_FEW = 64;
 template <typename T, int FMT, int VE, int LPH, bool BIG>
 __global__ void __launch_bounds__(CA_THREADS) k_attn_cached_few(CaArgs a) {
@@ -486,15 +502,10 @@ __global__ void __launch_bounds__(CA_THREADS) k_attn_cached_few(CaArgs a) {
     }
     return;
   }
-  const int64_t v = (m - a.cells) * CA_WAVES + (threadIdx.x >> 6);
-  if (v >= a.N) return;
+  const int64_t v = m - a.cells;
   int64_t s, t;
   ca_segment(a, v, s, t);
-  if (t - s > cap) return;
-  CaLane<VE> c;
-  ca_init<T, FMT, VE, LPH>(a, v, c);
-  ca_wave<FMT, VE, LPH, BIG>(a, s, t, c);
-  if (lane < a.L) ca_store<T, VE>(a, v, c);
+  if (t - s <= cap) ca_piece<T, FMT, VE, LPH, BIG>(a, v, s, t, -1, s_acc);
 }
 template <typename T>
 __global__ void __launch_bounds__(CJ_THREADS) k_attn_cached_few_join(CaArgs a) {
@@ -504,58 +515,81 @@ __global__ void __launch_bounds__(CJ_THREADS) k_attn_cached_few_join(CaArgs a) {
     ca_join<T>(a, blockIdx.x, s >> a.shift, ((t - 1) >> a.shift) - (s >> a.shift) + 1, blockIdx.y);
 }
 
-// A wave per segment where they are few, or long; else L lanes each.
-static bool ca_wave_each(int64_t N, int64_t E, int L) {
-  return N <= 4096 || E / N >= 2 * CA_ROWS * (64 / L);
-}
-
-// Piece length: a workgroup's 4 waves take 64 edges each; more where a wave owns a segment
-// (a few lanes would be long over 1024 edges) and there are pieces enough.
-static int ca_shift(int64_t E, bool wave) {
-  int s = CA_SHIFT;
-  while (wave && s < CA_SHIFT_MAX && (E >> (s + 1)) >= 2 * CA_CELLS) ++s;
-  return s;
-}
-
 static int pow2_at_least(int x) {
   int p = 1;
   while (p < x) p *= 2;
   return p;
 }
 
-// FEW: fewer than CA_FEW segments, at least one of which may be long.
-enum CaMode { CA_GROUP, CA_WAVE, CA_FEW_MODE };
+// How a call is carried out.
+struct CaPlan {
+  int ve, lph, L;
+  CaOwner owner;
+  bool few;                            // k_attn_cached_few
+  int shift;
+  int64_t cells;
+};
+static CaPlan ca_plan(int64_t N, int64_t E, int H, int dh) {
+  CaPlan p = {};
+  // 16 codes a lane (fewer instructions per record) where every lane's codes lie in
+  // one group: a head's last piece may start 8 codes early, which crosses a
+  // group's border where 1 to 8 elements are left past one.
+  p.ve = dh > 8 && (dh % MX_GROUP == 0 || dh % MX_GROUP > 8) ? 16 : 8;
+  p.lph = pow2_at_least((dh + p.ve - 1) / p.ve);
+  int hpw = pow2_at_least(H);
+  if (hpw > 64 / p.lph) hpw = 64 / p.lph;
+  p.L = p.lph * hpw;
+  // A wave per segment where they are few or longer than two rounds of its lanes, else L lanes;
+  // a workgroup where workgroups are few and the mean segment gives each wave work.
+  // L lanes / wave / workgroup, us, 4 x 32 bf16: 20,000 segments of 10 edges 31 / 39 / 109, 5000 of
+  // 10 16 / 16 / 33, 3000 of 100 74 / 33 / 34, 400 of 250 162 / 30 / 19, 600 of 10 12 / 9 / 11.
+  const int64_t mean = N > 0 ? E / N : 0;
+  if (mean >= 64 && N <= CA_BLOCKS) p.owner = CA_BLOCK;
+  else if (N <= 4096 || mean >= 2 * CA_ROWS * (64 / p.L)) p.owner = CA_WAVE;
+  else p.owner = CA_GROUP;
+  // Pieces of 256 edges: a workgroup's 4 waves take 64 each.  Longer ones
+  //   - where there are about 500 all the same, as they join faster (256 / 2048 edges, one
+  //     segment of 1,000,000 edges 4 x 32 bf16: 121 / 79 us; four of 100,003 in all: 22 / 50),
+  //   - where a whole block is no more than a workgroup gets through meanwhile (cutting
+  //     takes two launches): four segments of 1000 edges in all 11 / 8 us,
+  //   - where many segments are about that long, so that most are not cut (256 / 512, 5000
+  //     segments of 200 on average 163 / 86; 256 / 2048, 100 of 1000: 35 / 29).
+  // Not where a few lanes own a segment: they would be long over one of 1024.
+  p.shift = CA_SHIFT;
+  if (p.owner != CA_GROUP) {
+    while (p.shift < CA_SHIFT_MAX && (E >> (p.shift + 1)) >= 480) ++p.shift;
+    if (E <= 1024 && p.shift < 10) p.shift = 10;
+    if (N >= 32 && mean <= 2048)
+      while ((int64_t(1) << p.shift) < 2 * mean) ++p.shift;
+  }
+  // cells of cap edges; none where no segment can be long
+  p.cells = E > (int64_t(1) << p.shift) ? ((E - 1) >> p.shift) + 1 : 0;
+  p.few = N < CA_FEW && p.cells > 0;
+  return p;
+}
+static size_t ca_part_bytes(int64_t cells, int H, int dh) {
+  return align_up(size_t(2 * cells) * H * (dh + 2) * sizeof(float), 16);
+}
+
 template <typename T, int FMT>
-static void launch_ca(const CaArgs& a, int ve, bool big, CaMode mode, dim3 grid, dim3 long_grid,
-                      hipStream_t st) {
-#define FAST_CA(V, N, B)                                                                                 \
-  do {                                                                                                   \
-    if (mode == CA_FEW_MODE) {                                                                           \
-      hipLaunchKernelGGL((k_attn_cached_few<T, FMT, V, N, B>), grid, dim3(CA_THREADS), 0, st, a);        \
-      break;                                                                                             \
-    }                                                                                                    \
-    if (mode == CA_WAVE)                                                                                 \
-      hipLaunchKernelGGL((k_attn_cached<T, FMT, V, N, B, true>), grid, dim3(CA_THREADS), 0, st, a);      \
-    else                                                                                                 \
-      hipLaunchKernelGGL((k_attn_cached<T, FMT, V, N, B, false>), grid, dim3(CA_THREADS), 0, st, a);     \
-    if (a.cells > 0)                                                                                     \
-      hipLaunchKernelGGL((k_attn_cached_long<T, FMT, V, N, B>), long_grid, dim3(CA_THREADS), 0, st, a);  \
+static void launch_ca(const CaArgs& a, const CaPlan& p, bool big, dim3 grid, dim3 long_grid, hipStream_t st) {
+#define FAST_CAK(K, g) hipLaunchKernelGGL(K, g, dim3(CA_THREADS), 0, st, a)
+#define FAST_CA(V, N, B)                                                                       \
+  do {                                                                                         \
+    if (p.few) FAST_CAK((k_attn_cached_few<T, FMT, V, N, B>), grid);                           \
+    else if (p.owner == CA_BLOCK) FAST_CAK((k_attn_cached<T, FMT, V, N, B, CA_BLOCK>), grid);  \
+    else if (p.owner == CA_WAVE) FAST_CAK((k_attn_cached<T, FMT, V, N, B, CA_WAVE>), grid);    \
+    else FAST_CAK((k_attn_cached<T, FMT, V, N, B, CA_GROUP>), grid);                           \
+    if (a.cells > 0 && !p.few) FAST_CAK((k_attn_cached_long<T, FMT, V, N, B>), long_grid);     \
   } while (0)
-  if (ve == 8) FAST_CA(8, 0, true);
+  if (p.ve == 8) FAST_CA(8, 0, true);
   else if (big) FAST_CA(16, 0, true);
   else if (a.lph == 2) FAST_CA(16, 2, false);
   else if (a.lph == 4) FAST_CA(16, 4, false);
   else if (a.lph == 8) FAST_CA(16, 8, false);
   else FAST_CA(16, 0, true);
 #undef FAST_CA
-}
-
-// Cells of cap edges; none where no segment can be long.
-static int64_t ca_cells(int64_t E, int shift) {
-  return E > (int64_t(1) << shift) ? ((E - 1) >> shift) + 1 : 0;
-}
-static size_t ca_part_bytes(int64_t cells, int H, int dh) {
-  return align_up(size_t(2 * cells) * H * (dh + 2) * sizeof(float), 16);
+#undef FAST_CAK
 }
 
 }  // namespace fast
@@ -567,8 +601,8 @@ extern "C" size_t fast_edge_attention_cached_workspace(int64_t num_dst, int64_t 
   if (num_dst < 0 || num_edges < 0 || num_edges >= (int64_t(1) << 31) || H <= 0 || dh <= 0 || H > 64 ||
       dh > 256 || H * dh > 1024)
     return 0;
-  // never 0; partial results, then a mark per cell (the shortest pieces have the most)
-  const int64_t cells = ca_cells(num_edges, CA_SHIFT);
+  // never 0; partial results, then a mark per cell
+  const int64_t cells = ca_plan(num_dst, num_edges, H, dh).cells;
   return ca_part_bytes(cells, H, dh) + align_up(size_t(cells + CA_CELLS) * sizeof(int32_t), 16);
 }
 
@@ -622,37 +656,30 @@ extern "C" fast_status_t fast_edge_attention_fwd_cached(
   a.out = out;
   a.lse = lse;
   a.part = static_cast<float*>(ws);
-  // 16 codes a lane (fewer instructions per record) where every lane's codes lie in
-  // one group: a head's last piece may start 8 codes early, which crosses a
-  // group's border where 1 to 8 elements are left past one.
-  const int ve = dh > 8 && (dh % MX_GROUP == 0 || dh % MX_GROUP > 8) ? 16 : 8;
-  a.lph = pow2_at_least((dh + ve - 1) / ve);
-  int hpw = pow2_at_least(H);
-  if (hpw > 64 / a.lph) hpw = 64 / a.lph;
-  a.L = a.lph * hpw;
-  const bool big = a.rec.stride * cache_rows >= (int64_t(1) << 32);
-  const bool wave = ca_wave_each(N, E, a.L);
-  a.shift = ca_shift(E, wave);
-  a.cells = ca_cells(E, a.shift);
+  const CaPlan p = ca_plan(N, E, H, dh);
+  a.lph = p.lph;
+  a.L = p.L;
+  a.shift = p.shift;
+  a.cells = p.cells;
   a.rounds = (a.cells + CA_CELLS - 1) / CA_CELLS;
   a.mark = reinterpret_cast<int32_t*>(static_cast<char*>(ws) + ca_part_bytes(a.cells, H, dh));
-  const int64_t per = wave ? CA_WAVES : CA_THREADS / a.L;
+  const bool big = a.rec.stride * cache_rows >= (int64_t(1) << 32);
+  const int hpw = p.L / p.lph;
   const uint32_t heads = uint32_t((H + hpw - 1) / hpw);
-  const bool few = N < CA_FEW && a.cells > 0;
-  const CaMode mode = few ? CA_FEW_MODE : wave ? CA_WAVE : CA_GROUP;
-  const dim3 grid(uint32_t((few ? a.cells : 0) + (N + per - 1) / per), heads);
+  const int64_t per = p.few || p.owner == CA_BLOCK ? 1 : p.owner == CA_WAVE ? CA_WAVES : CA_THREADS / a.L;
+  const dim3 grid(uint32_t((p.few ? a.cells : 0) + (N + per - 1) / per), heads);
   const uint32_t cells = uint32_t(a.cells < CA_CELLS ? a.cells : CA_CELLS);
   if (!grid_fits(grid.x, CA_THREADS)) return fail(FAST_ERR_UNSUPPORTED, "%s: 2^32 threads or more", fn);
   const dim3 long_grid(cells, heads);
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (dtype == FAST_F32) {
-    if (format == FAST_MXFP8) launch_ca<float, FAST_MXFP8>(a, ve, big, mode, grid, long_grid, st);
-    else launch_ca<float, FAST_MXFP4>(a, ve, big, mode, grid, long_grid, st);
+    if (format == FAST_MXFP8) launch_ca<float, FAST_MXFP8>(a, p, big, grid, long_grid, st);
+    else launch_ca<float, FAST_MXFP4>(a, p, big, grid, long_grid, st);
   } else {
-    if (format == FAST_MXFP8) launch_ca<uint16_t, FAST_MXFP8>(a, ve, big, mode, grid, long_grid, st);
-    else launch_ca<uint16_t, FAST_MXFP4>(a, ve, big, mode, grid, long_grid, st);
+    if (format == FAST_MXFP8) launch_ca<uint16_t, FAST_MXFP8>(a, p, big, grid, long_grid, st);
+    else launch_ca<uint16_t, FAST_MXFP4>(a, p, big, grid, long_grid, st);
   }
-  if (few) {
+  if (p.few) {
     const dim3 join_grid = dim3(uint32_t(N), uint32_t(H));
     if (dtype == FAST_F32)
       hipLaunchKernelGGL((k_attn_cached_few_join<float>), join_grid, dim3(CJ_THREADS), 0, st, a);
