@@ -2,7 +2,7 @@
 // (record layout and conversions in mx.h).
 //
 // Bound by HBM: a write reads a row and writes its record, a read the other way
-// round, at random slots.  A workgroup looks up the slots of its rows once, in LDS;
+// round, at random slots (264,000 rows of 4 x 50 fp32 in 8 bits: 54 us = 5.1 TB/s and 45 = 6.2).  A workgroup looks up the slots of its rows once, in LDS;
 // then a thread moves CR_UNROLL pieces of 16 bytes of a row (4 fp32 or 8 bf16
 // elements), all of whose loads are in flight together.  The 8 or 4 neighbouring lanes of
 // a group of 32 find its largest magnitude with DPP exchanges, so a row is read once.

