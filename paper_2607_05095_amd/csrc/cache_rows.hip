@@ -31,27 +31,37 @@ struct CacheArgs {
   const uint8_t* cache_in;
   uint8_t* cache;
   int32_t* owner;                    // write: the last i of each slot, or NULL
+  int32_t* slots;                    // write with owners: the slot of each i, looked up once
   bool search;                       // write of at most CR_SMALL rows: repeats are looked for here
 };
 
-// Two passes over the ids find the last i of every slot: the first clears the
-// slots that the ids name, the second takes the maximum.
+// Two passes find the last i of every slot: the first looks the slots up and clears their
+// owners, the second takes the maximum.
 __global__ void __launch_bounds__(CR_THREADS) k_cache_claim(CacheArgs a, int pass) {
   const int64_t i = int64_t(blockIdx.x) * CR_THREADS + threadIdx.x;
   if (i >= a.n) return;
-  const int64_t s = mx_slot(a.ids[i], a.id_bound, a.slot_map, a.cache_rows);
-  if (s < 0) return;
-  if (pass == 0) a.owner[s] = -1;
-  else atomicMax(a.owner + s, int32_t(i));
+  if (pass == 0) {
+    const int64_t s = mx_slot(a.ids[i], a.id_bound, a.slot_map, a.cache_rows);
+    a.slots[i] = int32_t(s);
+    if (s >= 0) a.owner[s] = -1;
+  } else {
+    const int32_t s = a.slots[i];
+    if (s >= 0) atomicMax(a.owner + s, int32_t(i));
+  }
 }
 
 // Slots of the workgroup's rows (-1: none), in LDS.
 __device__ __forceinline__ void cr_slots(const CacheArgs& a, int64_t row0, int rows, int32_t* s_slot) {
   for (int r = threadIdx.x; r < rows; r += CR_THREADS) {
     const int64_t i = row0 + r;
-    int64_t s = mx_slot(a.ids[i], a.id_bound, a.slot_map, a.cache_rows);
-    if (a.owner && s >= 0 && a.owner[s] != int32_t(i)) s = -1;
-    s_slot[r] = int32_t(s);
+    int32_t s;
+    if (a.owner) {
+      s = a.slots[i];
+      if (s >= 0 && a.owner[s] != int32_t(i)) s = -1;
+    } else {
+      s = int32_t(mx_slot(a.ids[i], a.id_bound, a.slot_map, a.cache_rows));
+    }
+    s_slot[r] = s;
   }
   __syncthreads();
 }
@@ -221,7 +231,9 @@ extern "C" size_t fast_cache_row_bytes(int parts, int width, fast_cache_format_t
 
 extern "C" size_t fast_cache_write_workspace(int64_t n, int64_t cache_rows) {
   if (n < 0 || cache_rows < 0 || n >= (int64_t(1) << 31) || cache_rows >= (int64_t(1) << 31)) return 0;
-  return align_up(size_t(cache_rows > 0 ? cache_rows : 1) * sizeof(int32_t), 16);
+  // owners, then slots
+  return align_up(size_t(cache_rows > 0 ? cache_rows : 1) * sizeof(int32_t), 16) +
+         align_up(size_t(n) * sizeof(int32_t), 16);
 }
 
 extern "C" fast_status_t fast_cache_write(const int64_t* ids, int64_t n, int64_t id_bound,
@@ -250,6 +262,7 @@ extern "C" fast_status_t fast_cache_write(const int64_t* ids, int64_t n, int64_t
   a.search = !distinct && n <= CR_SMALL;
   if (!distinct && !a.search) {
     a.owner = static_cast<int32_t*>(ws);
+    a.slots = a.owner + align_up(size_t(cache_rows) * sizeof(int32_t), 16) / sizeof(int32_t);
     const uint32_t g = uint32_t((n + CR_THREADS - 1) / CR_THREADS);
     hipLaunchKernelGGL(k_cache_claim, dim3(g), dim3(CR_THREADS), 0, st, a, 0);
     hipLaunchKernelGGL(k_cache_claim, dim3(g), dim3(CR_THREADS), 0, st, a, 1);
