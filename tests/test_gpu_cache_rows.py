@@ -267,6 +267,31 @@ def test_cached_attention_long_histories(E, N):
     b.check(*b.run())
 
 
+def test_cached_attention_queries_past_two_to_the_31_elements():
+    """Segments of no edges but at the first, the last and those around element 2^31 of Q."""
+    H, dh, N = 4, 32, 17_000_000
+    mid = (1 << 31) // (H * dh)
+    assert N > mid + 1
+    print(f"[cache] attention N={N}", flush=True)
+    at = np.array([0, mid - 1, mid, mid + 1, N - 1])
+    b = Block([3, 1, 7, 2, 300], H, dh, 8, "bf16", rows=50, bound=60)
+    off = torch.zeros(N + 1, dtype=torch.int32, device="cuda")
+    for v, c in zip(at, np.diff(b.off)):
+        off[v + 1:] += int(c)
+    Q = torch.zeros(N, H, dh, dtype=torch.bfloat16, device="cuda")
+    Q[to_dev(at)] = b.Q
+    out = torch.full((N, H, dh), 7.0, dtype=torch.bfloat16, device="cuda")
+    lse = torch.empty(N, H, device="cuda")
+    wsb = fast.fast_edge_attention_cached_workspace(N, b.E, H, dh)
+    ws = torch.empty(wsb, dtype=torch.uint8, device="cuda")
+    fast.fast_edge_attention_fwd_cached(fast.tcsr(off, b.E), H, dh, fast.BF16, Q, to_dev(b.ids), b.bound,
+                                        to_dev(b.smap), fast.MXFP8, b.cache, b.rows, b.scale, b.slope, out, lse, ws, wsb)
+    pad = torch.full((1, H, dh), 7.0, dtype=torch.bfloat16, device="cuda")
+    b.check(torch.cat([out[to_dev(at)], pad]), torch.cat([lse[to_dev(at)], pad[:, :, 0].float()]))
+    out[to_dev(at)] = 0
+    assert not out.any()
+
+
 def test_cached_attention_no_edge_is_cached():
     b = Block([3, 100, 0, 700], 2, 50, 8, "f32")
     b.smap[:] = -1

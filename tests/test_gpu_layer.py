@@ -216,6 +216,45 @@ def test_rotary_axis_out_of_range_null_axis_and_infinite_position():
     assert torch.isnan(z[2, 0, 0]) and not torch.isnan(z[[0, 1, 3]]).any() and torch.equal(z[3], x[3])
 
 
+# ------------------------------------------------------------------ arrays past 2^31 elements
+def test_norm_and_rotary_past_two_to_the_31_elements():
+    """The first rows, the last ones, and those around element 2^31."""
+    n, H, dh = 34_000_000, 2, 32
+    D = H * dh
+    assert n * D > 1 << 31
+    print(f"[layer] {n} x {D} bf16", flush=True)
+    torch.manual_seed(1)
+    x = torch.randn(n, D, dtype=torch.bfloat16, device="cuda")
+    mid = (1 << 31) // D
+    rows = torch.tensor([0, 1, mid - 1, mid, mid + 1, n - 2, n - 1], device="cuda")
+    x64 = host(x[rows])
+    y = torch.empty_like(x)
+    mean, rstd = torch.empty(2, n, device="cuda").unbind(0)
+    fast.fast_layer_norm_fwd(n, D, fast.BF16, x, None, None, None, 1e-5, y, None, mean, rstd)
+    ref, mu, rs = p64.layer_norm(x64, 1.0, 0.0, 1e-5)
+    within(y[rows], ref, norm_bounds(x64, mu, rs, 1.0, 0.0, ref, "bf16"), "y")
+    dx = torch.empty_like(x)
+    dg, db = torch.empty(2, D, device="cuda").unbind(0)
+    wsb = fast.fast_layer_norm_bwd_workspace(n, D)
+    ws = torch.empty(wsb, dtype=torch.uint8, device="cuda")
+    fast.fast_layer_norm_bwd(n, D, fast.BF16, x, None, mean, rstd, y, None, dx, dg, db, ws, wsb)
+    # with dy = y, dx = r (y - xhat) up to terms of eps: 2^-8 |y|, |y| < 6, r < 1.5
+    assert float(dx[rows].float().abs().max()) <= 2.0 ** -8 * 10
+    total = torch.zeros(D, dtype=torch.float64, device="cuda")
+    for a in range(0, n, 1 << 22):
+        total += y[a:a + (1 << 22)].double().sum(0)
+    # 33 U of each of 32 rows' magnitudes, at most 6 on n rows
+    assert (db.double() - total).abs().max() <= 33 * U * 6 * n
+    del dx
+    pos = torch.full((n, 1), 3.0, device="cuda")
+    om = torch.ones(dh // 2, device="cuda")
+    fast.fast_rotary_fwd(n, H, dh, fast.BF16, x, D, pos, 1, None, om, dh // 2, 0, y, D)
+    ref = p64.rotary(x64.reshape(-1, H, dh), np.full((len(rows), 1), 3.0), np.zeros(dh // 2, int), np.ones(dh // 2),
+                     dh // 2, False)
+    big = np.abs(x64).max()
+    within(y[rows].view(-1, H, dh), ref, 2 * big * (2e-7 + 3 * U) + HALF["bf16"] * np.abs(ref), "turned")
+
+
 # ------------------------------------------------------------------ streams, graphs, several at once
 def test_norm_and_rotary_on_another_stream_and_in_a_graph():
     n, D, H, dh = 3000, 100, 2, 50
