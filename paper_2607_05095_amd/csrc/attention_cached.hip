@@ -246,10 +246,14 @@ __device__ __forceinline__ void ca_store(const CaArgs& a, int64_t v, CaLane<VE>&
 }
 
 // Edges [e0, e1) of segment v by a workgroup, into partial result `slot` (-1: they are the segment).
+// The waves' groups, at most CA_JOIN each, meet in LDS: a thread per element adds its
+// weighted accumulators (joining a wave's 8 groups by lane exchanges and the waves in
+// one of them took 4400 cycles).
+constexpr int CA_JOIN = 1, CA_PAD = 65;      // odd: a column of LDS in as many banks
 template <typename T, int FMT, int VE, int LPH, bool BIG>
 __device__ __forceinline__ void ca_piece(const CaArgs& a, int64_t v, int64_t e0, int64_t e1, int64_t slot,
-                                         float (*s_acc)[VE + 2][64]) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+                                         float (*s_acc)[VE + 2][CA_PAD]) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, L = a.L;
   CaLane<VE> c;
   ca_init<T, FMT, VE, LPH>(a, v, c);
   const int64_t each = (e1 - e0 + CA_WAVES - 1) / CA_WAVES;
@@ -260,30 +264,31 @@ __device__ __forceinline__ void ca_piece(const CaArgs& a, int64_t v, int64_t e0,
 #pragma unroll
   for (int j = 0; j < VE; ++j) s_acc[wave][j][lane] = c.acc[j];
   __syncthreads();
-  if (wave == 0 && lane < a.L && c.mine) {
-    float mx = -INFINITY, Z = 0.f;
-    for (int w = 0; w < CA_WAVES; ++w) mx = fmaxf(mx, s_acc[w][VE][lane]);
-#pragma unroll
-    for (int j = 0; j < VE; ++j) c.acc[j] = 0.f;
+  const int lph = ca_lph<LPH>(a), last = (a.dh + MX_PIECE - 1) / MX_PIECE * MX_PIECE - VE;
+  for (int t = threadIdx.x; t < VE * L; t += CA_THREADS) {
+    const int j = t % VE, p = t / VE;          // element j of lane p
+    const int h = blockIdx.y * (L / lph) + p / lph, own = (p & (lph - 1)) * VE;
+    const int e = (own < last ? own : last) + j;
+    if (h >= a.H || e < own || e >= a.dh) continue;
+    float mx = -INFINITY, Z = 0.f, acc = 0.f;
+    for (int w = 0; w < CA_WAVES; ++w) mx = fmaxf(mx, s_acc[w][VE][p]);
     for (int w = 0; w < CA_WAVES; ++w) {
-      const float k = ca_pow2(s_acc[w][VE][lane], mx);
-      Z = fmaf(s_acc[w][VE + 1][lane], k, Z);
-#pragma unroll
-      for (int j = 0; j < VE; ++j) c.acc[j] = fmaf(s_acc[w][j][lane], k, c.acc[j]);
+      const float k = ca_pow2(s_acc[w][VE][p], mx);
+      Z = fmaf(s_acc[w][VE + 1][p], k, Z);
+      acc = fmaf(s_acc[w][j][p], k, acc);
     }
     if (slot < 0) {
-      c.mx = mx;
-      c.Z = Z;
-      ca_store<T, VE>(a, v, c);
+      const bool some = !(Z == 0.f);           // also of a NaN
+      const float o = some ? acc / Z : 0.f;
+      VecIO<T, 1>::store(static_cast<T*>(a.out) + (v * a.H + h) * a.dh + e, &o);
+      if (a.lse && e == 0) a.lse[v * a.H + h] = some ? (mx + log2f(Z)) * LN2 : -INFINITY;
     } else {
-      float* p = a.part + (slot * a.H + c.h) * (a.dh + 2);
-      if (c.l == 0) {
-        p[0] = mx;
-        p[1] = Z;
+      float* q = a.part + (slot * a.H + h) * (a.dh + 2);
+      if (e == 0) {
+        q[0] = mx;
+        q[1] = Z;
       }
-#pragma unroll
-      for (int j = 0; j < VE; ++j)
-        if (c.first + j >= c.own && c.first + j < a.dh) p[2 + c.first + j] = c.acc[j];
+      q[2 + e] = acc;
     }
   }
   __syncthreads();                     // before the next piece of this workgroup
@@ -312,7 +317,7 @@ __global__ void __launch_bounds__(CA_THREADS) k_attn_cached(CaArgs a) {
   CaLane<VE> c;
   int64_t s, t;
   if constexpr (OWNER == CA_BLOCK) {
-    __shared__ float s_acc[CA_WAVES][VE + 2][64];
+    __shared__ float s_acc[CA_WAVES][VE + 2][CA_PAD];
     const int64_t v = blockIdx.x;
     ca_segment(a, v, s, t);
     if (a.cells > 0) ca_mark(a, v, s, t, threadIdx.x, CA_THREADS);
@@ -443,7 +448,7 @@ __device__ __forceinline__ uint64_t ca_marks(const CaArgs& a, int64_t b, int64_t
 // spread over the workgroups).
 template <typename T, int FMT, int VE, int LPH, bool BIG>
 __global__ void __launch_bounds__(CA_THREADS) k_attn_cached_long(CaArgs a) {
-  __shared__ float s_acc[CA_WAVES][VE + 2][64];
+  __shared__ float s_acc[CA_WAVES][VE + 2][CA_PAD];
   const int64_t cap = int64_t(1) << a.shift;
   for (int64_t base = 0; base < a.rounds; base += 64) {
     int32_t here, next;
@@ -491,7 +496,7 @@ __global__ void __launch_bounds__(CJ_THREADS) k_attn_cached_join(CaArgs a) {
 constexpr int CA_FEW = 64;
 template <typename T, int FMT, int VE, int LPH, bool BIG>
 __global__ void __launch_bounds__(CA_THREADS) k_attn_cached_few(CaArgs a) {
-  __shared__ float s_acc[CA_WAVES][VE + 2][64];
+  __shared__ float s_acc[CA_WAVES][VE + 2][CA_PAD];
   const int lane = threadIdx.x & 63;
   const int64_t cap = int64_t(1) << a.shift, m = blockIdx.x;
   if (m < a.cells) {
