@@ -1,6 +1,8 @@
 """GPU parity of layer norm and rotary positions against their plain 64-bit
 definitions, through the C ABI.  Tolerances are rounding bounds written beside
 each comparison (U = 2^-24, half a step of fp32)."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -214,6 +216,26 @@ def test_rotary_axis_out_of_range_null_axis_and_infinite_position():
     fast.fast_rotary_fwd(4, 1, 8, 0, x, 8, pos, 2, to_dev(np.zeros(4, np.int32)), om, 4, 0, w, 8)
     assert torch.equal(z.nan_to_num(9), w.nan_to_num(9))
     assert torch.isnan(z[2, 0, 0]) and not torch.isnan(z[[0, 1, 3]]).any() and torch.equal(z[3], x[3])
+
+
+@pytest.mark.parametrize("inter", [False, True])
+def test_rotary_angles_of_any_size(inter):
+    """Sine and cosine within 2e-7 at Unix seconds, nanoseconds and the largest fp32 position."""
+    r = np.random.default_rng(5)
+    mags = np.repeat([1e8, 1.6e9, 1.6e12, 2e13, 1e15, 1.6e18, 1e25, 3e38], 40)
+    pos = (r.uniform(0.5, 1, len(mags)) * mags * r.choice([-1, 1], len(mags))).astype(np.float32)
+    om = np.array([1.0, 0.37, 1e-3, 3.0], np.float32)
+    n, x = len(pos), torch.zeros(len(pos), 1, 8, device="cuda")
+    a = np.arange(4) * (2 if inter else 1)
+    b = a + (1 if inter else 4)
+    x[..., a] = 1.0                              # (1, 0) turns into (cos, sin)
+    y = torch.empty_like(x)
+    fast.fast_rotary_fwd(n, 1, 8, 0, x, 8, to_dev(pos[:, None]), 1, None, to_dev(om), 4, int(inter), y, 8)
+    th = pos.astype(np.float64)[:, None] * om.astype(np.float64)      # exact: 48 bits
+    y = y.cpu().numpy().astype(np.float64)[:, 0]
+    for got, f in ((y[:, a], math.cos), (y[:, b], math.sin)):
+        ref = np.vectorize(f)(th)
+        assert np.abs(got - ref).max() <= 2e-7 + U       # and the product with 1
 
 
 # ------------------------------------------------------------------ arrays past 2^31 elements
