@@ -433,6 +433,7 @@ extern "C" fast_status_t fast_layer_norm_fwd(int64_t n, int D, fast_dtype_t dtyp
   if (s != FAST_OK) return s;
   if (!(eps >= 0.f)) return fail(FAST_ERR_INVALID_ARG, "%s: eps is negative or not a number", fn);
   if (sum && !res) return fail(FAST_ERR_INVALID_ARG, "%s: sum without res", fn);
+  if (sum && sum == y) return fail(FAST_ERR_INVALID_ARG, "%s: y and sum are one array", fn);
   if (n == 0) return ok();
   if (!x || !y) return fail(FAST_ERR_INVALID_ARG, "%s: NULL x/y", fn);
   const size_t es = elem_size(dtype);

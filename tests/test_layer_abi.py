@@ -36,6 +36,10 @@ def test_layer_norm_fwd_refusals(kw, status):
     assert (fast.fast_last_error() == "") == (status == OK)
 
 
+def test_layer_norm_sum_and_y_in_one_array_refused():
+    assert call("fast_layer_norm_fwd", NORM, dict(res=FAKE + 4096, sum=FAKE, y=FAKE)) == INVALID
+
+
 NORM_B = dict(n=5, D=10, dt=0, h=FAKE, gamma=FAKE, mean=FAKE, rstd=FAKE, dy=FAKE, dsum=None, dx=FAKE,
               dgamma=FAKE, dbeta=FAKE, ws=FAKE, wsb=1 << 20, st=None)
 
