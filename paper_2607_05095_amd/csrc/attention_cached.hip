@@ -37,7 +37,7 @@ namespace fast {
 constexpr int CA_THREADS = 256, CA_WAVES = CA_THREADS / 64;
 constexpr int CA_ROWS = 4;           // records in flight per lane
 constexpr int CA_AHEAD = 2;          // places that a lane looks up at once
-constexpr int CA_SHIFT = 8, CA_SHIFT_MAX = 11;   // cap = 256 .. 2048 (4096: see ca_plan)
+constexpr int CA_SHIFT = 8, CA_SHIFT_MAX = 11;   // cap = 256 .. 2048 (64, 128, 4096: see ca_plan)
 constexpr int CA_BLOCKS = 2048;      // segments that get a workgroup each, at most: 8 per CU
 constexpr int CA_CELLS = 1024;       // workgroups of the second launch, at most: 4 per CU (a power of two)
 
@@ -564,13 +564,19 @@ static CaPlan ca_plan(int64_t N, int64_t E, int H, int dh) {
   //     takes two launches): four segments of 1000 edges in all 11 / 8 us,
   //   - where many segments are about that long, so that most are not cut (256 / 512, 5000
   //     segments of 200 on average 163 / 86; 256 / 2048, 100 of 1000: 35 / 29).
-  // Not where a few lanes own a segment: they would be long over one of 1024.
+  // Not where a few lanes own a segment: they would be long over one of 1024, and over one of
+  // 256 (45 us) in a block that takes less; so shorter pieces there, 64 / 128 / 256: 6600
+  // segments of 2200 edges in all, three hubs, 14.1 / 17.2 / 53.0 us; 20,000 of 20,000 with
+  // hubs 17.0 / 17.3 / 17.6; 50,000 of 100,000 with hubs 35.3 / 31.5 / 31.9; 100,000 of
+  // 1,000,000 with hubs 130.6 / 111.6 / 100.6.
   p.shift = CA_SHIFT;
   if (p.owner != CA_GROUP) {
     while (p.shift < CA_SHIFT_MAX && (E >> (p.shift + 1)) >= 480) ++p.shift;
     if (E <= 1024 && p.shift < 10) p.shift = 10;
     if (N >= 32 && mean <= 2048)
       while ((int64_t(1) << p.shift) < 2 * mean) ++p.shift;
+  } else if (E < 131072) {
+    p.shift = E < 8192 ? 6 : 7;
   }
   // cells of cap edges; none where no segment can be long
   p.cells = E > (int64_t(1) << p.shift) ? ((E - 1) >> p.shift) + 1 : 0;

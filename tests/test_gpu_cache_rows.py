@@ -256,6 +256,20 @@ def test_cached_attention_many_segments(H, dh, fmt):
     b.check(*b.run())
 
 
+@pytest.mark.parametrize("most", [1, 20, 40])
+def test_cached_attention_long_among_very_many_short(most):
+    """Lengths about every cut of a block whose segments belong to a few lanes each."""
+    r = np.random.default_rng(most)
+    counts = r.integers(0, most, 6000)
+    long = [63, 64, 65, 66, 127, 128, 129, 130, 255, 256, 257, 600]
+    counts[100:100 + len(long)] = long
+    counts[r.choice(np.arange(1000, 6000), len(long), replace=False)] = long
+    counts[5999] = 65
+    print(f"[cache] attention long among short N=6000 E={counts.sum()}", flush=True)
+    b = Block(counts, 2, 50, 8, "f32", seed=most)
+    b.check(*b.run())
+
+
 @pytest.mark.parametrize("E,N", [(400000, 3), (600000, 20000)])
 def test_cached_attention_long_histories(E, N):
     """Piece lengths above the shortest, a hub across very many pieces."""
