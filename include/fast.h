@@ -556,7 +556,7 @@ fast_status_t fast_layer_norm_fwd(int64_t n, int D, fast_dtype_t dtype, const vo
  * added in fp32 over at most 32 rows and in fp64 beyond (a workgroup's sum
  * rounded to fp32 in between), in a fixed order: repeated calls give the same bits.  dx: [n, D] of dtype; it may be dy or dsum.
  * Workspace, needed for dgamma or dbeta only: fast_layer_norm_bwd_workspace(n, D)
- * bytes, 8-byte aligned. */
+ * bytes, 8-byte aligned; one for the largest n serves smaller ones. */
 size_t fast_layer_norm_bwd_workspace(int64_t n, int D);
 fast_status_t fast_layer_norm_bwd(int64_t n, int D, fast_dtype_t dtype, const void* h,
                                   const float* gamma, const float* mean, const float* rstd,
@@ -657,7 +657,7 @@ fast_status_t fast_cache_gather(const int64_t* ids, int64_t n, int64_t id_bound,
  * a second launch joins in their order (repeated calls give the same bits).
  * Limits: H <= 64, dh <= 256, H*dh <= 1024.
  * Workspace: fast_edge_attention_cached_workspace(N, E, H, dh) bytes (never 0 for valid
- * sizes), 16-byte aligned.
+ * sizes), 16-byte aligned; one for the largest N and E serves smaller blocks.
  * ------------------------------------------------------------------------ */
 size_t fast_edge_attention_cached_workspace(int64_t num_dst, int64_t num_edges, int H, int dh);
 fast_status_t fast_edge_attention_fwd_cached(const fast_tcsr_t* g, int H, int dh,

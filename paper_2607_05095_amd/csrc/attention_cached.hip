@@ -28,6 +28,8 @@
 // four histories of 100,003 edges.  Looking for the long segments with a search of the
 // offsets, in the first launch, cost 30 us of 190 in registers and waves for a
 // block of 264,000 short segments.)
+#include <algorithm>
+
 #include "attention.h"
 #include "mx.h"
 #include "rows.h"
@@ -40,6 +42,9 @@ constexpr int CA_AHEAD = 2;          // places that a lane looks up at once
 constexpr int CA_SHIFT = 8, CA_SHIFT_MAX = 11;   // cap = 256 .. 2048 (64, 128, 4096: see ca_plan)
 constexpr int CA_BLOCKS = 2048;      // segments that get a workgroup each, at most: 8 per CU
 constexpr int CA_CELLS = 1024;       // workgroups of the second launch, at most: 4 per CU (a power of two)
+
+constexpr int64_t CA_LANES_N = 4096; // segments above which a few lanes may own one
+constexpr int64_t CA_SHORT_E = 8191, CA_MEDIUM_E = 131071;   // edges up to which cap is 64 and 128 there
 
 struct CaArgs {
   int64_t N, E;
@@ -555,7 +560,7 @@ static CaPlan ca_plan(int64_t N, int64_t E, int H, int dh) {
   // 10 16 / 16 / 33, 3000 of 100 74 / 33 / 34, 400 of 250 162 / 30 / 19, 600 of 10 12 / 9 / 11.
   const int64_t mean = N > 0 ? E / N : 0;
   if (mean >= 64 && N <= CA_BLOCKS) p.owner = CA_BLOCK;
-  else if (N <= 4096 || mean >= 2 * CA_ROWS * (64 / p.L)) p.owner = CA_WAVE;
+  else if (N <= CA_LANES_N || mean >= 2 * CA_ROWS * (64 / p.L)) p.owner = CA_WAVE;
   else p.owner = CA_GROUP;
   // Pieces of 256 edges: a workgroup's 4 waves take 64 each.  Longer ones
   //   - where there are about 500 all the same, as they join faster (256 / 2048 edges, one
@@ -575,13 +580,28 @@ static CaPlan ca_plan(int64_t N, int64_t E, int H, int dh) {
     if (E <= 1024 && p.shift < 10) p.shift = 10;
     if (N >= 32 && mean <= 2048)
       while ((int64_t(1) << p.shift) < 2 * mean) ++p.shift;
-  } else if (E < 131072) {
-    p.shift = E < 8192 ? 6 : 7;
+  } else if (E <= CA_MEDIUM_E) {
+    p.shift = E <= CA_SHORT_E ? 6 : 7;
   }
   // cells of cap edges; none where no segment can be long
   p.cells = E > (int64_t(1) << p.shift) ? ((E - 1) >> p.shift) + 1 : 0;
   p.few = N < CA_FEW && p.cells > 0;
   return p;
+}
+// The most cells that ca_plan takes for up to N segments and up to E edges: the workspace grows
+// with both, so that one for the largest block serves all.
+static int64_t ca_cells_most(int64_t N, int64_t E, int H, int dh) {
+  const CaPlan p = ca_plan(N, E, H, dh);
+  auto cells = [](int64_t e, int shift) { return (e >> shift) + 1; };
+  // pieces of 256 and more are taken where there would be 2 * 480 of the next shorter ones
+  int64_t most = std::max({p.cells, cells(std::min<int64_t>(E, 480 << (CA_SHIFT + 1)), CA_SHIFT),
+                           cells(E, CA_SHIFT_MAX)});
+  if (N > CA_LANES_N) {                // a few lanes may own a segment, at this many edges or fewer
+    const int64_t e = std::min(E, 2 * CA_ROWS * (64 / p.L) * N);
+    most = std::max({most, cells(std::min(e, CA_SHORT_E), 6), cells(std::min(e, CA_MEDIUM_E), 7),
+                     cells(e, CA_SHIFT)});
+  }
+  return most;
 }
 static size_t ca_part_bytes(int64_t cells, int H, int dh) {
   return align_up(size_t(2 * cells) * H * (dh + 2) * sizeof(float), 16);
@@ -614,11 +634,12 @@ using namespace fast;
 
 extern "C" size_t fast_edge_attention_cached_workspace(int64_t num_dst, int64_t num_edges, int H,
                                                        int dh) {
-  if (num_dst < 0 || num_edges < 0 || num_edges >= (int64_t(1) << 31) || H <= 0 || dh <= 0 || H > 64 ||
+  if (num_dst < 0 || num_edges < 0 || num_dst >= (int64_t(1) << 31) ||
+      num_edges >= (int64_t(1) << 31) || H <= 0 || dh <= 0 || H > 64 ||
       dh > 256 || H * dh > 1024)
     return 0;
   // never 0; partial results, then a mark per cell
-  const int64_t cells = ca_plan(num_dst, num_edges, H, dh).cells;
+  const int64_t cells = ca_cells_most(num_dst, num_edges, H, dh);
   return ca_part_bytes(cells, H, dh) + align_up(size_t(cells + CA_CELLS) * sizeof(int32_t), 16);
 }
 

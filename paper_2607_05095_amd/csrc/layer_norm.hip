@@ -17,6 +17,8 @@
 // LN_ROWS of them in fp32; a workgroup joins its groups in fp64 in LDS and
 // writes one partial row, and a second launch adds the partial rows in fp64 in
 // their order.  No atomics: repeated calls give the same bits.
+#include <algorithm>
+
 #include "rows.h"
 
 namespace fast {
@@ -455,9 +457,15 @@ extern "C" fast_status_t fast_layer_norm_fwd(int64_t n, int D, fast_dtype_t dtyp
 
 extern "C" size_t fast_layer_norm_bwd_workspace(int64_t n, int D) {
   if (n < 0 || n >= (int64_t(1) << 31) || D <= 0 || D > LN_MAX_D) return 0;
-  const LnPlan a = ln_plan(n, D, 4), b = ln_plan(n, D, 8);
-  const int64_t nb = a.nb > b.nb ? a.nb : b.nb;
-  return size_t(nb > 0 ? nb : 1) * 2 * D * sizeof(float);
+  // for either type, the most workgroups of up to n rows: it grows with n, so that one for
+  // the largest call serves all
+  int64_t nb = 1;
+  for (int ve = 4; ve <= 8; ve += 4) {
+    const LnPlan L = ln_plan(n, D, ve);
+    const int64_t units = (n + L.threads / L.G - 1) / (L.threads / L.G);
+    nb = std::max({nb, L.nb, std::min(units, LN_BLOCKS)});
+  }
+  return size_t(nb) * 2 * D * sizeof(float);
 }
 
 extern "C" fast_status_t fast_layer_norm_bwd(int64_t n, int D, fast_dtype_t dtype, const void* h,

@@ -230,3 +230,24 @@ def test_plain_formats(fmt):
         np.abs(x) * 0.25, top / 3 * 0.25)
     assert (np.abs(v - x) <= half).all()
     np.testing.assert_array_equal(p64.unpack(p64.pack(c, s, fmt), 2, 70, fmt), v)
+
+
+def test_a_workspace_for_the_largest_sizes_serves_all_smaller_ones():
+    r = np.random.default_rng(0)
+    size = lambda top: int(10 ** r.uniform(0, np.log10(top)))
+    for _ in range(4000):
+        D, n = size(8192), size(1e8)
+        n2 = min(n, max(0, n - size(n)) if r.random() < 0.5 else size(n))
+        assert fast.fast_layer_norm_bwd_workspace(n2, D) <= fast.fast_layer_norm_bwd_workspace(n, D), (n2, n, D)
+        H, dh = [(1, 1), (2, 50), (4, 32), (8, 128), (64, 16)][r.integers(5)]
+        N, E = size(1e7), size(1e8)
+        N2, E2 = (min(k, max(0, k - size(k)) if r.random() < 0.5 else size(k)) for k in (N, E))
+        big, small = (fast.fast_edge_attention_cached_workspace(a, b, H, dh) for a, b in ((N, E), (N2, E2)))
+        assert small <= big, (N2, E2, N, E, H, dh)
+    # and at the borders of the ways a call is carried out
+    for H, dh in ((2, 50), (4, 32), (64, 16)):
+        for N in (1, 31, 32, 64, 2048, 4096, 4097, 100000):
+            E = np.unique([b + d for b in (64, 128, 256, 1024, 4096, 8192, 65536, 131072, 245760, 491520, 983040,
+                                           64 * N, 128 * N, 2048 * N) for d in (-1, 0, 1)])
+            ws = [fast.fast_edge_attention_cached_workspace(N, int(e), H, dh) for e in E]
+            assert ws == sorted(ws), (H, dh, N)
