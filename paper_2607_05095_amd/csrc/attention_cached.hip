@@ -39,7 +39,7 @@ namespace fast {
 constexpr int CA_THREADS = 256, CA_WAVES = CA_THREADS / 64;
 constexpr int CA_ROWS = 4;           // records in flight per lane
 constexpr int CA_AHEAD = 2;          // places that a lane looks up at once
-constexpr int CA_SHIFT = 8, CA_SHIFT_MAX = 11;   // cap = 256 .. 2048 (64, 128, 4096: see ca_plan)
+constexpr int CA_SHIFT = 6, CA_SHIFT_MAX = 11;   // cap = 64 .. 2048 (4096: see ca_plan)
 constexpr int CA_BLOCKS = 2048;      // segments that get a workgroup each, at most: 8 per CU
 constexpr int CA_CELLS = 1024;       // workgroups of the second launch, at most: 4 per CU (a power of two)
 
@@ -536,6 +536,11 @@ static int pow2_at_least(int x) {
   return p;
 }
 
+// Pieces are taken twice as long while at least this many of them are left: more where a wave
+// has only one or two records of a kind in flight, fewer of the shortest.
+constexpr int64_t CA_PIECES = 640;
+static int64_t ca_pieces(int groups, int shift) { return groups <= 2 ? CA_PIECES : shift < 8 ? 320 : 480; }
+
 // How a call is carried out.
 struct CaPlan {
   int ve, lph, L;
@@ -562,26 +567,37 @@ static CaPlan ca_plan(int64_t N, int64_t E, int H, int dh) {
   if (mean >= 64 && N <= CA_BLOCKS) p.owner = CA_BLOCK;
   else if (N <= CA_LANES_N || mean >= 2 * CA_ROWS * (64 / p.L)) p.owner = CA_WAVE;
   else p.owner = CA_GROUP;
-  // Pieces of 256 edges: a workgroup's 4 waves take 64 each.  Longer ones
-  //   - where there are about 500 all the same, as they join faster (256 / 2048 edges, one
-  //     segment of 1,000,000 edges 4 x 32 bf16: 121 / 79 us; four of 100,003 in all: 22 / 50),
-  //   - where a whole block is no more than a workgroup gets through meanwhile (cutting
-  //     takes two launches): four segments of 1000 edges in all 11 / 8 us,
-  //   - where many segments are about that long, so that most are not cut (256 / 512, 5000
-  //     segments of 200 on average 163 / 86; 256 / 2048, 100 of 1000: 35 / 29).
-  // Not where a few lanes own a segment: they would be long over one of 1024, and over one of
-  // 256 (45 us) in a block that takes less; so shorter pieces there, 64 / 128 / 256: 6600
-  // segments of 2200 edges in all, three hubs, 14.1 / 17.2 / 53.0 us; 20,000 of 20,000 with
-  // hubs 17.0 / 17.3 / 17.6; 50,000 of 100,000 with hubs 35.3 / 31.5 / 31.9; 100,000 of
-  // 1,000,000 with hubs 130.6 / 111.6 / 100.6.
-  p.shift = CA_SHIFT;
-  if (p.owner != CA_GROUP) {
-    while (p.shift < CA_SHIFT_MAX && (E >> (p.shift + 1)) >= 480) ++p.shift;
-    if (E <= 1024 && p.shift < 10) p.shift = 10;
-    if (N >= 32 && mean <= 2048)
-      while ((int64_t(1) << p.shift) < 2 * mean) ++p.shift;
-  } else if (E <= CA_MEDIUM_E) {
-    p.shift = E <= CA_SHORT_E ? 6 : 7;
+  // Where a wave or a workgroup owns a segment, a piece of cap edges takes cap / (16 * 64 / L)
+  // rounds, each about 1 us of dependent loads, so pieces are short, 64 edges, and
+  // longer only as their number grows past what the chip runs at once: 64 / 256 / 1024
+  // edges, us, one segment of 1000, 8 x 128 14 / 28 / 70, 4 x 32 9.9 / 11.3 / 13.8; 60 of
+  // 60,000 in all, 4 x 32, 19 / 17 / 31; four of 100,003 28 / 21 / 32; one of 1,000,000
+  // 284 / 113 / 86.
+  //   - Not cut at all where the block is no more than a workgroup gets through while
+  //     the pieces' results are joined: four segments of 1000 in all, 4 x 32, 12.8 / 8.2 us.
+  //   - Not where 64 or more segments are about that long (fewer take one launch less), if
+  //     the rounds of an uncut one are few or pass while the block's bytes do: 379
+  //     segments of 139,715, cut at 128 / not cut, 4 x 32 52 / 22, 2 x 100 51 / 50 and with
+  //     three hubs 51 / 112, 8 x 128 105 / 72 and 107 / 199 (these two are cut); 1500 of
+  //     500,000, 8 x 128, not cut: 337 / 188 and 364 / 315.
+  // Where a few lanes own a segment, one of 256 takes 45 us, so there are shorter pieces in a block
+  // that takes less, 64 / 128 / 256: 6600 segments of 2200 edges in all, three hubs,
+  // 14.1 / 17.2 / 53.0 us; 20,000 of 20,000 with hubs 17.0 / 17.3 / 17.6; 50,000 of 100,000
+  // with hubs 35.3 / 31.5 / 31.9; 100,000 of 1,000,000 with hubs 130.6 / 111.6 / 100.6.
+  const int groups = 64 / p.L;
+  if (p.owner == CA_GROUP) {
+    p.shift = E <= CA_SHORT_E ? 6 : E <= CA_MEDIUM_E ? 7 : 8;
+  } else {
+    p.shift = CA_SHIFT;
+    while (p.shift < CA_SHIFT_MAX && (E >> (p.shift + 1)) >= ca_pieces(groups, p.shift)) ++p.shift;
+    if (E <= std::min(1024, 128 * groups) && std::min(E, 2 * mean) <= 80 * groups) {
+      p.shift = 10;
+    } else if (N >= CA_FEW && mean <= 2048) {
+      int whole = p.shift;
+      while ((int64_t(1) << whole) < 2 * mean) ++whole;
+      const int64_t round = groups * CA_ROWS * (p.owner == CA_BLOCK ? CA_WAVES : 1);
+      if ((int64_t(1) << whole) <= round * (12 + (3 * E * H * dh >> 23))) p.shift = whole;
+    }
   }
   // cells of cap edges; none where no segment can be long
   p.cells = E > (int64_t(1) << p.shift) ? ((E - 1) >> p.shift) + 1 : 0;
@@ -593,13 +609,13 @@ static CaPlan ca_plan(int64_t N, int64_t E, int H, int dh) {
 static int64_t ca_cells_most(int64_t N, int64_t E, int H, int dh) {
   const CaPlan p = ca_plan(N, E, H, dh);
   auto cells = [](int64_t e, int shift) { return (e >> shift) + 1; };
-  // pieces of 256 and more are taken where there would be 2 * 480 of the next shorter ones
-  int64_t most = std::max({p.cells, cells(std::min<int64_t>(E, 480 << (CA_SHIFT + 1)), CA_SHIFT),
+  // pieces of 64 up to twice CA_PIECES of them, then longer ones up to CA_SHIFT_MAX
+  int64_t most = std::max({p.cells, std::min(cells(E, CA_SHIFT), 2 * CA_PIECES + 1),
                            cells(E, CA_SHIFT_MAX)});
   if (N > CA_LANES_N) {                // a few lanes may own a segment, at this many edges or fewer
     const int64_t e = std::min(E, 2 * CA_ROWS * (64 / p.L) * N);
     most = std::max({most, cells(std::min(e, CA_SHORT_E), 6), cells(std::min(e, CA_MEDIUM_E), 7),
-                     cells(e, CA_SHIFT)});
+                     cells(e, 8)});
   }
   return most;
 }
