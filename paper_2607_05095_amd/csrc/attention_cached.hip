@@ -79,18 +79,23 @@ __device__ __forceinline__ float ca_pow2(float x, float m) {   // 2^(x - m), 0 f
 
 // A lane's place: head h, its codes [first, first + VE) of which those from `own` on
 // are its own (the last piece of a head of 8 (2 k + 1) codes starts 8 earlier
-// and shares them with its neighbour); the running softmax.
+// and shares them with its neighbour); the running softmax.  Its scale is that of its own
+// codes; where the 8 others are of the group before, they may not be finite under it,
+// and their products with q = 0 are dropped (`keep`).
 template <int VE>
 struct CaLane {
   int h, l, first, own;
   bool mine;                         // the lane holds codes
   uint32_t code, scale;              // its K codes and their scale within a record
+  uint32_t keep;                     // 0 where the first 8 codes are of another group, else all bits
   float q[VE], mx, Z, acc[VE];
 };
 
-// lanes per head: known to the compiler, or (LPH = 0) read from the arguments
+// lanes per head: known to the compiler, or (LPH = 0) read from the arguments; negative where a
+// last piece may begin in another group than its own codes (heads of 1 to 8 elements past
+// a multiple of 32): their test in the others took 3 to 5 per cent
 template <int LPH>
-__device__ __forceinline__ int ca_lph(const CaArgs& a) { return LPH > 0 ? LPH : a.lph; }
+__device__ __forceinline__ int ca_lph(const CaArgs& a) { return LPH > 0 ? LPH : LPH < 0 ? -LPH : a.lph; }
 
 template <typename T, int FMT, int VE, int LPH>
 __device__ __forceinline__ void ca_init(const CaArgs& a, int64_t v, CaLane<VE>& c) {
@@ -113,7 +118,8 @@ __device__ __forceinline__ void ca_init(const CaArgs& a, int64_t v, CaLane<VE>& 
   c.mx = -INFINITY;
   c.Z = 0.f;
   c.code = uint32_t(c.h * a.rec.code_bytes + (FMT == FAST_MXFP4 ? c.first / 2 : c.first));
-  c.scale = uint32_t(a.rec.scale_off + c.h * a.rec.groups + c.first / MX_GROUP);
+  c.scale = uint32_t(a.rec.scale_off + c.h * a.rec.groups + c.own / MX_GROUP);
+  c.keep = c.first / MX_GROUP == c.own / MX_GROUP ? ~0u : 0u;
 }
 
 // No record.
@@ -170,8 +176,11 @@ __device__ __forceinline__ void ca_fold(const CaArgs& a, const uint32_t (&rec)[C
       float k[VE], d = 0.f;
       r.k[i].unpack(mx_scale(r.ks[i]), k);
 #pragma unroll
-      for (int j = 0; j < VE; ++j) d = fmaf(c.q[j], k[j], d);
-      if constexpr (LPH > 0) d = group_sum_ct<LPH>(d);
+      for (int j = 0; j < VE; ++j) {
+        if (VE == 16 && LPH <= 0 && j == MX_PIECE) d = __uint_as_float(__float_as_uint(d) & c.keep);
+        d = fmaf(c.q[j], k[j], d);
+      }
+      if constexpr (LPH != 0) d = group_sum_ct<(LPH > 0 ? LPH : -LPH)>(d);
       else d = group_sum(d, a.lph);
       t[i] = d * (d > 0.f ? 1.f : a.slope);
     }
@@ -544,6 +553,7 @@ static int64_t ca_pieces(int groups, int shift) { return groups <= 2 ? CA_PIECES
 // How a call is carried out.
 struct CaPlan {
   int ve, lph, L;
+  bool cross;                          // a last piece may begin in another group than its own codes
   CaOwner owner;
   bool few;                            // k_attn_cached_few
   int shift;
@@ -551,10 +561,9 @@ struct CaPlan {
 };
 static CaPlan ca_plan(int64_t N, int64_t E, int H, int dh) {
   CaPlan p = {};
-  // 16 codes a lane (fewer instructions per record) where every lane's codes lie in
-  // one group: a head's last piece may start 8 codes early, which crosses a
-  // group's border where 1 to 8 elements are left past one.
-  p.ve = dh > 8 && (dh % MX_GROUP == 0 || dh % MX_GROUP > 8) ? 16 : 8;
+  // 16 codes a lane: half the lanes and fewer instructions per record
+  p.ve = dh > 8 ? 16 : 8;
+  p.cross = dh % MX_GROUP >= 1 && dh % MX_GROUP <= MX_PIECE;
   p.lph = pow2_at_least((dh + p.ve - 1) / p.ve);
   int hpw = pow2_at_least(H);
   if (hpw > 64 / p.lph) hpw = 64 / p.lph;
@@ -637,8 +646,10 @@ static void launch_ca(const CaArgs& a, const CaPlan& p, bool big, dim3 grid, dim
   if (p.ve == 8) FAST_CA(8, 0, true);
   else if (big) FAST_CA(16, 0, true);
   else if (a.lph == 2) FAST_CA(16, 2, false);
-  else if (a.lph == 4) FAST_CA(16, 4, false);
-  else if (a.lph == 8) FAST_CA(16, 8, false);
+  else if (a.lph == 4 && !p.cross) FAST_CA(16, 4, false);
+  else if (a.lph == 4) FAST_CA(16, -4, false);
+  else if (a.lph == 8 && !p.cross) FAST_CA(16, 8, false);
+  else if (a.lph == 8) FAST_CA(16, -8, false);
   else FAST_CA(16, 0, true);
 #undef FAST_CA
 #undef FAST_CAK

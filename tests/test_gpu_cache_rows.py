@@ -256,6 +256,35 @@ def test_cached_attention_many_segments(H, dh, fmt):
     b.check(*b.run())
 
 
+@pytest.mark.parametrize("H,dh", [(2, 33), (4, 40), (3, 65), (2, 100), (1, 136), (3, 161), (1, 232)])
+@pytest.mark.parametrize("fmt", [8, 4])
+def test_cached_attention_heads_just_past_a_group(H, dh, fmt):
+    """The last piece of a head starts in the group before its own codes, whose scale may be any
+    other: here so large that the codes before would overflow under it."""
+    print(f"[cache] attention H={H} dh={dh} fmt={fmt}, scales far apart", flush=True)
+    counts = [3, 0, 70, 9, 1] * 30
+    b = Block(counts, H, dh, fmt, "bf16", seed=dh)
+    b.check(*b.run())
+    b = Block(counts, H, dh, fmt, "f32", seed=dh)
+    r = np.random.default_rng(dh)
+    last = dh // 32 * 32
+    kv = r.normal(size=(b.rows, 2 * H, dh)).astype(np.float32)
+    kv[:, :, last - 32:last] = np.clip(kv[:, :, last - 32:last], -1, 1)
+    kv[:, :, last - 8:last] = 1.0                       # 256 or 4 times its group's scale
+    # the largest magnitude, 2^120 (2^126) times a code, is finite; 256 (4) times that scale is not
+    top = np.float32(3.0e38 if fmt == 8 else 2.6e38)
+    kv[:, :H, last:] = np.clip(kv[:, :H, last:], -1, 1) * top
+    kv[:, :H, last] = top
+    c, s = p64.quantize(kv, fmt)
+    b.kv = p64.values(c, s, fmt)
+    assert np.abs(b.kv).max() < 3.4e38
+    b.cache = to_dev(p64.pack(c, s, fmt, fill=0xFF))
+    b.q64[..., last:] *= 1e-37
+    b.q64 = b.q64.astype(np.float32).astype(np.float64)
+    b.Q = to_dev(b.q64.astype(np.float32))
+    b.check(*b.run())
+
+
 @pytest.mark.parametrize("most", [1, 20, 40])
 def test_cached_attention_long_among_very_many_short(most):
     """Lengths about every cut of a block whose segments belong to a few lanes each."""
