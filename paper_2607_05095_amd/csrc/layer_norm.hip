@@ -16,7 +16,7 @@
 // row, so the terms of dgamma and dbeta are added in its registers, at most
 // LN_ROWS of them in fp32; a workgroup joins its groups in fp64 in LDS and
 // writes one partial row, and a second launch adds the partial rows in fp64 in
-// their order.  No atomics: repeated calls give the same bits.
+// their order (one workgroup writes the sums itself).  No atomics: repeated calls give the same bits.
 #include <algorithm>
 
 #include "rows.h"
@@ -28,6 +28,7 @@ constexpr int LN_MAX_G = 1024;   // lanes of a group, at most
 constexpr int LN_ELEMS = 16;     // elements of a row per lane, at most
 constexpr int64_t LN_BLOCKS = 1024;   // workgroups of the backward, about
 constexpr int LN_ROWS = 32;      // rows that a lane adds up in fp32, at most
+constexpr int64_t LN_ALONE = 2;  // rows per group up to which one workgroup does the backward
 constexpr int64_t LN_MAX_D = 8192;
 
 // Sums over the G lanes of a group; G > 64: over the workgroup, through
@@ -197,7 +198,9 @@ struct LnBwdArgs {
   const void* dy;
   const void* dsum;
   void* dx;
-  float* part;         // [workgroups][2][D], or NULL: dx only
+  float* part;         // [workgroups][2][D], or NULL: dx only, or one workgroup
+  float* dgamma;       // one workgroup: the sums themselves, each may be NULL
+  float* dbeta;
 };
 
 template <typename T, int P, bool TAIL, bool NT>
@@ -273,8 +276,9 @@ __global__ void __launch_bounds__(LN_MAX_G) k_ln_bwd(LnBwdArgs a) {
       ln_store<T, TAIL, NT>(static_cast<T*>(a.dx) + row * D, Chunk(lane + p * G, D), d[p]);
     }
   }
-  if (!a.part) return;
-  float* out = a.part + int64_t(blockIdx.x) * 2 * D;
+  float* og = a.part ? a.part + int64_t(blockIdx.x) * 2 * D : a.dgamma;
+  float* ob = a.part ? og + D : a.dbeta;
+  if (!og && !ob) return;
   if (groups == 1) {                     // the lanes of the workgroup own different columns
 #pragma unroll
     for (int p = 0; p < P; ++p) {
@@ -282,8 +286,8 @@ __global__ void __launch_bounds__(LN_MAX_G) k_ln_bwd(LnBwdArgs a) {
 #pragma unroll
       for (int j = 0; j < VE; ++j)
         if (k.own(j)) {
-          out[k.first + j] = dg[p][j];
-          out[D + k.first + j] = db[p][j];
+          if (og) og[k.first + j] = dg[p][j];
+          if (ob) ob[k.first + j] = db[p][j];
         }
     }
     return;
@@ -303,7 +307,8 @@ __global__ void __launch_bounds__(LN_MAX_G) k_ln_bwd(LnBwdArgs a) {
     double t = 0.0;
 #pragma unroll 8
     for (int k = 0; k < groups; ++k) t += s_col[2 * k * D + col];
-    out[col] = float(t);
+    float* o = col < D ? og : ob;
+    if (o) o[col < D ? col : col - D] = float(t);
   }
 }
 
@@ -361,6 +366,10 @@ static LnPlan ln_plan(int64_t n, int D, int ve) {
   int64_t per = (n + LN_BLOCKS * groups - 1) / (LN_BLOCKS * groups);
   per = per < 1 ? 1 : (per > LN_ROWS ? LN_ROWS : per);
   L.nb = (n + per * groups - 1) / (per * groups);
+  // Few rows: one workgroup, which writes the sums itself; both directions of 4 rows
+  // of 54 fp32 in two launches 5.2 us, in three 7.3.  2 / 4 rows per group: 32 / 64 rows of 172
+  // fp32 8.8 / 11.3, with more workgroups and a launch for their sums 9.8 / 9.7.
+  if (n <= LN_ALONE * groups) L.nb = 1;
   return L;
 }
 
@@ -497,14 +506,14 @@ extern "C" fast_status_t fast_layer_norm_bwd(int64_t n, int D, fast_dtype_t dtyp
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (n > 0) {
     const LnBwdArgs a = {n, D, L.G, h, gamma, mean, rstd, dy, dsum, dx,
-                         sums ? static_cast<float*>(ws) : nullptr};
+                         sums && L.nb > 1 ? static_cast<float*>(ws) : nullptr, dgamma, dbeta};
     // at most 32 KB: a lane owns at most LN_ELEMS columns
     const size_t lds = sums && L.G < L.threads ? size_t(L.threads / L.G) * 2 * D * sizeof(float) : 0;
     const void* rows[] = {h, dy, dsum, dx};
     const bool nt = ln_stream(n, D, es, 3 + (dsum != nullptr), rows, 4);
     launch_ln(a, L, uint32_t(L.nb), lds, dtype, nt, st);
   }
-  if (sums)
+  if (sums && (n == 0 || L.nb > 1))
     hipLaunchKernelGGL(k_ln_bwd_sum, dim3((2 * D + LNS_COLS - 1) / LNS_COLS), dim3(LNS_THREADS), 0, st,
                        static_cast<const float*>(ws), n > 0 ? L.nb : 0, D, dgamma, dbeta);
   return check_launch(fn);

@@ -148,6 +148,22 @@ def test_layer_norm_bwd(n, D, dt, dsum):
         assert torch.equal(dx3, dx[:n])
 
 
+@pytest.mark.parametrize("n,D", [(1, 1), (2, 54), (32, 54), (33, 54), (2, 944), (1, 8192), (2, 8192), (3, 8192), (70000, 4)])
+def test_layer_norm_bwd_of_one_weight_alone(n, D):
+    """Whether one workgroup writes the sums or several have theirs added."""
+    h, dy = rand((n, D), "f32", 21)[0], rand((n, D), "f32", 22)[0]
+    mean, rstd = h.mean(1), 1 / (h.var(1, unbiased=False) + 1e-3).sqrt()
+    dx, wsb = torch.empty_like(h), fast.fast_layer_norm_bwd_workspace(n, D)
+    ws = torch.empty(wsb, dtype=torch.uint8, device="cuda")
+    both, one = torch.full((2, 2, D + 1), 7.0, device="cuda").unbind(0)
+    args = (n, D, fast.F32, h, None, mean, rstd, dy, None, dx)
+    fast.fast_layer_norm_bwd(*args, both[0], both[1], ws, wsb)
+    fast.fast_layer_norm_bwd(*args, one[0], None, ws, wsb)
+    assert (one[1] == 7).all()
+    fast.fast_layer_norm_bwd(*args, None, one[1], ws, wsb)
+    assert torch.equal(both, one) and (both[:, D] == 7).all()
+
+
 def test_layer_norm_bwd_without_rows_zeroes_the_weight_gradients():
     dg, db = torch.full((2, 12), 7.0, device="cuda").unbind(0)
     wsb = fast.fast_layer_norm_bwd_workspace(0, 12)
