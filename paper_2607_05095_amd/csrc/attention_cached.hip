@@ -445,13 +445,11 @@ __device__ __forceinline__ void ca_join(const CaArgs& a, int64_t v, int64_t m, i
   __syncthreads();                     // before the next segment's sums
 }
 
-// The marks of cells b + i CA_CELLS, and of the cells behind them, for i in [base, base + 64): a
-// lane each, one round trip for all.  Returns the lanes that have one.
-__device__ __forceinline__ uint64_t ca_marks(const CaArgs& a, int64_t b, int64_t base, int32_t& here,
-                                             int32_t& next) {
-  const int64_t i = base + (threadIdx.x & 63), m = b + i * CA_CELLS;
-  here = i < a.rounds && m < a.cells ? a.mark[ca_mark_at(a, m)] : -1;
-  next = i < a.rounds && m + 1 < a.cells ? a.mark[ca_mark_at(a, m + 1)] : -1;
+// The marks of a lane's cell m (-1: none) and of the cell behind it, one round trip for the
+// wave.  Returns the lanes that have one.
+__device__ __forceinline__ uint64_t ca_marks(const CaArgs& a, int64_t m, int32_t& here, int32_t& next) {
+  here = m >= 0 && m < a.cells ? a.mark[ca_mark_at(a, m)] : -1;
+  next = m >= 0 && m + 1 < a.cells ? a.mark[ca_mark_at(a, m + 1)] : -1;
   // marks of malformed offsets may be anything
   if (here >= a.N) here = -1;
   if (next >= a.N) next = -1;
@@ -465,8 +463,10 @@ __global__ void __launch_bounds__(CA_THREADS) k_attn_cached_long(CaArgs a) {
   __shared__ float s_acc[CA_WAVES][VE + 2][CA_PAD];
   const int64_t cap = int64_t(1) << a.shift;
   for (int64_t base = 0; base < a.rounds; base += 64) {
+    const int64_t k = base + (threadIdx.x & 63);
     int32_t here, next;
-    for (uint64_t set = ca_marks(a, blockIdx.x, base, here, next); set; set &= set - 1) {   // the same in every wave
+    for (uint64_t set = ca_marks(a, k < a.rounds ? blockIdx.x + k * CA_CELLS : -1, here, next); set;
+         set &= set - 1) {             // the same in every wave
       const int i = __builtin_ctzll(set);
       const int64_t x = (blockIdx.x + (base + i) * CA_CELLS) << a.shift, y = x + cap;
       int32_t seg[2] = {__builtin_amdgcn_readlane(here, i), __builtin_amdgcn_readlane(next, i)};
@@ -487,19 +487,21 @@ __global__ void __launch_bounds__(CA_THREADS) k_attn_cached_long(CaArgs a) {
 // gridDim.x, ..., head blockIdx.y: those that hold the next cell's first edge.
 template <typename T>
 __global__ void __launch_bounds__(CJ_THREADS) k_attn_cached_join(CaArgs a) {
-  for (int64_t b = blockIdx.x; b < CA_CELLS && b < a.cells; b += gridDim.x) {
-    for (int64_t base = 0; base < a.rounds; base += 64) {
-      int32_t here, next;
-      for (uint64_t set = ca_marks(a, b, base, here, next); set; set &= set - 1) {
-        const int i = __builtin_ctzll(set);
-        const int64_t m = b + (base + i) * CA_CELLS;
-        const int32_t v = __builtin_amdgcn_readlane(next, i);
-        if (v < 0) continue;
-        int64_t s, t;
-        ca_segment(a, v, s, t);
-        if (t - s > (int64_t(1) << a.shift) && s >> a.shift == m)
-          ca_join<T>(a, v, m, ((t - 1) >> a.shift) - m + 1, blockIdx.y);
-      }
+  // the cells of all b, CA_CELLS apart, in one list: 64 of them at a time
+  const uint32_t rounds = uint32_t(a.rounds), lists = (CA_CELLS - blockIdx.x + gridDim.x - 1) / gridDim.x;
+  for (uint32_t base = 0; base < lists * rounds; base += 64) {
+    const uint32_t q = base + (threadIdx.x & 63), l = q / rounds;
+    const int64_t m = l < lists ? blockIdx.x + l * gridDim.x + int64_t(q - l * rounds) * CA_CELLS : -1;
+    int32_t here, next;
+    for (uint64_t set = ca_marks(a, m, here, next); set; set &= set - 1) {
+      const int i = __builtin_ctzll(set);
+      const int32_t v = __builtin_amdgcn_readlane(next, i);
+      if (v < 0) continue;
+      const int64_t at = __builtin_amdgcn_readlane(int32_t(m), i);    // at most 2^23 cells
+      int64_t s, t;
+      ca_segment(a, v, s, t);
+      if (t - s > (int64_t(1) << a.shift) && s >> a.shift == at)
+        ca_join<T>(a, v, at, ((t - 1) >> a.shift) - at + 1, blockIdx.y);
     }
   }
 }
