@@ -7,8 +7,8 @@
 // at a random place, against two fused multiply-adds per element.  L lanes
 // hold a record's heads, 16 (or 8) codes of K and of V each; CA_ROWS records per lane
 // are in flight.  A running maximum, sum and accumulators in base 2 make one pass.
-// 264,000 segments of 2.4 M edges, 8 bits, 2 x 50 fp32: 154 us for the first launch, 6.9 TB/s of the
-// lines it touches (a record two, a slot of an 8 MB map one), 164 with the other two.
+// 264,000 segments of 2.4 M edges, 8 bits, 2 x 50 fp32: 153 us for the first launch, 6.9 TB/s of the
+// lines it touches (a record two, a slot of an 8 MB map one), 162 with the other two.
 //
 // Where there are many short segments, L lanes own one and walk its edges: no
 // joins.  Where segments are longer, or too few to fill the chip that way, a wave
