@@ -599,9 +599,12 @@ fast_status_t fast_rotary_bwd(int64_t n, int H, int dh, fast_dtype_t dtype, cons
  * feature rows, 2H of dh for packed K|V rows.  Every vector is cut into
  * groups of 32 elements (the last may be shorter); a group has a scale 2^k,
  * the smallest for which its largest magnitude is at most the format's largest
- * value, and an element is the nearest code (ties to even) times the scale:
- *   FAST_MXFP8: e4m3, largest 448, relative error at most 2^-4
- *   FAST_MXFP4: e2m1, values 0, 0.5, 1, 1.5, 2, 3, 4, 6
+ * value, and an element is the nearest code (ties to even) times the scale, of
+ * the codes for which that product is below 2^128: finite rows read back finite.
+ *   FAST_MXFP8: e4m3, largest 448, smallest step 2^-9: an element is off by at
+ *     most the larger of its 16th and 2^(k-10)
+ *   FAST_MXFP4: e2m1, values 0, 0.5, 1, 1.5, 2, 3, 4, 6: off by at most the
+ *     larger of its 4th and 2^(k-2)
  * with k >= -127.  A group that holds an infinity or a NaN reads back as NaN.
  * Record (row s of the cache at byte s * fast_cache_row_bytes): the codes of
  * each vector, padded to 8 (a 4-bit pair's first code in the low half), then

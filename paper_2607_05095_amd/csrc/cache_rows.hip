@@ -128,6 +128,10 @@ __global__ void __launch_bounds__(CR_THREADS) k_cache_write(CacheArgs a) {
       m = m > o ? m : o;
     }
     const uint32_t sb = mx_scale_byte<FMT>(__uint_as_float(m));
+    if (sb == MX_TOP_BYTE<FMT>) {    // finite rows read back finite
+#pragma unroll
+      for (int j = 0; j < N; ++j) x[k][j] = fminf(fmaxf(x[k][j], -MX_TOP<FMT>), MX_TOP<FMT>);
+    }
     MxPiece<FMT, N> p;
     if (sb == 255u) p.zero();
     else p.pack(mx_scale(sb), x[k]);

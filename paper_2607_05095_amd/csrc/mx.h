@@ -185,4 +185,9 @@ __device__ __forceinline__ uint32_t mx_scale_byte(float amax) {
   return e > 0 ? uint32_t(e) : 0u;
 }
 
+// The scale byte under which the nearest code may stand for 2^128, which fp32 does not hold
+// (groups of more than 448 2^119, 6 2^125), and the largest value below: 240 2^120, 3 2^126.
+template <int FMT> constexpr uint32_t MX_TOP_BYTE = FMT == FAST_MXFP4 ? 253u : 247u;
+template <int FMT> constexpr float MX_TOP = FMT == FAST_MXFP4 ? 0x1.8p127f : 0x1.ep127f;
+
 }  // namespace fast
