@@ -698,8 +698,9 @@ extern "C" fast_status_t fast_edge_attention_fwd_cached(
   const size_t es = elem_size(dtype);
   if (!aligned(Q, es) || !aligned(out, es))
     return fail(FAST_ERR_UNSUPPORTED, "%s: rows not %d-byte aligned", fn, int(es));
-  if (!aligned(cache, 16) || !aligned(ids, 8) || !aligned(lse, 4))
-    return fail(FAST_ERR_UNSUPPORTED, "%s: cache, ids or lse misaligned", fn);
+  if (!aligned(cache, 16) || !aligned(ids, 8) || !aligned(slot_map, 4) || !aligned(g->dst_offsets, 4) ||
+      !aligned(lse, 4))
+    return fail(FAST_ERR_UNSUPPORTED, "%s: cache, ids, slot_map, dst_offsets or lse misaligned", fn);
   const size_t need = fast_edge_attention_cached_workspace(N, E, H, dh);
   if (!ws || ws_bytes < need)
     return fail(FAST_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", fn, ws ? ws_bytes : 0, need);

@@ -179,8 +179,9 @@ __global__ void __launch_bounds__(CR_THREADS) k_cache_gather(CacheArgs a) {
 }
 
 static fast_status_t cache_check(const char* fn, const int64_t* ids, int64_t n, int64_t id_bound,
-                                 int parts, int width, fast_dtype_t dtype, const void* rows,
-                                 fast_cache_format_t fmt, const void* cache, int64_t cache_rows) {
+                                 const int32_t* slot_map, int parts, int width, fast_dtype_t dtype,
+                                 const void* rows, fast_cache_format_t fmt, const void* cache,
+                                 int64_t cache_rows) {
   if (n < 0 || id_bound < 0 || cache_rows < 0) return fail(FAST_ERR_INVALID_ARG, "%s: negative size", fn);
   if (dtype != FAST_F32 && dtype != FAST_BF16) return fail(FAST_ERR_INVALID_ARG, "%s: bad dtype", fn);
   const fast_status_t s = mx_check(fn, parts, width, fmt);
@@ -193,6 +194,7 @@ static fast_status_t cache_check(const char* fn, const int64_t* ids, int64_t n, 
   if (!aligned(rows, es)) return fail(FAST_ERR_UNSUPPORTED, "%s: rows not %d-byte aligned", fn, int(es));
   if (!aligned(cache, 16)) return fail(FAST_ERR_UNSUPPORTED, "%s: cache not 16-byte aligned", fn);
   if (!aligned(ids, 8)) return fail(FAST_ERR_UNSUPPORTED, "%s: ids not 8-byte aligned", fn);
+  if (!aligned(slot_map, 4)) return fail(FAST_ERR_UNSUPPORTED, "%s: slot_map not 4-byte aligned", fn);
   return FAST_OK;
 }
 
@@ -247,8 +249,8 @@ extern "C" fast_status_t fast_cache_write(const int64_t* ids, int64_t n, int64_t
                                           int64_t cache_rows, int distinct, void* ws,
                                           size_t ws_bytes, fast_stream_t stream) {
   const char* fn = "fast_cache_write";
-  const fast_status_t s = cache_check(fn, ids, n, id_bound, parts, width, dtype, src, format, cache,
-                                      cache_rows);
+  const fast_status_t s = cache_check(fn, ids, n, id_bound, slot_map, parts, width, dtype, src, format,
+                                      cache, cache_rows);
   if (s != FAST_OK) return s;
   if (n == 0 || cache_rows == 0) return ok();
   if (!distinct) {
@@ -289,8 +291,8 @@ extern "C" fast_status_t fast_cache_gather(const int64_t* ids, int64_t n, int64_
                                            int64_t cache_rows, fast_dtype_t dtype, void* rows,
                                            fast_stream_t stream) {
   const char* fn = "fast_cache_gather";
-  const fast_status_t s = cache_check(fn, ids, n, id_bound, parts, width, dtype, rows, format, cache,
-                                      cache_rows);
+  const fast_status_t s = cache_check(fn, ids, n, id_bound, slot_map, parts, width, dtype, rows, format,
+                                      cache, cache_rows);
   if (s != FAST_OK) return s;
   if (n == 0 || cache_rows == 0) return ok();
   CacheArgs a = cache_args(ids, n, id_bound, slot_map, parts, width, format, cache_rows, dtype, false);
