@@ -580,7 +580,8 @@ fast_status_t fast_layer_norm_bwd(int64_t n, int D, fast_dtype_t dtype, const vo
  * outside [0, axes) read the nearest axis; omega: [pairs] fp32.  The angle is
  * exact in fp64, its sine and cosine are within 2e-7 at any position; a position that
  * is not finite gives NaN.
- * Limits: H <= 64, dh <= 256, 2 * pairs <= dh, n < 2^31.
+ * Limits: H <= 64, dh <= 256, 2 * pairs <= dh, n and the strides < 2^31, rows
+ * that span less than 2^56 elements.
  * The backward turns dy by -theta (pos and omega are constants); its
  * arguments are the forward's, with dy in place of x and dx in place of y.
  * ------------------------------------------------------------------------ */

@@ -202,6 +202,10 @@ static fast_status_t rotary(const char* fn, int64_t n, int H, int dh, fast_dtype
   if (ldx >= (int64_t(1) << 31) || ldy >= (int64_t(1) << 31))
     return fail(FAST_ERR_UNSUPPORTED, "%s: row stride >= 2^31", fn);
   if (n == 0) return ok();
+  // (n and the strides are below 2^31 each: the products fit, their bytes might not)
+  if ((n - 1) * (ldx > ldy ? ldx : ldy) >= (int64_t(1) << 56))
+    return fail(FAST_ERR_UNSUPPORTED, "%s: %lld rows, %lld and %lld elements apart", fn, (long long)n,
+                (long long)ldx, (long long)ldy);
   if (!x || !y || (pairs > 0 && (!pos || !omega)))
     return fail(FAST_ERR_INVALID_ARG, "%s: NULL rows/pos/omega", fn);
   if (!aligned(x, es) || !aligned(y, es))
