@@ -540,7 +540,8 @@ fast_status_t fast_index_add_scaled_rows(const int32_t* occ_off, const int32_t* 
  * Statistics and products are fp32, the mean taken before the squares.
  * Limits: 1 <= D <= 8192, n < 2^31, and (as for the operators below) fewer than
  * 2^32 threads: rows of some 1.7e10 elements.  Rows aligned to their element; y and sum
- * may each be x or res, not both the same.  eps >= 0.
+ * may each be x or res, not both the same (arrays of rows that overlap otherwise are
+ * refused).  eps >= 0.
  * ------------------------------------------------------------------------ */
 fast_status_t fast_layer_norm_fwd(int64_t n, int D, fast_dtype_t dtype, const void* x,
                                   const void* res, const float* gamma, const float* beta,
@@ -554,7 +555,9 @@ fast_status_t fast_layer_norm_fwd(int64_t n, int D, fast_dtype_t dtype, const vo
  * NULL, or the gradient [n, D] of dtype that reaches the sum on another path.
  * dgamma, dbeta: [D] fp32, overwritten (zeros when n = 0), each optional;
  * added in fp32 over at most 32 rows and in fp64 beyond (a workgroup's sum
- * rounded to fp32 in between), in a fixed order: repeated calls give the same bits.  dx: [n, D] of dtype; it may be dy or dsum.
+ * rounded to fp32 in between), in a fixed order: repeated calls give the same bits.
+ * dx: [n, D] of dtype; it may be dy or dsum, and lies apart from them and h otherwise
+ * (rows of dx shifted against those of h, dy or dsum are refused).
  * Workspace, needed for dgamma or dbeta only: fast_layer_norm_bwd_workspace(n, D)
  * bytes, 8-byte aligned; one for the largest n serves smaller ones. */
 size_t fast_layer_norm_bwd_workspace(int64_t n, int D);

@@ -452,6 +452,10 @@ extern "C" fast_status_t fast_layer_norm_fwd(int64_t n, int D, fast_dtype_t dtyp
     return fail(FAST_ERR_UNSUPPORTED, "%s: rows not %d-byte aligned", fn, int(es));
   if (!aligned(gamma, 4) || !aligned(beta, 4) || !aligned(mean, 4) || !aligned(rstd, 4))
     return fail(FAST_ERR_UNSUPPORTED, "%s: gamma/beta/mean/rstd not 4-byte aligned", fn);
+  const int64_t bytes = n * D * int64_t(es);
+  if (shifted(y, x, bytes) || shifted(y, res, bytes) || shifted(sum, x, bytes) || shifted(sum, res, bytes) ||
+      shifted(y, sum, bytes))
+    return fail(FAST_ERR_INVALID_ARG, "%s: y or sum overlaps x, res or the other, shifted", fn);
   const LnPlan L = ln_plan(n, D, 16 / int(es));
   const LnArgs a = {n, D, L.G, x, res, gamma, beta, eps, y, sum, mean, rstd};
   const int64_t per = L.threads / L.G;
@@ -494,6 +498,9 @@ extern "C" fast_status_t fast_layer_norm_bwd(int64_t n, int D, fast_dtype_t dtyp
   if (!aligned(gamma, 4) || !aligned(mean, 4) || !aligned(rstd, 4) || !aligned(dgamma, 4) ||
       !aligned(dbeta, 4))
     return fail(FAST_ERR_UNSUPPORTED, "%s: gamma/mean/rstd/dgamma/dbeta not 4-byte aligned", fn);
+  const int64_t bytes = n * D * int64_t(es);
+  if (shifted(dx, h, bytes) || shifted(dx, dy, bytes) || shifted(dx, dsum, bytes))
+    return fail(FAST_ERR_INVALID_ARG, "%s: dx overlaps h, dy or dsum, shifted", fn);
   if (sums) {
     if (!ws || ws_bytes < fast_layer_norm_bwd_workspace(n, D))
       return fail(FAST_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", fn, ws ? ws_bytes : 0,

@@ -106,6 +106,13 @@ __device__ __forceinline__ void store_chunk(T* __restrict__ p, int n, const floa
   store_chunk_of<NT>(p, n, x);
 }
 
+// Do two arrays of as many bytes overlap other than byte on byte?  NULL: no array.
+inline bool shifted(const void* a, const void* b, int64_t bytes) {
+  if (!a || !b || a == b) return false;
+  const uintptr_t p = reinterpret_cast<uintptr_t>(a), q = reinterpret_cast<uintptr_t>(b);
+  return (p > q ? p - q : q - p) < uint64_t(bytes);
+}
+
 // A launch has fewer than 2^32 threads along an axis.
 inline bool grid_fits(int64_t blocks, int64_t threads) { return blocks * threads < (int64_t(1) << 32); }
 

@@ -5,7 +5,8 @@ import ctypes
 import pytest
 
 import paper_2607_05095_amd as fast
-from tests.test_layer_abi import ATT, BIG, CG, CW, FAKE, ROT, UNSUPPORTED, call
+from tests.test_layer_abi import (ATT, BIG, CG, CW, FAKE, INVALID, NORM, NORM_B, OK, ROT, UNSUPPORTED,
+                                  call)
 
 
 # ------------------------------------------------------------------ alignment
@@ -32,3 +33,36 @@ def test_rows_that_span_more_than_an_address_space_are_refused(name, kw):
     a.update(kw)
     assert call(name, a, {}) == UNSUPPORTED
     assert "apart" in fast.fast_last_error()
+
+
+# ------------------------------------------------------------------ overlaps
+NORM_BYTES = 5 * 10 * 4                          # rows of NORM and NORM_B
+
+
+@pytest.mark.parametrize("kw", [
+    dict(y=FAKE + 4), dict(y=FAKE - 4), dict(y=FAKE + NORM_BYTES - 4), dict(y=FAKE - NORM_BYTES + 4),
+    dict(res=FAKE + 4096, y=FAKE + 4096 + 8), dict(res=FAKE + 4096, y=FAKE + 4096, sum=FAKE + 40),
+    dict(res=FAKE + 4096, y=FAKE, sum=FAKE + 4096 + 40), dict(res=FAKE + 4096, y=FAKE + 8192, sum=FAKE + 8192 + 4),
+    dict(res=FAKE + 4096, y=FAKE + 8192, sum=FAKE + 8192 - 4)])
+def test_layer_norm_refuses_shifted_outputs(kw):
+    """An output that lies across an input or the other output: rows read what other rows wrote."""
+    assert call("fast_layer_norm_fwd", NORM, kw) == INVALID
+    assert "overlap" in fast.fast_last_error()
+
+
+@pytest.mark.parametrize("kw", [dict(dx=FAKE + 4), dict(dx=FAKE - NORM_BYTES + 4),
+                                dict(dy=FAKE + 4096, dx=FAKE + 4096 + 4), dict(h=FAKE + 4096, dx=FAKE + 4096 - 4),
+                                dict(dsum=FAKE + 4096, dx=FAKE + 4096 + NORM_BYTES - 4)])
+def test_layer_norm_bwd_refuses_a_shifted_gradient(kw):
+    assert call("fast_layer_norm_bwd", NORM_B, kw) == INVALID
+    assert "overlap" in fast.fast_last_error()
+
+
+def test_arrays_that_touch_do_not_overlap():
+    """Nor do those in one place: such calls get as far as the limit of a launch."""
+    n, D = BIG - 1, 500
+    for y in (FAKE + n * D * 4, FAKE):
+        assert call("fast_layer_norm_fwd", NORM, dict(n=n, D=D, y=y)) == UNSUPPORTED
+        assert "threads" in fast.fast_last_error()
+    assert call("fast_layer_norm_fwd", NORM, dict(n=n, D=D, y=FAKE + n * D * 4 - 4)) == INVALID
+    assert call("fast_layer_norm_fwd", NORM, dict(n=0, y=FAKE + 4)) == OK
