@@ -541,7 +541,7 @@ def fast_edge_attention_cached_workspace(num_dst: int, num_edges: int, H: int, d
 def fast_edge_attention_fwd_cached(g: TCSR, H, dh, dtype, Q, ids, id_bound, slot_map, format, cache,
                                    cache_rows, scale, neg_slope, out, lse, ws, ws_bytes,
                                    stream=None):
-    _resident((Q, ids, slot_map, cache, out, lse, ws))
+    _resident((*getattr(g, "_keep", ())[:1], Q, ids, slot_map, cache, out, lse, ws))   # its offsets first
     _check(lib().fast_edge_attention_fwd_cached(C.byref(g), H, dh, dtype, _ptr(Q), _ptr(ids),
                                                 id_bound, _ptr(slot_map), format, _ptr(cache),
                                                 cache_rows, scale, neg_slope, _ptr(out),

@@ -66,3 +66,13 @@ def test_arrays_that_touch_do_not_overlap():
         assert "threads" in fast.fast_last_error()
     assert call("fast_layer_norm_fwd", NORM, dict(n=n, D=D, y=FAKE + n * D * 4 - 4)) == INVALID
     assert call("fast_layer_norm_fwd", NORM, dict(n=0, y=FAKE + 4)) == OK
+
+
+# ------------------------------------------------------------------ tensors
+def test_offsets_of_the_host_are_refused():
+    """The graph's offsets live where the call's other tensors have to."""
+    import torch
+    g = fast.tcsr(torch.tensor([0, 3], dtype=torch.int32), 3)
+    with pytest.raises(fast.FastError, match="not on the current GPU"):
+        fast.fast_edge_attention_fwd_cached(g, 2, 50, fast.F32, FAKE, FAKE, 10, FAKE, fast.MXFP8, FAKE, 10, 1.0, 0.2,
+                                            FAKE, None, FAKE, 1 << 20, 0)
