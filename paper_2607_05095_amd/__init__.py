@@ -189,6 +189,24 @@ def _check(st: int):
         raise FastError(st, fast_last_error())
 
 
+def _rows_as_said(t, F, ld):
+    """A view's rows are F elements side by side, ld apart; raises otherwise."""
+    side = 1                             # elements side by side, from the last dimension on
+    outer = []
+    for size, step in zip(reversed(t.shape), reversed(t.stride())):
+        if size == 1:
+            continue
+        if side < F:
+            if step != side:
+                break
+            side *= size
+        else:
+            outer.append(step)
+    if side < F or (len(outer) == 1 and outer[0] != ld):
+        raise FastError(1, f"tensor of shape {tuple(t.shape)}, strides {tuple(t.stride())}: its rows "
+                           f"are not {F} elements side by side, {ld} apart")
+
+
 def _resident(dense=(), strided=()):
     """Tensors of a call live on the current device, and those without a row
     stride of their own are contiguous; raises otherwise."""
@@ -204,6 +222,13 @@ def _resident(dense=(), strided=()):
     for t in dense:
         if t is not None and not isinstance(t, int) and not t.is_contiguous():
             raise FastError(1, f"tensor of shape {tuple(t.shape)} is not contiguous")
+
+
+def _strided(F, x, ldx, y, ldy):
+    for t, ld in ((x, ldx), (y, ldy)):
+        # contiguous tensors hold rows of any stride
+        if t is not None and not isinstance(t, int) and not t.is_contiguous():
+            _rows_as_said(t, F, ld)
 
 
 def dtype_of(t) -> int:
@@ -498,6 +523,7 @@ def fast_rotary_fwd(n, H, dh, dtype, x, ldx, pos, axes, axis, omega, pairs, inte
                     stream=None):
     """x and y may be views whose rows are ldx and ldy elements apart."""
     _resident((pos, axis, omega), (x, y))
+    _strided(H * dh, x, ldx, y, ldy)
     _check(lib().fast_rotary_fwd(n, H, dh, dtype, _ptr(x), ldx, _ptr(pos), axes, _ptr(axis),
                                  _ptr(omega), pairs, int(interleaved), _ptr(y), ldy,
                                  _stream(stream)))
@@ -506,6 +532,7 @@ def fast_rotary_fwd(n, H, dh, dtype, x, ldx, pos, axes, axis, omega, pairs, inte
 def fast_rotary_bwd(n, H, dh, dtype, dy, lddy, pos, axes, axis, omega, pairs, interleaved, dx, lddx,
                     stream=None):
     _resident((pos, axis, omega), (dy, dx))
+    _strided(H * dh, dy, lddy, dx, lddx)
     _check(lib().fast_rotary_bwd(n, H, dh, dtype, _ptr(dy), lddy, _ptr(pos), axes, _ptr(axis),
                                  _ptr(omega), pairs, int(interleaved), _ptr(dx), lddx,
                                  _stream(stream)))

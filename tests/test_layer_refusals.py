@@ -69,6 +69,26 @@ def test_arrays_that_touch_do_not_overlap():
 
 
 # ------------------------------------------------------------------ tensors
+def test_rows_of_a_view_are_what_the_call_says():
+    """_rows_as_said looks at shapes and strides alone; ctypes callers have no views."""
+    import torch
+    H, dh = 2, 6
+    F = H * dh
+    kv = torch.zeros(5, 2, H, dh)
+    wide = torch.zeros(5, H, 2 * dh)
+    good = [(kv, 2 * F), (kv[:, 1], 2 * F), (kv[:, :1], 2 * F), (kv[::2], 4 * F), (kv[:1, 1], 99), (kv[:, 1].flatten(1), 2 * F),
+            (torch.zeros(5, 40)[:, :F], 40), (kv[:, 0].unflatten(0, (5, 1)), 2 * F), (torch.zeros(5, F), F)]
+    for t, ld in good:
+        fast._rows_as_said(t, F, ld)
+    bad = [(kv[:, 0].transpose(1, 2), 2 * F),           # a head's elements apart
+           (wide[..., :dh], 2 * F), (wide[..., ::2], 2 * F),
+           (kv[:, 1].transpose(0, 1), 2 * F), (torch.zeros(5, 40)[:, :F], F), (kv[:, 1], F),
+           (torch.zeros(F, 5).t(), F), (kv[:, 0].expand(5, H, dh)[:, :1].expand(5, H, dh), 2 * F)]
+    for t, ld in bad:
+        with pytest.raises(fast.FastError):
+            fast._rows_as_said(t, F, ld)
+
+
 def test_offsets_of_the_host_are_refused():
     """The graph's offsets live where the call's other tensors have to."""
     import torch
