@@ -92,7 +92,79 @@ def test_slots_named_by_the_ids_themselves():
         b.check(out, lse)
 
 
+BLOCKS = {"waves": [3, 0, 70, 9, 1] * 30, "few": [0, 1, 64, 65, 3, 3000], "lanes": [2] * 4500 + [300, 0, 70],
+          "workgroups": [100] * 90 + [255, 256, 257, 900]}
+
+
+@pytest.mark.parametrize("H,dh", [(2, 50), (8, 128)])
+def test_a_workspace_left_by_other_blocks(H, dh):
+    """One workspace for the largest block, never cleared, whatever block used it before."""
+    blocks = [Block(c, H, dh, 8, "f32", seed=k) for k, c in enumerate(BLOCKS.values())]
+    N, E = max(b.N for b in blocks), max(b.E for b in blocks)
+    wsb = fast.fast_edge_attention_cached_workspace(N, E, H, dh)
+    ws = torch.zeros(wsb, dtype=torch.uint8, device="cuda")
+    for b in blocks + blocks[::-1]:
+        out, lse, _, _, g, ids, smap = b.buffers()
+        b.check(*b.run(bufs=(out, lse, ws, wsb, g, ids, smap)))
+
+
+@pytest.mark.parametrize("name", list(BLOCKS))
+@pytest.mark.parametrize("H,dh", [(2, 50), (8, 128)])
+def test_malformed_offsets_write_nothing_else(name, H, dh):
+    """Offsets that decrease, are negative or past the last edge are clamped: the results say nothing, but only
+    they and the workspace are written, and the next call finds all it needs."""
+    print(f"[routes] malformed offsets {name} H={H} dh={dh}", flush=True)
+    b = Block(BLOCKS[name], H, dh, 8, "f32", seed=5)
+    guard = 4096
+    wsb = fast.fast_edge_attention_cached_workspace(b.N, b.E, H, dh)
+    r = np.random.default_rng(H)
+    for kind in range(4):
+        off = b.off.copy()
+        at = r.choice(b.N + 1, max(b.N // 3, 2), replace=False)
+        if kind == 0:
+            off[at] = r.integers(-2 ** 31, 2 ** 31, len(at))
+        elif kind == 1:
+            off = off[::-1].copy()
+        elif kind == 2:
+            off[:] = r.integers(0, b.E + 1, len(off))
+        else:
+            off[1::2] = 2 ** 31 - 1
+        ws = torch.full((wsb + guard,), kind, dtype=torch.uint8, device="cuda")
+        ws[wsb:] = 0xA5
+        bufs = b.buffers()
+        fast.fast_edge_attention_fwd_cached(fast.tcsr(to_dev(off.astype(np.int32)), b.E), H, dh, 0, b.Q, bufs[5], b.bound,
+                                            bufs[6], fast.MXFP8, b.cache, b.rows, b.scale, b.slope, bufs[0], bufs[1],
+                                            ws, wsb)
+        assert (bufs[0][b.N] == 7).all() and (bufs[1][b.N] == 7).all() and (ws[wsb:] == 0xA5).all()
+        b.check(*b.run(bufs=(bufs[0], bufs[1], ws, wsb) + bufs[4:]))
+
+
 # ------------------------------------------------------------------ cached rows
+def test_cached_rows_past_two_to_the_31_elements():
+    """Rows written from and read to arrays of more than 2^31 elements."""
+    n, width, rows = 13_000_000, 172, 3_000_000
+    assert n * width > 1 << 31
+    print(f"[routes] cache write and gather {n} x {width} bf16", flush=True)
+    torch.manual_seed(4)
+    src = torch.randn(n, 1, width, dtype=torch.bfloat16, device="cuda")
+    ids = torch.arange(n, device="cuda") % (rows + 7)            # seven without a row; the last of a slot stays
+    stride = fast.fast_cache_row_bytes(1, width, fast.MXFP4)
+    cache = torch.zeros(rows, stride, dtype=torch.uint8, device="cuda")
+    wsb = fast.fast_cache_write_workspace(n, rows)
+    ws = torch.empty(wsb, dtype=torch.uint8, device="cuda")
+    fast.fast_cache_write(ids, n, rows, None, 1, width, fast.BF16, src, fast.MXFP4, cache, rows, False, ws, wsb)
+    at = some_rows(rows, 7)
+    last = (n - 1 - at) // (rows + 7) * (rows + 7) + at
+    assert int(last.max()) * width > 1 << 31
+    c, s = p64.quantize(host(src[last]), 4)
+    np.testing.assert_array_equal(cache[at].cpu().numpy(), p64.pack(c, s, 4))
+    src.fill_(7.0)
+    fast.fast_cache_gather(ids, n, rows, None, 1, width, fast.MXFP4, cache, rows, fast.BF16, src)
+    np.testing.assert_array_equal(host(src[at]), p64.values(c, s, 4))
+    np.testing.assert_array_equal(host(src[last]), p64.values(c, s, 4))
+    assert (src[rows:rows + 7] == 7).all()
+
+
 @pytest.mark.parametrize("fmt", [8, 4])
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 @pytest.mark.parametrize("width", [172, 43])
