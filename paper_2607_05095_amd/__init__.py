@@ -207,27 +207,28 @@ def _rows_as_said(t, F, ld):
                            f"are not {F} elements side by side, {ld} apart")
 
 
-def _resident(dense=(), strided=()):
-    """Tensors of a call live on the current device, and those without a row
-    stride of their own are contiguous; raises otherwise."""
+def _resident(dense=(), rows=(), F=0):
+    """Tensors of a call live on the current device, and are contiguous or, as (tensor, stride) in
+    `rows`, views of rows of F elements that far apart; raises otherwise."""
     import torch
     dev = None
-    for t in (*dense, *strided):
+    for t in dense:
         if t is None or isinstance(t, int):
             continue
         if dev is None and t.is_cuda:
             dev = torch.cuda.current_device()
         if t.get_device() != dev:
             raise FastError(1, f"tensor on {t.device}, not on the current GPU")
-    for t in dense:
-        if t is not None and not isinstance(t, int) and not t.is_contiguous():
+        if not t.is_contiguous():
             raise FastError(1, f"tensor of shape {tuple(t.shape)} is not contiguous")
-
-
-def _strided(F, x, ldx, y, ldy):
-    for t, ld in ((x, ldx), (y, ldy)):
-        # contiguous tensors hold rows of any stride
-        if t is not None and not isinstance(t, int) and not t.is_contiguous():
+    for t, ld in rows:
+        if t is None or isinstance(t, int):
+            continue
+        if dev is None and t.is_cuda:
+            dev = torch.cuda.current_device()
+        if t.get_device() != dev:
+            raise FastError(1, f"tensor on {t.device}, not on the current GPU")
+        if not t.is_contiguous():        # contiguous tensors hold rows of any stride
             _rows_as_said(t, F, ld)
 
 
@@ -522,8 +523,7 @@ def fast_layer_norm_bwd(n, D, dtype, h, gamma, mean, rstd, dy, dsum, dx, dgamma,
 def fast_rotary_fwd(n, H, dh, dtype, x, ldx, pos, axes, axis, omega, pairs, interleaved, y, ldy,
                     stream=None):
     """x and y may be views whose rows are ldx and ldy elements apart."""
-    _resident((pos, axis, omega), (x, y))
-    _strided(H * dh, x, ldx, y, ldy)
+    _resident((pos, axis, omega), ((x, ldx), (y, ldy)), H * dh)
     _check(lib().fast_rotary_fwd(n, H, dh, dtype, _ptr(x), ldx, _ptr(pos), axes, _ptr(axis),
                                  _ptr(omega), pairs, int(interleaved), _ptr(y), ldy,
                                  _stream(stream)))
@@ -531,8 +531,7 @@ def fast_rotary_fwd(n, H, dh, dtype, x, ldx, pos, axes, axis, omega, pairs, inte
 
 def fast_rotary_bwd(n, H, dh, dtype, dy, lddy, pos, axes, axis, omega, pairs, interleaved, dx, lddx,
                     stream=None):
-    _resident((pos, axis, omega), (dy, dx))
-    _strided(H * dh, dy, lddy, dx, lddx)
+    _resident((pos, axis, omega), ((dy, lddy), (dx, lddx)), H * dh)
     _check(lib().fast_rotary_bwd(n, H, dh, dtype, _ptr(dy), lddy, _ptr(pos), axes, _ptr(axis),
                                  _ptr(omega), pairs, int(interleaved), _ptr(dx), lddx,
                                  _stream(stream)))
