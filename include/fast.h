@@ -578,7 +578,8 @@ fast_status_t fast_layer_norm_bwd(int64_t n, int D, fast_dtype_t dtype, const vo
  * 2 * pairs on are copied.
  * x, y: rows of [H, dh] of dtype, ldx and ldy elements apart (>= H*dh: the K
  * half of packed K|V rows has ldx = 2*H*dh).  y may be x with ldy = ldx; any
- * other overlap of their elements is refused.  pos: [n, axes] fp32 (event
+ * other overlap of their elements is refused, and with ldy != ldx any of the
+ * spans of their rows.  pos: [n, axes] fp32 (event
  * times, ranks, coordinates); axis: [pairs] int32, NULL for all 0, values
  * outside [0, axes) read the nearest axis; omega: [pairs] fp32.  The angle is
  * exact in fp64, its sine and cosine are within 2e-7 at any position; a position that
@@ -661,7 +662,7 @@ fast_status_t fast_cache_gather(const int64_t* ids, int64_t n, int64_t id_bound,
  * Q, out: [N, H, dh] of dtype; ids: [E] int64 (g->edge_ids, or src_ids where
  * rows belong to nodes); slot_map, cache: as in fast_cache_write.  Reads
  * g->dst_offsets.  Segments of any length: long ones are cut into pieces that
- * a second launch joins in their order (repeated calls give the same bits).
+ * the call's last launch joins in their order (repeated calls give the same bits).
  * Limits: H <= 64, dh <= 256, H*dh <= 1024.
  * Workspace: fast_edge_attention_cached_workspace(N, E, H, dh) bytes (never 0 for valid
  * sizes), 16-byte aligned; one for the largest N and E serves smaller blocks.

@@ -8,7 +8,8 @@
 // hold a record's heads, 16 (or 8) codes of K and of V each; CA_ROWS records per lane
 // are in flight.  A running maximum, sum and accumulators in base 2 make one pass.
 // 264,000 segments of 2.4 M edges, 8 bits, 2 x 50 fp32: 153 us for the first launch, 6.9 TB/s of the
-// lines it touches (a record two, a slot of an 8 MB map one), 162 with the other two.
+// lines it touches (a record of a 272 MB cache two, a slot of an 8 MB map one), 162 with the other
+// two; 226 on a cache of 4.3 GB with a map of 800 MB, 176 without a map.
 //
 // Where there are many short segments, L lanes own one and walk its edges: no
 // joins.  Where segments are longer, or too few to fill the chip that way, a wave
@@ -634,6 +635,11 @@ static size_t ca_part_bytes(int64_t cells, int H, int dh) {
   return align_up(size_t(2 * cells) * H * (dh + 2) * sizeof(float), 16);
 }
 
+// Lanes per head known to the compiler and 32-bit record addresses where a cache is below 4 GiB
+// and heads have 17 to 128 elements; else one kernel that reads the lanes from the arguments and
+// addresses records in 64 bits.  The former / the latter on a cache just below 4 GiB, with a map of
+// 200,000,000 ids, 264,000 segments of 2.4 M edges: 2 x 50 fp32 8 bits 226 / 252 us, 4 x 32
+// bf16 4 bits 208 / 235 (5.4 GB, by the latter: 253 and 236); without a map 176 / 204, 156 / 188.
 template <typename T, int FMT>
 static void launch_ca(const CaArgs& a, const CaPlan& p, bool big, dim3 grid, dim3 long_grid, hipStream_t st) {
 #define FAST_CAK(K, g) hipLaunchKernelGGL(K, g, dim3(CA_THREADS), 0, st, a)
