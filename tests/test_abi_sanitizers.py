@@ -46,6 +46,17 @@ def test_boundary_suite_passes_under_asan_and_ubsan(sanitized):
     assert " passed" in r.stdout, tail
 
 
+def test_layer_boundary_suites_pass_under_asan_and_ubsan(sanitized):
+    """Sizes up to their limits among them, whose products overflow where they are formed too narrowly."""
+    _, env = sanitized
+    r = _child(env, ["-m", "pytest", "-q", "-x", "-p", "no:cacheprovider", "-m", "not gpu"] +
+               [os.path.join(ROOT, "tests", f) for f in ("test_layer_abi.py", "test_layer_refusals.py")])
+    tail = (r.stdout + r.stderr)[-4000:]
+    assert r.returncode == 0, tail
+    assert "AddressSanitizer" not in r.stderr and "runtime error" not in r.stderr, tail
+    assert " passed" in r.stdout, tail
+
+
 def test_sanitized_build_catches_a_short_host_array(sanitized):
     """The instrumentation is live: a caller that declares one more layer
     block than its host array of block sizes holds makes the library read
