@@ -122,6 +122,10 @@ def _sizes(case):
     return size
 
 
+def _act_of(fast, kind):
+    return {"none": fast.ACT_NONE, "relu": fast.ACT_RELU, "gelu": fast.ACT_GELU, "silu": fast.ACT_SILU}[kind]
+
+
 def prepare(case, seed):
     g = _gen(seed)
     s = dict(case)
@@ -143,7 +147,8 @@ def prepare(case, seed):
             s["pre"] = torch.empty_like(s["z"]) if s["z"] is not None else None
             if case["train"]:
                 s["dx"], s["dw"], s["db"] = new(n, K, t=dt), new(M, K), new(M)
-                s["wsb"] = fast.fast_linear_bwd_workspace(n, K, M)
+                s["wsb"] = fast.fast_linear_bwd_workspace(
+                    n, K, M, fast.F32 if case["dtype"] == "f32" else fast.BF16, _act_of(fast, case["act"]))
                 s["ws"] = new(max(s["wsb"], 16), t=torch.uint8)
     elif op == "scan":
         N, E, D, dt = case["N"], case["E"], case["D"], _T[case["dtype"]]
@@ -411,7 +416,7 @@ def run(s):
     import paper_2607_05095_amd as fast
     if op == "linear":
         n, K, M, dt = s["n"], s["K"], s["M"], fast.F32 if s["dtype"] == "f32" else fast.BF16
-        act = {"none": fast.ACT_NONE, "relu": fast.ACT_RELU, "gelu": fast.ACT_GELU, "silu": fast.ACT_SILU}[s["act"]]
+        act = _act_of(fast, s["act"])
         fast.fast_linear_fwd(n, K, M, dt, s["x"], K, s["w"], s["b"], act, s["r"], M, s["y"], M, s["pre"])
         if not s["train"]:
             return (s["y"],)
