@@ -22,6 +22,9 @@
  *   fast_rotary_fwd/bwd       rotary positions of queries and keys, several axes
  *   fast_cache_write, fast_cache_gather  cached rows in 8 or 4 bits   (Sec. 4.2)
  *   fast_edge_attention_fwd_cached   ESM and AGG over K|V rows of such a cache
+ *   fast_linear_fwd/bwd       products of rows with weights: projections and updates
+ *   fast_gated_scan_fwd/bwd   gated recurrence over a segment's events (node memory)
+ *   fast_adamw, fast_grad_norm  the step over all weights, the norm that clips it
  *
  * Conventions shared by every entry point
  *   - Memory: every array argument is a DEVICE pointer into HBM owned by the
@@ -676,6 +679,160 @@ fast_status_t fast_edge_attention_fwd_cached(const fast_tcsr_t* g, int H, int dh
                                              int64_t cache_rows, float scale, float neg_slope,
                                              void* out, float* lse, void* ws, size_t ws_bytes,
                                              fast_stream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Products of rows with weights (the projections that make Q, K|V, gates and the
+ * update of Eq. 1 out of rows), with bias, activation and residual in the epilogue.
+ *   z = x w^T + bias
+ *   y = act(z) + res,  pre = z   (each rounded once)
+ * FAST_ACT_NONE: z; FAST_ACT_RELU: max(z, 0) (slope 0 at 0); FAST_ACT_GELU: z Phi(z),
+ * Phi the normal distribution function; FAST_ACT_SILU: z / (1 + exp(-z)).
+ * x: rows of `in` elements of dtype, ldx apart; w: [out, in] of dtype; bias: [out]
+ * fp32, NULL for none; res, y: rows of `out` elements of dtype, ldres and ldy apart
+ * (res NULL for none); pre: [n, out] of dtype, optional, only with an activation.
+ * y may be res with ldy = ldres; y and pre lie apart from every other array
+ * (spans of their rows that meet are refused).  Products of dtype's values are exact
+ * or rounded to fp32, sums fp32.  Whatever n, ldx and the alignment, a row's result does
+ * not depend on the other rows' values.
+ * Limits: in, out <= 16384, n and the strides < 2^31, rows that span less than 2^56
+ * elements, and fewer than 2^32 threads.
+ * ------------------------------------------------------------------------ */
+typedef enum {
+  FAST_ACT_NONE = 0,
+  FAST_ACT_RELU = 1,
+  FAST_ACT_GELU = 2,
+  FAST_ACT_SILU = 3,
+  FAST_ACT_MAX_ENUM = 0x7fffffff /* as FAST_DTYPE_MAX_ENUM */
+} fast_act_t;
+
+fast_status_t fast_linear_fwd(int64_t n, int in, int out, fast_dtype_t dtype, const void* x,
+                              int64_t ldx, const void* w, const float* bias, fast_act_t act,
+                              const void* res, int64_t ldres, void* y, int64_t ldy, void* pre,
+                              fast_stream_t stream);
+
+/* Backward for dy (rows of `out` elements of dtype, lddy apart):
+ *   dz = dy act'(pre)
+ *   dx = dz w,  dw = dz^T x,  dbias = sum over rows of dz      (dres is dy)
+ * pre: the forward's (needed with an activation, refused without).  dx: rows of `in`
+ * elements of dtype, lddx apart, apart from every input; dw: [out, in] fp32, dbias:
+ * [out] fp32, both overwritten (zeros when n = 0); each of the three may be NULL, w
+ * where dx is, x where dw is.  Sums over rows: fp32 over a few thousand rows, fp64
+ * beyond, in a fixed order (repeated calls give the same bits).
+ * Workspace: fast_linear_bwd_workspace(n, in, out, dtype, act) bytes, 256-byte aligned;
+ * one for the largest n serves smaller ones. */
+size_t fast_linear_bwd_workspace(int64_t n, int in, int out, fast_dtype_t dtype, fast_act_t act);
+fast_status_t fast_linear_bwd(int64_t n, int in, int out, fast_dtype_t dtype, const void* x,
+                              int64_t ldx, const void* w, fast_act_t act, const void* pre,
+                              const void* dy, int64_t lddy, void* dx, int64_t lddx, float* dw,
+                              float* dbias, void* ws, size_t ws_bytes, fast_stream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Gated linear recurrence over the events of each segment, in their order: a memory
+ * row that decays towards every event's row at a rate of its own, over the time since
+ * the event before (the trained memory of temporal models; Eq. 1's aggregation without
+ * a softmax).  For event e of segment v, element by element of a row of D:
+ *   rate = log(1 + exp(gate[e])),  a = exp(-rate dt[e]),  u = 1 - a
+ *   s = a s + u x[e],  h[e] = s          from s = h0[v] (0 where h0 is NULL)
+ * dt NULL: 1 for every event, so that u is the sigmoid of the gate.  h_last[v]: s
+ * after the last event (h0[v] for an empty segment).
+ * x, gate: rows of D elements of dtype, both ldx apart (x and gate side by side, as one
+ * product writes them: ldx = 2 D); dt: [E] fp32, times since the event before, >= 0 (a
+ * negative one counts as 0); h0, h_last: [N, D] fp32, each optional, h_last may be h0;
+ * h: [E, D] of dtype, optional.  s is fp32.  Reads g->dst_offsets.
+ * states: what a backward reads: fp32 [fast_gated_scan_state_rows(E), D], s before some
+ * of the events (rows that it does not need stay as they were); NULL without a backward.
+ * longest: a length that no segment exceeds, 0 where none is known.  It only chooses
+ * launches: short segments then need fewer; a longer segment is right all the same.
+ * Outputs lie apart from the inputs and each other (but h_last and h0).
+ * Limits: D <= 8192, ldx < 2^31, rows that span less than 2^56 elements, N, E < 2^31,
+ * fewer than 2^32 threads.  Repeated calls give the same bits.
+ * Workspace: fast_gated_scan_workspace(N, E, D) bytes, 256-byte aligned; one for the
+ * largest N, E serves smaller blocks of the same D.
+ * ------------------------------------------------------------------------ */
+int64_t fast_gated_scan_state_rows(int64_t num_edges);
+size_t fast_gated_scan_workspace(int64_t num_dst, int64_t num_edges, int D);
+fast_status_t fast_gated_scan_fwd(const fast_tcsr_t* g, int D, fast_dtype_t dtype, const void* x,
+                                  const void* gate, int64_t ldx, const float* dt,
+                                  const float* h0, int64_t longest, void* h, float* h_last,
+                                  float* states, void* ws, size_t ws_bytes, fast_stream_t stream);
+
+/* Backward for dh ([E, D] of dtype) and dh_last ([N, D] fp32), each optional (NULL: 0):
+ *   d = dh[e] + (a d of the event behind, dh_last[v] at the last one)
+ *   dx = u d,  dgate = d (x - s before) a dt sigmoid(gate),  dh0[v] = a d of the first
+ * event (dh_last[v] for an empty segment).  dt is a constant.  x, gate, ldx, dt, h0: the
+ * forward's; states: as the forward wrote it.  dx, dgate: rows of D elements of dtype,
+ * lddx apart; dh0: [N, D] fp32, optional, may be dh_last.  s is taken in fp32 from
+ * states, not from the rounded h.  Limits and workspace as the forward's. */
+fast_status_t fast_gated_scan_bwd(const fast_tcsr_t* g, int D, fast_dtype_t dtype, const void* x,
+                                  const void* gate, int64_t ldx, const float* dt,
+                                  const float* h0, int64_t longest, const float* states,
+                                  const void* dh, const float* dh_last, void* dx, void* dgate,
+                                  int64_t lddx, float* dh0, void* ws, size_t ws_bytes,
+                                  fast_stream_t stream);
+
+/* ------------------------------------------------------------------------
+ * The step that ends a training step: AdamW over many tensors at once (the weight
+ * gradients of the products, the norm, the time encoding, the row sums).
+ *   g = scale grad,  m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2
+ *   w = w - lr (decay w + (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps))
+ * t: the number of this step, 1 for the first.
+ * tensors: a HOST array of `count` descriptors, copied during the call.  A tensor: n
+ * elements of w (fp32), grad (of grad_dtype), the states, and, where `copy` is not
+ * NULL, the weights rounded to bf16 for the products that read them (written only).
+ *   FAST_STATE_F32: m, v fp32 [n]; m_scale, v_scale NULL
+ *   FAST_STATE_MXFP8: m, and the square root of v, in 8 bits: groups of 32 elements of
+ *     the tensor; a byte m_scale[group] = k + 127 (k >= -127 the smallest for which the
+ *     group's largest magnitude is at most 448 * 2^k; 255 and codes 0: the group holds an
+ *     infinity or a NaN, and reads back as NaN) and a code of e4m3 per element, its value
+ *     times 2^k.  Between two codes the upper (in magnitude) is taken where the fraction
+ *     above the lower is more than the element's random number / 65536, so that what a step
+ *     adds is kept in the mean however small; a square root that is not 0 is never rounded
+ *     to 0 (the step would divide by eps).  The random number of element i of tensor j is
+ *     the low (m) or high (v) half of
+ *       mix(mix(mix(mix(seed ^ t * 0x9E3779B9) ^ j) + (i >> 32) * 0x9E3779B9) ^ i)
+ *     in 32 bits, mix(x): x ^= x >> 16, x *= 0x6A09E667, x ^= x >> 15, x *= 0xBB67AE85,
+ *     x ^= x >> 16.  m and v are formed in fp64 and rounded to fp32 (v's root) before that.
+ *     All-zero bytes are zeros.
+ * lr, t: *lr_dev and *step_dev (device) in place of lr and step where not NULL, for a
+ * captured step.  scale: device, NULL for 1; where it is not finite the call leaves
+ * weights and states as they are.  grad_scale [1] of fast_grad_norm is one.
+ * Arrays that the call writes and that overlap each other or a grad are refused.
+ * Limits: count <= 1024, n < 2^40 each, t >= 1; alignment: each array's element.
+ * ------------------------------------------------------------------------ */
+typedef enum {
+  FAST_STATE_F32 = 0,
+  FAST_STATE_MXFP8 = 1,
+  FAST_STATE_MAX_ENUM = 0x7fffffff /* as FAST_DTYPE_MAX_ENUM */
+} fast_state_format_t;
+
+typedef struct {
+  float* w;
+  const void* grad;
+  void* m;
+  void* v;
+  uint8_t* m_scale;
+  uint8_t* v_scale;
+  uint16_t* copy;
+  int64_t n;
+  float decay;
+} fast_adamw_tensor_t;
+
+fast_status_t fast_adamw(const fast_adamw_tensor_t* tensors, int count, fast_dtype_t grad_dtype,
+                         fast_state_format_t format, double lr, double beta1, double beta2,
+                         double eps, int64_t step, uint32_t seed, const float* lr_dev,
+                         const int64_t* step_dev, const float* scale, fast_stream_t stream);
+
+/* The norm of all gradients of the list (its grad and n; the rest is not read) and the
+ * factor that clips them:
+ *   norm = sqrt(sum grad^2) (squares and sums in fp64, in a fixed order)
+ *   scale = max_norm / norm where norm > max_norm, else 1; NaN where norm is not finite
+ * norm, scale: [1] fp32 device, scale optional.  max_norm > 0 (infinity: never clips).
+ * Workspace: fast_grad_norm_workspace(total elements, count) bytes, 8-byte aligned; one
+ * for the largest list serves smaller ones. */
+size_t fast_grad_norm_workspace(int64_t total, int count);
+fast_status_t fast_grad_norm(const fast_adamw_tensor_t* tensors, int count,
+                             fast_dtype_t grad_dtype, float max_norm, float* norm, float* scale,
+                             void* ws, size_t ws_bytes, fast_stream_t stream);
 
 #ifdef __cplusplus
 }

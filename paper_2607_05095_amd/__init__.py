@@ -36,6 +36,10 @@ __all__ = [
     "fast_rotary_fwd", "fast_rotary_bwd", "MXFP8", "MXFP4", "fast_cache_row_bytes",
     "fast_cache_write_workspace", "fast_cache_write", "fast_cache_gather",
     "fast_edge_attention_cached_workspace", "fast_edge_attention_fwd_cached",
+    "ACT_NONE", "ACT_RELU", "ACT_GELU", "ACT_SILU", "fast_linear_fwd", "fast_linear_bwd_workspace",
+    "fast_linear_bwd", "fast_gated_scan_state_rows", "fast_gated_scan_workspace",
+    "fast_gated_scan_fwd", "fast_gated_scan_bwd", "STATE_F32", "STATE_MXFP8", "AdamWTensor",
+    "adamw_tensors", "fast_adamw", "fast_grad_norm_workspace", "fast_grad_norm",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -45,6 +49,8 @@ LIB_PATH = os.environ.get("FAST_LIB") or os.path.join(_HERE, "libfast.so")
 
 F32, BF16 = 0, 1
 MXFP8, MXFP4 = 0, 1   # fast_cache_format_t
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU = 0, 1, 2, 3   # fast_act_t
+STATE_F32, STATE_MXFP8 = 0, 1   # fast_state_format_t
 NOALLOC_SCRATCH_BYTES = 128 << 20   # FAST_NOALLOC_SCRATCH_BYTES of include/fast.h
 _STATUS = {0: "FAST_OK", 1: "FAST_ERR_INVALID_ARG", 2: "FAST_ERR_UNSUPPORTED",
            3: "FAST_ERR_WORKSPACE", 4: "FAST_ERR_HIP"}
@@ -81,7 +87,23 @@ class TemporalGraphDesc(C.Structure):
     ]
 
 
+class AdamWTensor(C.Structure):
+    """fast_adamw_tensor_t: one tensor of an AdamW step (device pointers)."""
+    _fields_ = [
+        ("w", C.c_void_p),
+        ("grad", C.c_void_p),
+        ("m", C.c_void_p),
+        ("v", C.c_void_p),
+        ("m_scale", C.c_void_p),
+        ("v_scale", C.c_void_p),
+        ("copy", C.c_void_p),
+        ("n", C.c_int64),
+        ("decay", C.c_float),
+    ]
+
+
 _p, _i64, _i32, _f32, _sz = C.c_void_p, C.c_int64, C.c_int, C.c_float, C.c_size_t
+_f64 = C.c_double
 _G = C.POINTER(TCSR)
 _TG = C.POINTER(TemporalGraphDesc)
 _SIGS = {
@@ -148,6 +170,21 @@ _SIGS = {
     "fast_edge_attention_cached_workspace": (_sz, [_i64, _i64, _i32, _i32]),
     "fast_edge_attention_fwd_cached": (_i32, [_G, _i32, _i32, _i32, _p, _p, _i64, _p, _i32, _p,
                                               _i64, _f32, _f32, _p, _p, _p, _sz, _p]),
+    "fast_linear_fwd": (_i32, [_i64, _i32, _i32, _i32, _p, _i64, _p, _p, _i32, _p, _i64, _p, _i64, _p,
+                               _p]),
+    "fast_linear_bwd_workspace": (_sz, [_i64, _i32, _i32, _i32, _i32]),
+    "fast_linear_bwd": (_i32, [_i64, _i32, _i32, _i32, _p, _i64, _p, _i32, _p, _p, _i64, _p, _i64, _p,
+                               _p, _p, _sz, _p]),
+    "fast_gated_scan_state_rows": (_i64, [_i64]),
+    "fast_gated_scan_workspace": (_sz, [_i64, _i64, _i32]),
+    "fast_gated_scan_fwd": (_i32, [_G, _i32, _i32, _p, _p, _i64, _p, _p, _i64, _p, _p, _p, _p, _sz,
+                                   _p]),
+    "fast_gated_scan_bwd": (_i32, [_G, _i32, _i32, _p, _p, _i64, _p, _p, _i64, _p, _p, _p, _p, _p,
+                                   _i64, _p, _p, _sz, _p]),
+    "fast_adamw": (_i32, [_p, _i32, _i32, _i32, _f64, _f64, _f64, _f64, _i64, C.c_uint32, _p, _p, _p,
+                          _p]),
+    "fast_grad_norm_workspace": (_sz, [_i64, _i32]),
+    "fast_grad_norm": (_i32, [_p, _i32, _i32, _f32, _p, _p, _p, _sz, _p]),
 }
 
 _lib = None
@@ -572,3 +609,98 @@ def fast_edge_attention_fwd_cached(g: TCSR, H, dh, dtype, Q, ids, id_bound, slot
                                                 id_bound, _ptr(slot_map), format, _ptr(cache),
                                                 cache_rows, scale, neg_slope, _ptr(out),
                                                 _ptr(lse), _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def fast_linear_fwd(n, in_, out, dtype, x, ldx, w, bias, act, res, ldres, y, ldy, pre=None, stream=None):
+    """x, res and y may be views whose rows are ldx, ldres and ldy elements apart."""
+    _resident((w, bias, pre), ((x, ldx),), in_)
+    _resident((), ((res, ldres), (y, ldy)), out)
+    _check(lib().fast_linear_fwd(n, in_, out, dtype, _ptr(x), ldx, _ptr(w), _ptr(bias), act, _ptr(res),
+                                 ldres, _ptr(y), ldy, _ptr(pre), _stream(stream)))
+
+
+def fast_linear_bwd_workspace(n: int, in_: int, out: int, dtype: int, act: int) -> int:
+    return lib().fast_linear_bwd_workspace(n, in_, out, dtype, act)
+
+
+def fast_linear_bwd(n, in_, out, dtype, x, ldx, w, act, pre, dy, lddy, dx, lddx, dw, dbias, ws,
+                    ws_bytes, stream=None):
+    _resident((w, pre, dw, dbias, ws), ((x, ldx), (dx, lddx)), in_)
+    _resident((), ((dy, lddy),), out)
+    _check(lib().fast_linear_bwd(n, in_, out, dtype, _ptr(x), ldx, _ptr(w), act, _ptr(pre), _ptr(dy),
+                                 lddy, _ptr(dx), lddx, _ptr(dw), _ptr(dbias), _ptr(ws), ws_bytes,
+                                 _stream(stream)))
+
+
+def fast_gated_scan_state_rows(num_edges: int) -> int:
+    return lib().fast_gated_scan_state_rows(num_edges)
+
+
+def fast_gated_scan_workspace(num_dst: int, num_edges: int, D: int) -> int:
+    return lib().fast_gated_scan_workspace(num_dst, num_edges, D)
+
+
+def fast_gated_scan_fwd(g: TCSR, D, dtype, x, gate, ldx, dt, h0, longest, h, h_last, states, ws,
+                        ws_bytes, stream=None):
+    """x and gate may be views whose rows are ldx elements apart."""
+    _resident((*getattr(g, "_keep", ())[:1], dt, h0, h, h_last, states, ws), ((x, ldx), (gate, ldx)), D)
+    _check(lib().fast_gated_scan_fwd(C.byref(g), D, dtype, _ptr(x), _ptr(gate), ldx, _ptr(dt),
+                                     _ptr(h0), longest, _ptr(h), _ptr(h_last), _ptr(states), _ptr(ws),
+                                     ws_bytes, _stream(stream)))
+
+
+def fast_gated_scan_bwd(g: TCSR, D, dtype, x, gate, ldx, dt, h0, longest, states, dh, dh_last, dx,
+                        dgate, lddx, dh0, ws, ws_bytes, stream=None):
+    _resident((*getattr(g, "_keep", ())[:1], dt, h0, states, dh, dh_last, dh0, ws),
+              ((x, ldx), (gate, ldx), (dx, lddx), (dgate, lddx)), D)
+    _check(lib().fast_gated_scan_bwd(C.byref(g), D, dtype, _ptr(x), _ptr(gate), ldx, _ptr(dt),
+                                     _ptr(h0), longest, _ptr(states), _ptr(dh), _ptr(dh_last),
+                                     _ptr(dx), _ptr(dgate), lddx, _ptr(dh0), _ptr(ws), ws_bytes,
+                                     _stream(stream)))
+
+
+def adamw_tensors(w, grad, m, v, m_scale=None, v_scale=None, copy=None, decay=None):
+    """Builds the host array of fast_adamw_tensor_t over lists of device tensors, one entry per
+    tensor (m_scale, v_scale, copy: None, or lists; decay: a number, a list, or None for 0).  Built once
+    and passed to every step; it keeps a reference to each tensor."""
+    n = len(w)
+    lists = [w, grad, m, v, m_scale, v_scale, copy]
+    for k, x in enumerate(lists):
+        if x is None and k >= 4:
+            lists[k] = [None] * n
+        elif x is None or len(x) != n:
+            raise ValueError("one entry per tensor")
+    if decay is None or isinstance(decay, (int, float)):
+        decay = [float(decay or 0)] * n
+    elif len(decay) != n:
+        raise ValueError("one decay per tensor")
+    a = (AdamWTensor * max(n, 1))()
+    for j, ts in enumerate(zip(*lists)):
+        size = ts[0].numel()
+        for t, want in zip(ts, (size, size, size, size, (size + 31) // 32, (size + 31) // 32, size)):
+            if t is not None and t.numel() != want:
+                raise FastError(1, f"tensor {j}: an array of {t.numel()} elements, {want} wanted")
+        a[j] = AdamWTensor(*[_ptr(t) for t in ts], size, decay[j])
+    a._keep = tuple(t for x in lists for t in x if t is not None)
+    a._count = n
+    _resident(a._keep)
+    return a
+
+
+def fast_adamw(tensors, grad_dtype, format, lr, beta1, beta2, eps, step, seed=0, lr_dev=None,
+               step_dev=None, scale=None, stream=None):
+    """tensors: from adamw_tensors."""
+    _resident((*tensors._keep[:1], lr_dev, step_dev, scale))
+    _check(lib().fast_adamw(tensors, tensors._count, grad_dtype, format, lr, beta1, beta2, eps, step,
+                            seed, _ptr(lr_dev), _ptr(step_dev), _ptr(scale), _stream(stream)))
+
+
+def fast_grad_norm_workspace(total: int, count: int) -> int:
+    return lib().fast_grad_norm_workspace(total, count)
+
+
+def fast_grad_norm(tensors, grad_dtype, max_norm, norm, scale, ws, ws_bytes, stream=None):
+    """tensors: from adamw_tensors."""
+    _resident((*tensors._keep[:1], norm, scale, ws))
+    _check(lib().fast_grad_norm(tensors, tensors._count, grad_dtype, max_norm, _ptr(norm), _ptr(scale),
+                                _ptr(ws), ws_bytes, _stream(stream)))

@@ -168,20 +168,6 @@ __global__ void __launch_bounds__(ROT_THREADS) k_rotary(RotArgs a) {
   }
 }
 
-// Do the elements of rows of F elements, ldx and ldy apart, overlap other than
-// element on element?
-static bool rows_collide(const char* x, int64_t ldx, const char* y, int64_t ldy, int64_t n, int64_t F,
-                         int64_t es) {
-  const char* xe = x + ((n - 1) * ldx + F) * es;
-  const char* ye = y + ((n - 1) * ldy + F) * es;
-  if (x >= ye || y >= xe) return false;
-  if (ldx != ldy) return true;
-  if (x == y) return false;
-  // the same distance apart in every row: disjoint where one lies in the other's gap
-  const int64_t d = (y > x ? y - x : x - y) % (ldx * es);
-  return d < F * es || ldx * es - d < F * es;
-}
-
 static fast_status_t rotary(const char* fn, int64_t n, int H, int dh, fast_dtype_t dtype, const void* x,
                             int64_t ldx, const float* pos, int axes, const int32_t* axis,
                             const float* omega, int pairs, int interleaved, void* y, int64_t ldy,

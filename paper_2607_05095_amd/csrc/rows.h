@@ -113,6 +113,29 @@ inline bool shifted(const void* a, const void* b, int64_t bytes) {
   return (p > q ? p - q : q - p) < uint64_t(bytes);
 }
 
+// Do the elements of rows of F elements, ldx and ldy apart, overlap other than
+// element on element?
+inline bool rows_collide(const char* x, int64_t ldx, const char* y, int64_t ldy, int64_t n, int64_t F,
+                         int64_t es) {
+  const char* xe = x + ((n - 1) * ldx + F) * es;
+  const char* ye = y + ((n - 1) * ldy + F) * es;
+  if (x >= ye || y >= xe) return false;
+  if (ldx != ldy) return true;
+  if (x == y) return false;
+  // the same distance apart in every row: disjoint where one lies in the other's gap
+  const int64_t d = (y > x ? y - x : x - y) % (ldx * es);
+  return d < F * es || ldx * es - d < F * es;
+}
+
+// Do p bytes at a and q at b meet?  NULL: no array.
+inline bool meet(const void* a, int64_t p, const void* b, int64_t q) {
+  if (!a || !b || p <= 0 || q <= 0) return false;
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y ? y - x < uint64_t(p) : x - y < uint64_t(q);
+}
+// Bytes from the first to the last element of n rows of F elements, ld apart.
+inline int64_t span(int64_t n, int64_t F, int64_t ld, int64_t es) { return n > 0 ? ((n - 1) * ld + F) * es : 0; }
+
 // A launch has fewer than 2^32 threads along an axis.
 inline bool grid_fits(int64_t blocks, int64_t threads) { return blocks * threads < (int64_t(1) << 32); }
 
