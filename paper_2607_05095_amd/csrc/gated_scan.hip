@@ -23,9 +23,9 @@
 
 namespace fast {
 
-constexpr int GS_THREADS = 256;
+constexpr int GS_THREADS = 256, GS_WAVES = GS_THREADS / 64;
 constexpr int GS_AHEAD = 8;          // events whose rows are loaded together
-constexpr int GS_WIN = 16;           // events of a backward window
+constexpr int GS_WIN = 8;            // events of a backward window
 constexpr int64_t GS_MAX_D = 8192;
 constexpr int GS_CARRY = 16;         // pieces whose sums are loaded together
 
@@ -42,53 +42,44 @@ __device__ __forceinline__ float exp_neg(float x, float up = 0.f) {
   return h + up < -126.f ? e : fmaf(e, l * 0x1.62e43p-1f, e);
 }
 
-// 1 / x, x >= 1 (or not a number).
-__device__ __forceinline__ float rcp(float x) {
-  const float r = __builtin_amdgcn_rcpf(x);
-  return fmaf(fmaf(-x, r, 1.f), r, r);
-}
-
 // u = 1 - a keeps its relative accuracy for slow gates and a for fast ones.
 template <bool SPAN>
 __device__ __forceinline__ Gate gate_of(float g, float dt) {
   Gate q;
   const float t = exp_neg(fabsf(g));                       // sigmoid(|g|) = 1 / (1 + t)
-  const float r = rcp(1.f + t), big = r, small = t * r;
-  const float sig = g >= 0.f ? big : small;
+  const float r = __builtin_amdgcn_rcpf(1.f + t), small = t * r;
+  const float sig = g >= 0.f ? r : small;
   if constexpr (!SPAN) {
-    q.u = g >= 0.f ? big : small;
-    q.a = g >= 0.f ? small : big;
+    q.u = sig;
+    q.a = g >= 0.f ? small : r;
     q.k = q.a * sig;
     return q;
   }
-  // log(1 + t) = 2 artanh(z), z = t / (2 + t) <= 1/3: odd powers up to z^15 (2^-26)
-  const float z = t * rcp(2.f + t), z2 = z * z;
-  float p = 1.f / 15.f;
-  p = fmaf(p, z2, 1.f / 13.f);
-  p = fmaf(p, z2, 1.f / 11.f);
-  p = fmaf(p, z2, 1.f / 9.f);
-  p = fmaf(p, z2, 1.f / 7.f);
-  p = fmaf(p, z2, 1.f / 5.f);
-  p = fmaf(p, z2, 1.f / 3.f);
-  const float rate = fmaf(2.f * z * z2, p, 2.f * z) + (g > 0.f ? g : 0.f);
+  // log(1 + t) / t on (0, 1], within 2^-27 (a weighted least-squares fit)
+  float p = -0x1.a9330cp-9f;
+  p = fmaf(p, t, 0x1.453edcp-6f);
+  p = fmaf(p, t, -0x1.d29c9ap-5f);
+  p = fmaf(p, t, 0x1.b25348p-4f);
+  p = fmaf(p, t, -0x1.39755cp-3f);
+  p = fmaf(p, t, 0x1.92f694p-3f);
+  p = fmaf(p, t, -0x1.ff0f86p-3f);
+  p = fmaf(p, t, 0x1.554c80p-2f);
+  p = fmaf(p, t, -0x1.ffffbep-2f);
+  p = fmaf(p, t, 1.f);
+  const float rate = fmaf(p, t, g > 0.f ? g : 0.f);
   dt = dt < 0.f ? 0.f : dt;
   float y = rate * dt;
   const bool far = g < -86.f;                              // a rate below what fp32 holds, e^gate
   if (far) y = exp_neg(-g, 120.f) * (dt * 0x1p-120f);
-  // 1 - e^-y: its series up to y^10 below log 2 (2^-26), the difference above
-  const float e = exp_neg(y);
-  float s = -1.f / 3628800.f;
-  s = fmaf(s, y, 1.f / 362880.f);
-  s = fmaf(s, y, -1.f / 40320.f);
-  s = fmaf(s, y, 1.f / 5040.f);
-  s = fmaf(s, y, -1.f / 720.f);
-  s = fmaf(s, y, 1.f / 120.f);
-  s = fmaf(s, y, -1.f / 24.f);
-  s = fmaf(s, y, 1.f / 6.f);
-  s = fmaf(s, y, -0.5f);
-  s = fmaf(s * y, y, y);
-  const bool slow = y < 0.693f;
-  q.u = slow ? s : 1.f - e;
+  // (1 - e^-y) / y below log 2, within 2^-26; the difference above
+  const float e = __builtin_amdgcn_exp2f(y * -0x1.715476p+0f);
+  float s = -0x1.0ed322p-10f;
+  s = fmaf(s, y, 0x1.085898p-7f);
+  s = fmaf(s, y, -0x1.548ec0p-5f);
+  s = fmaf(s, y, 0x1.554d38p-3f);
+  s = fmaf(s, y, -0x1.ffffc0p-2f);
+  s = fmaf(s, y, 1.f);
+  q.u = y < 0.6931f ? s * y : 1.f - e;
   q.a = e;
   q.k = far ? e * y : e * dt * sig;
   return q;
@@ -99,6 +90,7 @@ struct GsArgs {
   const int32_t* off;
   int64_t N, E;
   int D, C;                          // columns; lanes of a row
+  int waves;                         // waves that share a piece
   const void* x;
   const void* gate;
   int64_t ldx;
@@ -124,59 +116,63 @@ struct GsArgs {
   uint32_t direct;                   // workgroups of the short segments, before those of the pieces
 };
 
-// VE columns at p, n of them in the row
-template <typename T, int VE>
-__device__ __forceinline__ void gs_load(const T* p, int n, float* x) {
-  if (n >= VE) {
-    if constexpr (VE == 4 && sizeof(T) == 4) {
-      load_chunk_of(p, 4, x);
-    } else if constexpr (VE == 4) {
-      const u32x2_e w = *reinterpret_cast<const u32x2_e*>(p);
-      x[0] = bf16_lo(w.x); x[1] = bf16_hi(w.x); x[2] = bf16_lo(w.y); x[3] = bf16_hi(w.y);
-    } else if constexpr (VE == 2 && sizeof(T) == 4) {
-      const f32x2_e w = *reinterpret_cast<const f32x2_e*>(p);
-      x[0] = w.x; x[1] = w.y;
-    } else if constexpr (VE == 2) {
-      const uint32_t w = *reinterpret_cast<const u32_e*>(p);
-      x[0] = bf16_lo(w); x[1] = bf16_hi(w);
-    } else if constexpr (sizeof(T) == 4) {
-      x[0] = p[0];
-    } else {
-      x[0] = bf16_at(p);
-    }
-    return;
-  }
-#pragma unroll
-  for (int j = 0; j < VE; ++j) {
-    x[j] = 0.f;
-    if (j < n) {
-      if constexpr (sizeof(T) == 4) x[j] = p[j];
-      else x[j] = bf16_at(p + j);
-    }
-  }
+// A lane's columns: VE from `first` on.  In a row that is no multiple of VE the last lane starts
+// early enough to end with the row; it loads VE columns like all others (a branch around a load
+// is a wait for it) and stores those from `skip` on.
+struct Cols {
+  int first, skip;
+};
+template <int VE>
+__device__ __forceinline__ Cols cols_of(int lane, int D) {
+  const int c = lane * VE, f = c + VE > D ? D - VE : c;
+  return Cols{f, c - f};
 }
+
+// VE elements as they lie in memory.
+template <typename T, int VE> struct Lump;
+template <> struct Lump<float, 1> {
+  float v;
+  __device__ void load(const float* p) { v = *p; }
+  __device__ void get(float* x) const { x[0] = v; }
+};
+template <> struct Lump<float, 2> {
+  f32x2_e v;
+  __device__ void load(const float* p) { v = *reinterpret_cast<const f32x2_e*>(p); }
+  __device__ void get(float* x) const { x[0] = v.x; x[1] = v.y; }
+};
+template <> struct Lump<uint16_t, 1> {
+  uint16_t v;
+  __device__ void load(const uint16_t* p) { v = *p; }
+  __device__ void get(float* x) const { x[0] = __uint_as_float(uint32_t(v) << 16); }
+};
+template <> struct Lump<uint16_t, 2> {
+  uint32_t v;
+  __device__ void load(const uint16_t* p) { v = *reinterpret_cast<const u32_e*>(p); }
+  __device__ void get(float* x) const { x[0] = bf16_lo(v); x[1] = bf16_hi(v); }
+};
 template <typename T, int VE>
-__device__ __forceinline__ void gs_store(T* p, int n, const float* x) {
-  if (n >= VE) {
-    if constexpr (VE == 4 && sizeof(T) == 4) store_chunk_of(p, 4, x);
-    else if constexpr (VE == 4) *reinterpret_cast<u32x2_e*>(p) = u32x2_e{bf16_pack(x[0], x[1]), bf16_pack(x[2], x[3])};
-    else if constexpr (VE == 2 && sizeof(T) == 4) *reinterpret_cast<f32x2_e*>(p) = f32x2_e{x[0], x[1]};
-    else if constexpr (VE == 2) *reinterpret_cast<u32_e*>(p) = bf16_pack(x[0], x[1]);
-    else if constexpr (sizeof(T) == 4) p[0] = x[0];
-    else p[0] = uint16_t(bf16_rne(x[0]));
-    return;
+__device__ __forceinline__ void gs_load(const T* p, float* x) {
+  Lump<T, VE> l;
+  l.load(p);
+  l.get(x);
+}
+__device__ __forceinline__ void gs_put(float* p, float x) { *p = x; }
+__device__ __forceinline__ void gs_put(uint16_t* p, float x) { *p = uint16_t(bf16_rne(x)); }
+template <typename T, int VE>
+__device__ __forceinline__ void gs_store(T* p, int skip, const float* x) {
+  if constexpr (VE == 1) {
+    gs_put(p, x[0]);
+  } else {
+    static_assert(VE == 2, "a lane owns one column or two");
+    if (skip) gs_put(p + 1, x[1]);
+    else if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x2_e*>(p) = f32x2_e{x[0], x[1]};
+    else *reinterpret_cast<u32_e*>(p) = bf16_pack(x[0], x[1]);
   }
-#pragma unroll
-  for (int j = 0; j < VE; ++j)
-    if (j < n) {
-      if constexpr (sizeof(T) == 4) p[j] = x[j];
-      else p[j] = uint16_t(bf16_rne(x[j]));
-    }
 }
 template <int VE>
-__device__ __forceinline__ void gs_start(const float* rows, int64_t row, int D, int c, int n, float* s) {
+__device__ __forceinline__ void gs_start(const float* rows, int64_t row, int D, int c, float* s) {
   if (rows) {
-    gs_load<float, VE>(rows + row * D + c, n, s);
+    gs_load<float, VE>(rows + row * D + c, s);
   } else {
 #pragma unroll
     for (int j = 0; j < VE; ++j) s[j] = 0.f;
@@ -185,30 +181,34 @@ __device__ __forceinline__ void gs_start(const float* rows, int64_t row, int D, 
 
 // Events [p, t) of a segment that starts at b, from the state s.
 template <typename T, int VE, bool SPAN>
-__device__ __forceinline__ void fwd_range(const GsArgs& a, int64_t b, int64_t p, int64_t t, int c, int n, float* s) {
-  const T* x = static_cast<const T*>(a.x) + c;
-  const T* g = static_cast<const T*>(a.gate) + c;
+__device__ __forceinline__ void fwd_range(const GsArgs& a, int64_t b, int64_t p, int64_t t, Cols c, float* s) {
+  const T* x = static_cast<const T*>(a.x) + c.first;
+  const T* g = static_cast<const T*>(a.gate) + c.first;
   for (int64_t e = p; e < t; e += GS_AHEAD) {
-    float xs[GS_AHEAD][VE], gs[GS_AHEAD][VE], dt[GS_AHEAD];
+    Lump<T, VE> xs[GS_AHEAD], gs[GS_AHEAD];
+    float dt[GS_AHEAD];
     const int m = t - e < GS_AHEAD ? int(t - e) : GS_AHEAD;
 #pragma unroll
-    for (int j = 0; j < GS_AHEAD; ++j)
-      if (j < m) {
-        gs_load<T, VE>(x + (e + j) * a.ldx, n, xs[j]);
-        gs_load<T, VE>(g + (e + j) * a.ldx, n, gs[j]);
-        dt[j] = SPAN ? a.dt[e + j] : 1.f;
-      }
+    for (int j = 0; j < GS_AHEAD; ++j) {
+      const int64_t i = e + (j < m ? j : m - 1);           // past the end: the last event again
+      xs[j].load(x + i * a.ldx);
+      gs[j].load(g + i * a.ldx);
+      dt[j] = SPAN ? a.dt[i] : 1.f;
+    }
     if (a.states && e > b && ((e - b) & (GS_WIN - 1)) == 0)
-      gs_store<float, VE>(a.states + e / GS_WIN * a.D + c, n, s);
+      gs_store<float, VE>(a.states + e / GS_WIN * a.D + c.first, c.skip, s);
 #pragma unroll
     for (int j = 0; j < GS_AHEAD; ++j)
       if (j < m) {
+        float xv[VE], gv[VE];
+        xs[j].get(xv);
+        gs[j].get(gv);
 #pragma unroll
         for (int q = 0; q < VE; ++q) {
-          const Gate k = gate_of<SPAN>(gs[j][q], dt[j]);
-          s[q] = fmaf(k.a, s[q], k.u * xs[j][q]);
+          const Gate k = gate_of<SPAN>(gv[q], dt[j]);
+          s[q] = fmaf(k.a, s[q], k.u * xv[q]);
         }
-        if (a.h) gs_store<T, VE>(static_cast<T*>(a.h) + (e + j) * a.D + c, n, s);
+        if (a.h) gs_store<T, VE>(static_cast<T*>(a.h) + (e + j) * a.D + c.first, c.skip, s);
       }
   }
 }
@@ -216,34 +216,39 @@ __device__ __forceinline__ void fwd_range(const GsArgs& a, int64_t b, int64_t p,
 // Events [p, t) in reverse, d: what reaches the last of them from behind; returns what reaches
 // the event before p.  v: the segment, for its start.
 template <typename T, int VE, bool SPAN>
-__device__ __forceinline__ void bwd_range(const GsArgs& a, int64_t v, int64_t b, int64_t p, int64_t t, int c, int n,
+__device__ __forceinline__ void bwd_range(const GsArgs& a, int64_t v, int64_t b, int64_t p, int64_t t, Cols c,
                                           float* d) {
   if (t <= p) return;
-  const T* x = static_cast<const T*>(a.x) + c;
-  const T* g = static_cast<const T*>(a.gate) + c;
-  const T* dh = static_cast<const T*>(a.dh) + c;
+  const T* x = static_cast<const T*>(a.x) + c.first;
+  const T* g = static_cast<const T*>(a.gate) + c.first;
+  const T* dh = a.dh ? static_cast<const T*>(a.dh) + c.first : g;        // (read, and left out below)
+  const int64_t lddh = a.dh ? a.D : a.ldx;
   for (int64_t e = p + (t - p - 1) / GS_WIN * GS_WIN; e >= p; e -= GS_WIN) {
-    float u[GS_WIN][VE], w[GS_WIN][VE], k[GS_WIN][VE];     // (w: x, then a)
+    Lump<T, VE> xs[GS_WIN], gs[GS_WIN], ds[GS_WIN];
+    float dt[GS_WIN], u[GS_WIN][VE], w[GS_WIN][VE], k[GS_WIN][VE];
     const int m = t - e < GS_WIN ? int(t - e) : GS_WIN;
+#pragma unroll
+    for (int j = 0; j < GS_WIN; ++j) {
+      const int64_t i = e + (j < m ? j : m - 1);
+      xs[j].load(x + i * a.ldx);
+      gs[j].load(g + i * a.ldx);
+      ds[j].load(dh + i * lddh);
+      dt[j] = SPAN ? a.dt[i] : 1.f;
+    }
     float s[VE];
-    if (e == b) gs_start<VE>(a.h0, v, a.D, c, n, s);
-    else gs_load<float, VE>(a.states + e / GS_WIN * a.D + c, n, s);
+    if (e == b) gs_start<VE>(a.h0, v, a.D, c.first, s);
+    else gs_load<float, VE>(a.states + e / GS_WIN * a.D + c.first, s);
 #pragma unroll
     for (int j = 0; j < GS_WIN; ++j)
       if (j < m) {
-        gs_load<T, VE>(x + (e + j) * a.ldx, n, w[j]);
-        gs_load<T, VE>(g + (e + j) * a.ldx, n, k[j]);
-      }
-#pragma unroll
-    for (int j = 0; j < GS_WIN; ++j)
-      if (j < m) {
-        const float dt = SPAN ? a.dt[e + j] : 1.f;
+        float xv[VE], gv[VE];
+        xs[j].get(xv);
+        gs[j].get(gv);
 #pragma unroll
         for (int q = 0; q < VE; ++q) {
-          const Gate y = gate_of<SPAN>(k[j][q], dt);
-          const float xv = w[j][q];
-          k[j][q] = y.k * (xv - s[q]);
-          s[q] = fmaf(y.a, s[q], y.u * xv);
+          const Gate y = gate_of<SPAN>(gv[q], dt[j]);
+          k[j][q] = y.k * (xv[q] - s[q]);
+          s[q] = fmaf(y.a, s[q], y.u * xv[q]);
           u[j][q] = y.u;
           w[j][q] = y.a;
         }
@@ -252,21 +257,16 @@ __device__ __forceinline__ void bwd_range(const GsArgs& a, int64_t v, int64_t b,
     for (int j = GS_WIN - 1; j >= 0; --j)
       if (j < m) {
         float y[VE], o[VE];
-        if (a.dh) {
-          gs_load<T, VE>(dh + (e + j) * a.D, n, y);
-        } else {
-#pragma unroll
-          for (int q = 0; q < VE; ++q) y[q] = 0.f;
-        }
+        ds[j].get(y);
 #pragma unroll
         for (int q = 0; q < VE; ++q) {
-          d[q] += y[q];
+          d[q] += a.dh ? y[q] : 0.f;
           y[q] = u[j][q] * d[q];
           o[q] = k[j][q] * d[q];
           d[q] *= w[j][q];
         }
-        gs_store<T, VE>(static_cast<T*>(a.dx) + (e + j) * a.lddx + c, n, y);
-        gs_store<T, VE>(static_cast<T*>(a.dgate) + (e + j) * a.lddx + c, n, o);
+        gs_store<T, VE>(static_cast<T*>(a.dx) + (e + j) * a.lddx + c.first, c.skip, y);
+        gs_store<T, VE>(static_cast<T*>(a.dgate) + (e + j) * a.lddx + c.first, c.skip, o);
       }
   }
 }
@@ -320,11 +320,11 @@ __device__ __forceinline__ int64_t find_owner(const GsArgs& a, int64_t k) {
   return -1;
 }
 
-// A workgroup per slot: threads over the columns of its piece.
+// A slot's piece: waves over its columns, `first` of them this wave's, `step` from one to its next.
 template <typename T, int VE, bool SPAN, bool BACK>
-__device__ __forceinline__ void piece_sums(const GsArgs& a, int64_t k) {
+__device__ __forceinline__ void piece_sums(const GsArgs& a, int64_t k, int first, int step) {
   const int64_t v = find_owner(a, k);
-  if (threadIdx.x == 0) a.owner[k] = int32_t(v);
+  if (first == 0) a.owner[k] = int32_t(v);
   if (v < 0) return;
   int64_t b, e;
   Piece r;
@@ -332,80 +332,94 @@ __device__ __forceinline__ void piece_sums(const GsArgs& a, int64_t k) {
   piece_in(a, b, e, k, r);
   // nothing reads the sums of the piece that the chain ends with
   if (BACK ? r.p == b : r.t == e) return;
-  for (int i = threadIdx.x; i < a.C; i += GS_THREADS) {
-    const int c = i * VE, n = a.D - c;
+  for (int i = first; i < a.C; i += step) {
+    const Cols c = cols_of<VE>(i, a.D);
     float pa[VE], pb[VE];
 #pragma unroll
     for (int q = 0; q < VE; ++q) {
       pa[q] = 1.f;
       pb[q] = 0.f;
     }
-    const T* x = (BACK ? static_cast<const T*>(a.dh) : static_cast<const T*>(a.x)) + c;
-    const int64_t ld = BACK ? a.D : a.ldx;
-    const T* g = static_cast<const T*>(a.gate) + c;
-    const int64_t len = r.t - r.p;
-    for (int64_t o = 0; o < len; o += GS_AHEAD) {
-      float xs[GS_AHEAD][VE], gs[GS_AHEAD][VE], dt[GS_AHEAD];
-      const int m = len - o < GS_AHEAD ? int(len - o) : GS_AHEAD;
+    const bool some = !BACK || a.dh;
+    const T* g = static_cast<const T*>(a.gate) + c.first;
+    const T* x = !some ? g : static_cast<const T*>(BACK ? a.dh : a.x) + c.first;
+    const int64_t ld = BACK && a.dh ? a.D : a.ldx;
+    for (int64_t o = r.p; o < r.t; o += GS_AHEAD) {
+      Lump<T, VE> xs[GS_AHEAD], gs[GS_AHEAD];
+      float dt[GS_AHEAD];
+      const int m = r.t - o < GS_AHEAD ? int(r.t - o) : GS_AHEAD;
+#pragma unroll
+      for (int j = 0; j < GS_AHEAD; ++j) {
+        const int64_t at = o + (j < m ? j : m - 1), i = BACK ? r.p + r.t - 1 - at : at;
+        gs[j].load(g + i * a.ldx);
+        xs[j].load(x + i * ld);
+        dt[j] = SPAN ? a.dt[i] : 1.f;
+      }
 #pragma unroll
       for (int j = 0; j < GS_AHEAD; ++j)
         if (j < m) {
-          const int64_t i = BACK ? r.t - 1 - o - j : r.p + o + j;
-          gs_load<T, VE>(g + i * a.ldx, n, gs[j]);
-          if (!BACK || a.dh) {
-            gs_load<T, VE>(x + i * ld, n, xs[j]);
-          } else {
-#pragma unroll
-            for (int q = 0; q < VE; ++q) xs[j][q] = 0.f;
-          }
-          dt[j] = SPAN ? a.dt[i] : 1.f;
-        }
-#pragma unroll
-      for (int j = 0; j < GS_AHEAD; ++j)
-        if (j < m) {
+          float xv[VE], gv[VE];
+          xs[j].get(xv);
+          gs[j].get(gv);
 #pragma unroll
           for (int q = 0; q < VE; ++q) {
-            const Gate y = gate_of<SPAN>(gs[j][q], dt[j]);
+            const Gate y = gate_of<SPAN>(gv[q], dt[j]);
             pa[q] *= y.a;
-            pb[q] = BACK ? y.a * (pb[q] + xs[j][q]) : fmaf(y.a, pb[q], y.u * xs[j][q]);
+            pb[q] = BACK ? y.a * (pb[q] + (some ? xv[q] : 0.f)) : fmaf(y.a, pb[q], y.u * xv[q]);
           }
         }
     }
-    gs_store<float, VE>(a.pa + k * a.D + c, n, pa);
-    gs_store<float, VE>(a.pb + k * a.D + c, n, pb);
+    gs_store<float, VE>(a.pa + k * a.D + c.first, c.skip, pa);
+    gs_store<float, VE>(a.pb + k * a.D + c.first, c.skip, pb);
   }
+}
+
+// The slot of this wave, the first column group of this lane and the stride to its next: a
+// workgroup's waves share one slot or hold several, by the row's width.
+struct Share {
+  int64_t slot;
+  int first, step;
+};
+__device__ __forceinline__ Share share_of(const GsArgs& a, uint32_t block) {
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  return Share{int64_t(block) * (GS_WAVES / a.waves) + wave / a.waves, (wave % a.waves) * 64 + lane, a.waves * 64};
 }
 
 // ------------------------------------------------------------------ kernels
 template <typename T, int VE, bool SPAN, bool BACK>
 __global__ void __launch_bounds__(GS_THREADS) k_scan(GsArgs a) {
   if (blockIdx.x >= a.direct) {
-    piece_sums<T, VE, SPAN, BACK>(a, blockIdx.x - a.direct);
+    const Share h = share_of(a, blockIdx.x - a.direct);
+    if (h.slot < a.slots) piece_sums<T, VE, SPAN, BACK>(a, h.slot, h.first, h.step);
     return;
   }
   const uint32_t i = blockIdx.x * GS_THREADS + threadIdx.x;
   const int64_t v = i / uint32_t(a.C);
   if (v >= a.N) return;
-  const int c = int(i - uint32_t(v) * uint32_t(a.C)) * VE, n = a.D - c;
+  const Cols c = cols_of<VE>(int(i - uint32_t(v) * uint32_t(a.C)), a.D);
   int64_t b, e;
   segment_of(a, v, b, e);
   if (e - b >= a.cut) return;
   float s[VE];
   if constexpr (BACK) {
-    gs_start<VE>(a.dh_last, v, a.D, c, n, s);
-    bwd_range<T, VE, SPAN>(a, v, b, b, e, c, n, s);
-    if (a.dh0) gs_store<float, VE>(a.dh0 + v * a.D + c, n, s);
+    gs_start<VE>(a.dh_last, v, a.D, c.first, s);
+    bwd_range<T, VE, SPAN>(a, v, b, b, e, c, s);
+    if (a.dh0) gs_store<float, VE>(a.dh0 + v * a.D + c.first, c.skip, s);
   } else {
-    gs_start<VE>(a.h0, v, a.D, c, n, s);
-    fwd_range<T, VE, SPAN>(a, b, b, e, c, n, s);
-    if (a.h_last) gs_store<float, VE>(a.h_last + v * a.D + c, n, s);
+    gs_start<VE>(a.h0, v, a.D, c.first, s);
+    fwd_range<T, VE, SPAN>(a, b, b, e, c, s);
+    if (a.h_last) gs_store<float, VE>(a.h_last + v * a.D + c.first, c.skip, s);
   }
 }
 
-// The pieces' starts: from the workgroup of the slot that holds a long segment's first piece
-// (backward: from the last piece on).  The start of slot k takes pa's place.
+// The pieces' starts: by the workgroup of the slot that holds a long segment's first piece
+// (backward: from the last piece on).  The start of slot k takes pa's place.  64 columns a
+// workgroup; each of its waves takes a stretch of the pieces, forms its product and result,
+// and, once it knows what the stretches before leave, the starts.
+constexpr int GS_CHAIN = 8;          // waves of a chain
 template <bool BACK>
-__global__ void __launch_bounds__(GS_THREADS) k_scan_chain(GsArgs a) {
+__global__ void __launch_bounds__(64 * GS_CHAIN) k_scan_chain(GsArgs a) {
+  __shared__ float s_a[GS_CHAIN][64], s_b[GS_CHAIN][64];
   const int64_t k = blockIdx.x;
   const int64_t v = a.owner[k];
   if (v < 0) return;
@@ -413,50 +427,73 @@ __global__ void __launch_bounds__(GS_THREADS) k_scan_chain(GsArgs a) {
   Piece r;
   segment_of(a, v, b, e);
   if (!piece_in(a, b, e, k, r) || r.p != b) return;
-  const int64_t pieces = (e - b) / a.piece;
-  for (int c = threadIdx.x; c < a.D; c += GS_THREADS) {
-    const float* first = BACK ? a.dh_last : a.h0;
-    float s = first ? first[v * a.D + c] : 0.f;
-    for (int64_t j = 0; j < pieces; j += GS_CARRY) {
-      float pa[GS_CARRY], pb[GS_CARRY];
-      const int m = pieces - j < GS_CARRY ? int(pieces - j) : GS_CARRY;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int c0 = blockIdx.y * 64 + lane, c = c0 < a.D ? c0 : a.D - 1;
+  const int64_t pieces = (e - b) / a.piece, links = pieces - 1;      // the chain's last piece has no sums
+  const int64_t per = (links + GS_CHAIN - 1) / GS_CHAIN;
+  const int64_t j0 = min(wave * per, links), j1 = min(j0 + per, links);
+  // piece j of the chain
+  auto at = [&](int64_t j) { return (k + (BACK ? pieces - 1 - j : j)) * a.D + c; };
+  float pa = 1.f, pb = 0.f;
+  for (int64_t j = j0; j < j1; j += GS_CARRY) {
+    float xa[GS_CARRY], xb[GS_CARRY];
 #pragma unroll
-      for (int q = 0; q < GS_CARRY; ++q)
-        if (q < m && j + q + 1 < pieces) {                 // the chain's last piece has no sums
-          const int64_t at = (b + (BACK ? pieces - 1 - j - q : j + q) * a.piece) / a.piece * a.D + c;
-          pa[q] = a.pa[at];
-          pb[q] = a.pb[at];
-        }
-#pragma unroll
-      for (int q = 0; q < GS_CARRY; ++q)
-        if (q < m) {
-          const int64_t at = (b + (BACK ? pieces - 1 - j - q : j + q) * a.piece) / a.piece * a.D + c;
-          a.pa[at] = s;
-          if (j + q + 1 < pieces) s = fmaf(pa[q], s, pb[q]);
-        }
+    for (int q = 0; q < GS_CARRY; ++q) {
+      const int64_t i = at(min(j + q, j1 - 1));
+      xa[q] = a.pa[i];
+      xb[q] = a.pb[i];
     }
+#pragma unroll
+    for (int q = 0; q < GS_CARRY; ++q)
+      if (j + q < j1) {
+        pb = fmaf(xa[q], pb, xb[q]);
+        pa *= xa[q];
+      }
   }
+  s_a[wave][lane] = pa;
+  s_b[wave][lane] = pb;
+  __syncthreads();
+  const float* first = BACK ? a.dh_last : a.h0;
+  float s = first ? first[v * a.D + c] : 0.f;
+  for (int w = 0; w < wave; ++w) s = fmaf(s_a[w][lane], s, s_b[w][lane]);
+  for (int64_t j = j0; j < j1; j += GS_CARRY) {
+    float xa[GS_CARRY], xb[GS_CARRY];
+#pragma unroll
+    for (int q = 0; q < GS_CARRY; ++q) {
+      const int64_t i = at(min(j + q, j1 - 1));
+      xa[q] = a.pa[i];
+      xb[q] = a.pb[i];
+    }
+#pragma unroll
+    for (int q = 0; q < GS_CARRY; ++q)
+      if (j + q < j1) {
+        if (c0 < a.D) a.pa[at(j + q)] = s;
+        s = fmaf(xa[q], s, xb[q]);
+      }
+  }
+  if (j1 == links && (j0 < j1 || wave == 0) && c0 < a.D) a.pa[at(links)] = s;
 }
 
 template <typename T, int VE, bool SPAN, bool BACK>
 __global__ void __launch_bounds__(GS_THREADS) k_scan_pieces(GsArgs a) {
-  const int64_t k = blockIdx.x;
-  const int64_t v = a.owner[k];
+  const Share h = share_of(a, blockIdx.x);
+  if (h.slot >= a.slots) return;
+  const int64_t k = h.slot, v = a.owner[k];
   if (v < 0) return;
   int64_t b, e;
   Piece r;
   segment_of(a, v, b, e);
   if (!piece_in(a, b, e, k, r)) return;
-  for (int i = threadIdx.x; i < a.C; i += GS_THREADS) {
-    const int c = i * VE, n = a.D - c;
+  for (int i = h.first; i < a.C; i += h.step) {
+    const Cols c = cols_of<VE>(i, a.D);
     float s[VE];
-    gs_load<float, VE>(a.pa + k * a.D + c, n, s);
+    gs_load<float, VE>(a.pa + k * a.D + c.first, s);
     if constexpr (BACK) {
-      bwd_range<T, VE, SPAN>(a, v, b, r.p, r.t, c, n, s);
-      if (r.p == b && a.dh0) gs_store<float, VE>(a.dh0 + v * a.D + c, n, s);
+      bwd_range<T, VE, SPAN>(a, v, b, r.p, r.t, c, s);
+      if (r.p == b && a.dh0) gs_store<float, VE>(a.dh0 + v * a.D + c.first, c.skip, s);
     } else {
-      fwd_range<T, VE, SPAN>(a, b, r.p, r.t, c, n, s);
-      if (r.t == e && a.h_last) gs_store<float, VE>(a.h_last + v * a.D + c, n, s);
+      fwd_range<T, VE, SPAN>(a, b, r.p, r.t, c, s);
+      if (r.t == e && a.h_last) gs_store<float, VE>(a.h_last + v * a.D + c.first, c.skip, s);
     }
   }
 }
@@ -521,31 +558,42 @@ static fast_status_t gs_check(const char* fn, const fast_tcsr_t* g, int D, fast_
 
 template <bool BACK, typename T, int VE, bool SPAN>
 static void gs_launch(const GsArgs& a, hipStream_t st) {
-  hipLaunchKernelGGL((k_scan<T, VE, SPAN, BACK>), dim3(uint32_t(a.direct + a.slots)), dim3(GS_THREADS), 0, st, a);
+  const int per = GS_WAVES / a.waves;
+  const uint32_t pieces = uint32_t((a.slots + per - 1) / per);
+  if (a.direct + pieces > 0)
+    hipLaunchKernelGGL((k_scan<T, VE, SPAN, BACK>), dim3(a.direct + pieces), dim3(GS_THREADS), 0, st, a);
   if (a.slots == 0) return;
-  hipLaunchKernelGGL((k_scan_chain<BACK>), dim3(uint32_t(a.slots)), dim3(GS_THREADS), 0, st, a);
-  hipLaunchKernelGGL((k_scan_pieces<T, VE, SPAN, BACK>), dim3(uint32_t(a.slots)), dim3(GS_THREADS), 0, st, a);
+  hipLaunchKernelGGL((k_scan_chain<BACK>), dim3(uint32_t(a.slots), uint32_t((a.D + 63) / 64)), dim3(64 * GS_CHAIN), 0,
+                     st, a);
+  hipLaunchKernelGGL((k_scan_pieces<T, VE, SPAN, BACK>), dim3(pieces), dim3(GS_THREADS), 0, st, a);
+}
+template <bool BACK, typename T, int VE>
+static void gs_launch(const GsArgs& a, hipStream_t st) {
+  if (a.dt) gs_launch<BACK, T, VE, true>(a, st);
+  else gs_launch<BACK, T, VE, false>(a, st);
 }
 
 template <bool BACK>
 static fast_status_t gs_run(const char* fn, GsArgs& a, fast_dtype_t dtype, int64_t longest, void* ws,
                             hipStream_t st) {
-  const int ve = 2;
+  const int ve = a.D > 1 ? 2 : 1;
   a.C = (a.D + ve - 1) / ve;
+  a.waves = a.C > 128 ? 4 : (a.C > 64 ? 2 : 1);
   const GsPlan p = gs_plan(a.N, a.E, a.D, elem_size(dtype), longest);
   a.cut = p.cut;
   a.piece = p.piece;
   a.slots = p.slots;
   gs_layout(p.slots, a.D, static_cast<char*>(ws), &a);
   const int64_t direct = (a.N * a.C + GS_THREADS - 1) / GS_THREADS;
-  if (!grid_fits(direct + a.slots, GS_THREADS)) return fail(FAST_ERR_UNSUPPORTED, "%s: 2^32 threads or more", fn);
+  if (!grid_fits(direct + a.slots, GS_THREADS) || !grid_fits(a.slots, 64 * GS_CHAIN))
+    return fail(FAST_ERR_UNSUPPORTED, "%s: 2^32 threads or more", fn);
   a.direct = uint32_t(direct);
   if (dtype == FAST_F32) {
-    if (a.dt) gs_launch<BACK, float, 2, true>(a, st);
-    else gs_launch<BACK, float, 2, false>(a, st);
+    if (ve == 2) gs_launch<BACK, float, 2>(a, st);
+    else gs_launch<BACK, float, 1>(a, st);
   } else {
-    if (a.dt) gs_launch<BACK, uint16_t, 2, true>(a, st);
-    else gs_launch<BACK, uint16_t, 2, false>(a, st);
+    if (ve == 2) gs_launch<BACK, uint16_t, 2>(a, st);
+    else gs_launch<BACK, uint16_t, 1>(a, st);
   }
   return check_launch(fn);
 }
