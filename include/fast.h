@@ -744,7 +744,7 @@ fast_status_t fast_linear_bwd(int64_t n, int in, int out, fast_dtype_t dtype, co
  * longest: a length that no segment exceeds, 0 where none is known.  It only chooses
  * launches: short segments then need fewer; a longer segment is right all the same.
  * Outputs lie apart from the inputs and each other (but h_last and h0).
- * Limits: D <= 8192, ldx < 2^31, rows that span less than 2^56 elements, N, E < 2^31,
+ * Limits: D <= 8192, ldx < 2^26, N, E < 2^31,
  * fewer than 2^32 threads.  Repeated calls give the same bits.
  * Workspace: fast_gated_scan_workspace(N, E, D) bytes, 256-byte aligned; one for the
  * largest N, E serves smaller blocks of the same D.

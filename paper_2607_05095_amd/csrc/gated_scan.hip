@@ -26,7 +26,7 @@ namespace fast {
 constexpr int GS_THREADS = 256, GS_WAVES = GS_THREADS / 64;
 constexpr int GS_AHEAD = 8;          // events whose rows are loaded together
 constexpr int GS_WIN = 8;            // events of a backward window
-constexpr int64_t GS_MAX_D = 8192;
+constexpr int64_t GS_MAX_D = 8192, GS_MAX_LD = 1 << 26;
 constexpr int GS_CARRY = 16;         // pieces whose sums are loaded together
 
 // ------------------------------------------------------------------ the gate
@@ -34,27 +34,38 @@ struct Gate {
   float a, u, k;                     // k: the slope of u over the gate, a dt sigmoid(gate)
 };
 
-// e^-x 2^up for x >= 0 within 2 ulp: the product with log2(e) in two parts.
-__device__ __forceinline__ float exp_neg(float x, float up = 0.f) {
-  const float h = -x * 0x1.715476p+0f;
-  const float l = fmaf(-x, 0x1.715476p+0f, -h) - x * 0x1.4ae0cp-26f;
-  const float e = __builtin_amdgcn_exp2f(h + up);
-  return h + up < -126.f ? e : fmaf(e, l * 0x1.62e43p-1f, e);
+// An event's time.  Where it is long, e^gate is formed 2^64 times as large and the time as much
+// smaller: a rate too small for fp32 counts over such a time.
+struct Span {
+  float dt, up, part, down;          // 2^up e^gate part = e^gate dt; 2^up e^gate down = e^gate
+};
+__device__ __forceinline__ Span span_of(float dt) {
+  dt = dt < 0.f ? 0.f : dt;
+  const bool l = dt > 0x1p20f;
+  return Span{dt, l ? 64.f : 0.f, l ? dt * 0x1p-64f : dt, l ? 0x1p-64f : 1.f};
 }
 
-// u = 1 - a keeps its relative accuracy for slow gates and a for fast ones.
+// u = 1 - a keeps its relative accuracy for slow gates and a for fast ones.  No branches: the
+// evaluations of several events and columns interleave.
 template <bool SPAN>
-__device__ __forceinline__ Gate gate_of(float g, float dt) {
+__device__ __forceinline__ Gate gate_of(float g, const Span& w) {
   Gate q;
-  const float t = exp_neg(fabsf(g));                       // sigmoid(|g|) = 1 / (1 + t)
-  const float r = __builtin_amdgcn_rcpf(1.f + t), small = t * r;
-  const float sig = g >= 0.f ? r : small;
+  // t = e^-|g| 2^up within 3 U: the product with log2(e) in two parts (the second is no number
+  // where g is infinite, and 0 or close to it otherwise)
+  const float x = fabsf(g), h = -x * 0x1.715476p+0f;
+  float l = fmaf(-x, 0x1.715476p+0f, -h);
+  l = __builtin_amdgcn_fmed3f(fmaf(-x, 0x1.4ae0cp-26f, l), -1.f, 1.f);
+  float ts = __builtin_amdgcn_exp2f(SPAN ? h + w.up : h);
+  ts = fmaf(ts, l * 0x1.62e43p-1f, ts);
+  const bool pos = g >= 0.f;
   if constexpr (!SPAN) {
-    q.u = sig;
-    q.a = g >= 0.f ? small : r;
-    q.k = q.a * sig;
+    const float r = __builtin_amdgcn_rcpf(1.f + ts), small = ts * r;   // sigmoid(|g|) = 1 / (1 + t)
+    q.u = pos ? r : small;
+    q.a = pos ? small : r;
+    q.k = q.a * q.u;
     return q;
   }
+  const float t = ts * w.down;
   // log(1 + t) / t on (0, 1], within 2^-27 (a weighted least-squares fit)
   float p = -0x1.a9330cp-9f;
   p = fmaf(p, t, 0x1.453edcp-6f);
@@ -66,11 +77,7 @@ __device__ __forceinline__ Gate gate_of(float g, float dt) {
   p = fmaf(p, t, 0x1.554c80p-2f);
   p = fmaf(p, t, -0x1.ffffbep-2f);
   p = fmaf(p, t, 1.f);
-  const float rate = fmaf(p, t, g > 0.f ? g : 0.f);
-  dt = dt < 0.f ? 0.f : dt;
-  float y = rate * dt;
-  const bool far = g < -86.f;                              // a rate below what fp32 holds, e^gate
-  if (far) y = exp_neg(-g, 120.f) * (dt * 0x1p-120f);
+  const float y = fmaf(p * ts, w.part, fmaxf(g, 0.f) * w.dt);          // rate dt
   // (1 - e^-y) / y below log 2, within 2^-26; the difference above
   const float e = __builtin_amdgcn_exp2f(y * -0x1.715476p+0f);
   float s = -0x1.0ed322p-10f;
@@ -81,7 +88,8 @@ __device__ __forceinline__ Gate gate_of(float g, float dt) {
   s = fmaf(s, y, 1.f);
   q.u = y < 0.6931f ? s * y : 1.f - e;
   q.a = e;
-  q.k = far ? e * y : e * dt * sig;
+  const float r = __builtin_amdgcn_rcpf(1.f + t);
+  q.k = e * (pos ? r * w.dt : ts * r * w.part);
   return q;
 }
 
@@ -179,37 +187,61 @@ __device__ __forceinline__ void gs_start(const float* rows, int64_t row, int D, 
   }
 }
 
+// The rows of events e, e + 1, ... of x and gate, a lane's columns of them.
+template <typename T, int VE, int COUNT>
+struct Rows {
+  Lump<T, VE> x[COUNT], g[COUNT];
+  float dt[COUNT];
+  // m events; the last one again from there on.  A round spans less than 2^32 bytes.
+  template <bool SPAN>
+  __device__ void load(const GsArgs& a, int c, int64_t e, int m) {
+    const char* px = reinterpret_cast<const char*>(static_cast<const T*>(a.x) + e * a.ldx + c);
+    const char* pg = reinterpret_cast<const char*>(static_cast<const T*>(a.gate) + e * a.ldx + c);
+    const uint32_t ld = uint32_t(a.ldx) * uint32_t(sizeof(T)), end = uint32_t(m - 1) * ld;
+#pragma unroll
+    for (int j = 0; j < COUNT; ++j) {
+      const uint32_t o = min(uint32_t(j) * ld, end);
+      x[j].load(reinterpret_cast<const T*>(px + o));
+      g[j].load(reinterpret_cast<const T*>(pg + o));
+      dt[j] = SPAN ? a.dt[e + min(j, m - 1)] : 1.f;
+    }
+  }
+};
+constexpr int GS_SIDE = 2;           // events whose gates are formed side by side
+
 // Events [p, t) of a segment that starts at b, from the state s.
 template <typename T, int VE, bool SPAN>
 __device__ __forceinline__ void fwd_range(const GsArgs& a, int64_t b, int64_t p, int64_t t, Cols c, float* s) {
-  const T* x = static_cast<const T*>(a.x) + c.first;
-  const T* g = static_cast<const T*>(a.gate) + c.first;
+  T* h = a.h ? static_cast<T*>(a.h) + p * a.D + c.first : nullptr;
   for (int64_t e = p; e < t; e += GS_AHEAD) {
-    Lump<T, VE> xs[GS_AHEAD], gs[GS_AHEAD];
-    float dt[GS_AHEAD];
     const int m = t - e < GS_AHEAD ? int(t - e) : GS_AHEAD;
-#pragma unroll
-    for (int j = 0; j < GS_AHEAD; ++j) {
-      const int64_t i = e + (j < m ? j : m - 1);           // past the end: the last event again
-      xs[j].load(x + i * a.ldx);
-      gs[j].load(g + i * a.ldx);
-      dt[j] = SPAN ? a.dt[i] : 1.f;
-    }
+    Rows<T, VE, GS_AHEAD> r;
+    r.template load<SPAN>(a, c.first, e, m);
     if (a.states && e > b && ((e - b) & (GS_WIN - 1)) == 0)
       gs_store<float, VE>(a.states + e / GS_WIN * a.D + c.first, c.skip, s);
 #pragma unroll
-    for (int j = 0; j < GS_AHEAD; ++j)
-      if (j < m) {
-        float xv[VE], gv[VE];
-        xs[j].get(xv);
-        gs[j].get(gv);
+    for (int i = 0; i < GS_AHEAD; i += GS_SIDE) {
+      if (!__any(i < m)) break;
+      Gate k[GS_SIDE][VE];
+      float xv[GS_SIDE][VE];
 #pragma unroll
-        for (int q = 0; q < VE; ++q) {
-          const Gate k = gate_of<SPAN>(gv[q], dt[j]);
-          s[q] = fmaf(k.a, s[q], k.u * xv[q]);
-        }
-        if (a.h) gs_store<T, VE>(static_cast<T*>(a.h) + (e + j) * a.D + c.first, c.skip, s);
+      for (int j = 0; j < GS_SIDE; ++j) {
+        float gv[VE];
+        r.x[i + j].get(xv[j]);
+        r.g[i + j].get(gv);
+        const Span w = span_of(r.dt[i + j]);
+#pragma unroll
+        for (int q = 0; q < VE; ++q) k[j][q] = gate_of<SPAN>(gv[q], w);
       }
+#pragma unroll
+      for (int j = 0; j < GS_SIDE; ++j)
+        if (i + j < m) {
+#pragma unroll
+          for (int q = 0; q < VE; ++q) s[q] = fmaf(k[j][q].a, s[q], k[j][q].u * xv[j][q]);
+          if (h) gs_store<T, VE>(h + int64_t(i + j) * a.D, c.skip, s);
+        }
+    }
+    if (h) h += int64_t(GS_AHEAD) * a.D;
   }
 }
 
@@ -219,40 +251,44 @@ template <typename T, int VE, bool SPAN>
 __device__ __forceinline__ void bwd_range(const GsArgs& a, int64_t v, int64_t b, int64_t p, int64_t t, Cols c,
                                           float* d) {
   if (t <= p) return;
-  const T* x = static_cast<const T*>(a.x) + c.first;
-  const T* g = static_cast<const T*>(a.gate) + c.first;
-  const T* dh = a.dh ? static_cast<const T*>(a.dh) + c.first : g;        // (read, and left out below)
-  const int64_t lddh = a.dh ? a.D : a.ldx;
   for (int64_t e = p + (t - p - 1) / GS_WIN * GS_WIN; e >= p; e -= GS_WIN) {
-    Lump<T, VE> xs[GS_WIN], gs[GS_WIN], ds[GS_WIN];
-    float dt[GS_WIN], u[GS_WIN][VE], w[GS_WIN][VE], k[GS_WIN][VE];
     const int m = t - e < GS_WIN ? int(t - e) : GS_WIN;
+    Rows<T, VE, GS_WIN> r;
+    r.template load<SPAN>(a, c.first, e, m);
+    Lump<T, VE> ds[GS_WIN];
+    {
+      // (without dh a row of the gate, which is left out below)
+      const T* dh = a.dh ? static_cast<const T*>(a.dh) + e * a.D + c.first
+                         : static_cast<const T*>(a.gate) + e * a.ldx + c.first;
+      const uint32_t ld = a.dh ? uint32_t(a.D) : uint32_t(a.ldx), end = uint32_t(m - 1) * ld;
 #pragma unroll
-    for (int j = 0; j < GS_WIN; ++j) {
-      const int64_t i = e + (j < m ? j : m - 1);
-      xs[j].load(x + i * a.ldx);
-      gs[j].load(g + i * a.ldx);
-      ds[j].load(dh + i * lddh);
-      dt[j] = SPAN ? a.dt[i] : 1.f;
+      for (int j = 0; j < GS_WIN; ++j) ds[j].load(dh + min(uint32_t(j) * ld, end));
     }
     float s[VE];
     if (e == b) gs_start<VE>(a.h0, v, a.D, c.first, s);
     else gs_load<float, VE>(a.states + e / GS_WIN * a.D + c.first, s);
+    float u[GS_WIN][VE], w[GS_WIN][VE], k[GS_WIN][VE];
 #pragma unroll
-    for (int j = 0; j < GS_WIN; ++j)
-      if (j < m) {
-        float xv[VE], gv[VE];
-        xs[j].get(xv);
-        gs[j].get(gv);
+    for (int i = 0; i < GS_WIN; i += GS_SIDE)
+      if (__any(i < m)) {
 #pragma unroll
-        for (int q = 0; q < VE; ++q) {
-          const Gate y = gate_of<SPAN>(gv[q], dt[j]);
-          k[j][q] = y.k * (xv[q] - s[q]);
-          s[q] = fmaf(y.a, s[q], y.u * xv[q]);
-          u[j][q] = y.u;
-          w[j][q] = y.a;
+        for (int j = i; j < i + GS_SIDE; ++j) {
+          float xv[VE], gv[VE];
+          r.x[j].get(xv);
+          r.g[j].get(gv);
+          const Span span = span_of(r.dt[j]);
+#pragma unroll
+          for (int q = 0; q < VE; ++q) {
+            const Gate y = gate_of<SPAN>(gv[q], span);
+            k[j][q] = y.k * (xv[q] - s[q]);
+            s[q] = fmaf(y.a, s[q], y.u * xv[q]);           // (past the end: used no more)
+            u[j][q] = y.u;
+            w[j][q] = y.a;
+          }
         }
       }
+    T* dx = static_cast<T*>(a.dx) + e * a.lddx + c.first;
+    T* dg = static_cast<T*>(a.dgate) + e * a.lddx + c.first;
 #pragma unroll
     for (int j = GS_WIN - 1; j >= 0; --j)
       if (j < m) {
@@ -265,8 +301,8 @@ __device__ __forceinline__ void bwd_range(const GsArgs& a, int64_t v, int64_t b,
           o[q] = k[j][q] * d[q];
           d[q] *= w[j][q];
         }
-        gs_store<T, VE>(static_cast<T*>(a.dx) + (e + j) * a.lddx + c.first, c.skip, y);
-        gs_store<T, VE>(static_cast<T*>(a.dgate) + (e + j) * a.lddx + c.first, c.skip, o);
+        gs_store<T, VE>(dx + j * a.lddx, c.skip, y);
+        gs_store<T, VE>(dg + j * a.lddx, c.skip, o);
       }
   }
 }
@@ -340,34 +376,39 @@ __device__ __forceinline__ void piece_sums(const GsArgs& a, int64_t k, int first
       pa[q] = 1.f;
       pb[q] = 0.f;
     }
-    const bool some = !BACK || a.dh;
-    const T* g = static_cast<const T*>(a.gate) + c.first;
-    const T* x = !some ? g : static_cast<const T*>(BACK ? a.dh : a.x) + c.first;
-    const int64_t ld = BACK && a.dh ? a.D : a.ldx;
-    for (int64_t o = r.p; o < r.t; o += GS_AHEAD) {
-      Lump<T, VE> xs[GS_AHEAD], gs[GS_AHEAD];
-      float dt[GS_AHEAD];
-      const int m = r.t - o < GS_AHEAD ? int(r.t - o) : GS_AHEAD;
+    for (int64_t o = 0; o < r.t - r.p; o += GS_AHEAD) {
+      const int m = r.t - r.p - o < GS_AHEAD ? int(r.t - r.p - o) : GS_AHEAD;
+      const int64_t at = BACK ? r.t - o - m : r.p + o;
+      Rows<T, VE, GS_AHEAD> w;
+      w.template load<SPAN>(a, c.first, at, m);
+      if constexpr (BACK) {                               // dh in x's place
+        if (a.dh) {
+          const T* dh = static_cast<const T*>(a.dh) + at * a.D + c.first;
+#pragma unroll
+          for (int j = 0; j < GS_AHEAD; ++j) w.x[j].load(dh + min(j, m - 1) * a.D);
+        }
+      }
+      Gate y[GS_AHEAD][VE];
 #pragma unroll
       for (int j = 0; j < GS_AHEAD; ++j) {
-        const int64_t at = o + (j < m ? j : m - 1), i = BACK ? r.p + r.t - 1 - at : at;
-        gs[j].load(g + i * a.ldx);
-        xs[j].load(x + i * ld);
-        dt[j] = SPAN ? a.dt[i] : 1.f;
+        float gv[VE];
+        w.g[j].get(gv);
+        const Span span = span_of(w.dt[j]);
+#pragma unroll
+        for (int q = 0; q < VE; ++q) y[j][q] = gate_of<SPAN>(gv[q], span);
       }
 #pragma unroll
-      for (int j = 0; j < GS_AHEAD; ++j)
-        if (j < m) {
-          float xv[VE], gv[VE];
-          xs[j].get(xv);
-          gs[j].get(gv);
+      for (int jj = 0; jj < GS_AHEAD; ++jj) {
+        const int j = BACK ? GS_AHEAD - 1 - jj : jj;
+        float xv[VE];
+        w.x[j].get(xv);
 #pragma unroll
-          for (int q = 0; q < VE; ++q) {
-            const Gate y = gate_of<SPAN>(gv[q], dt[j]);
-            pa[q] *= y.a;
-            pb[q] = BACK ? y.a * (pb[q] + (some ? xv[q] : 0.f)) : fmaf(y.a, pb[q], y.u * xv[q]);
-          }
+        for (int q = 0; q < VE; ++q) {
+          const float in = BACK ? y[j][q].a * (pb[q] + (a.dh ? xv[q] : 0.f)) : fmaf(y[j][q].a, pb[q], y[j][q].u * xv[q]);
+          pb[q] = j < m ? in : pb[q];
+          pa[q] = j < m ? pa[q] * y[j][q].a : pa[q];
         }
+      }
     }
     gs_store<float, VE>(a.pa + k * a.D + c.first, c.skip, pa);
     gs_store<float, VE>(a.pb + k * a.D + c.first, c.skip, pb);
@@ -412,66 +453,87 @@ __global__ void __launch_bounds__(GS_THREADS) k_scan(GsArgs a) {
   }
 }
 
-// The pieces' starts: by the workgroup of the slot that holds a long segment's first piece
-// (backward: from the last piece on).  The start of slot k takes pa's place.  64 columns a
-// workgroup; each of its waves takes a stretch of the pieces, forms its product and result,
-// and, once it knows what the stretches before leave, the starts.
-constexpr int GS_CHAIN = 8;          // waves of a chain
+// The pieces' starts (backward: from the last piece on), over 64 columns a workgroup.  It looks
+// at GS_CHAIN slots, a wave each: the wave whose slot holds a long segment's first piece walks
+// its pieces.  The start of slot k takes pa's place.  A chain of more than GS_ALONE pieces (of
+// the slots of a workgroup one at most starts such) is walked by all its waves, each a stretch:
+// its product and result first, then, once it knows what the stretches before leave, the starts.
+constexpr int GS_CHAIN = 8, GS_ALONE = 64;
+static_assert(GS_ALONE > GS_CHAIN, "one long chain a workgroup");
+struct Chain {
+  int64_t k, pieces;
+  const GsArgs& a;
+  int c;
+  bool back;
+  // where piece j of the chain lies
+  __device__ int64_t at(int64_t j) const { return (k + (back ? pieces - 1 - j : j)) * a.D + c; }
+  // pieces [j0, j1) from the state s; starts are written where `write`
+  template <bool WRITE>
+  __device__ void walk(int64_t j0, int64_t j1, bool write, float& pa, float& s) const {
+    for (int64_t j = j0; j < j1; j += GS_CARRY) {
+      float xa[GS_CARRY], xb[GS_CARRY];
+#pragma unroll
+      for (int q = 0; q < GS_CARRY; ++q) {
+        const int64_t i = at(min(j + q, j1 - 1));
+        xa[q] = a.pa[i];
+        xb[q] = a.pb[i];
+      }
+#pragma unroll
+      for (int q = 0; q < GS_CARRY; ++q)
+        if (j + q < j1) {
+          if (WRITE && write) a.pa[at(j + q)] = s;
+          s = fmaf(xa[q], s, xb[q]);
+          pa *= xa[q];
+        }
+    }
+  }
+};
 template <bool BACK>
 __global__ void __launch_bounds__(64 * GS_CHAIN) k_scan_chain(GsArgs a) {
   __shared__ float s_a[GS_CHAIN][64], s_b[GS_CHAIN][64];
-  const int64_t k = blockIdx.x;
-  const int64_t v = a.owner[k];
-  if (v < 0) return;
-  int64_t b, e;
-  Piece r;
-  segment_of(a, v, b, e);
-  if (!piece_in(a, b, e, k, r) || r.p != b) return;
+  __shared__ int64_t s_long[2];                           // slot and segment of a long chain
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int c0 = blockIdx.y * 64 + lane, c = c0 < a.D ? c0 : a.D - 1;
-  const int64_t pieces = (e - b) / a.piece, links = pieces - 1;      // the chain's last piece has no sums
-  const int64_t per = (links + GS_CHAIN - 1) / GS_CHAIN;
-  const int64_t j0 = min(wave * per, links), j1 = min(j0 + per, links);
-  // piece j of the chain
-  auto at = [&](int64_t j) { return (k + (BACK ? pieces - 1 - j : j)) * a.D + c; };
-  float pa = 1.f, pb = 0.f;
-  for (int64_t j = j0; j < j1; j += GS_CARRY) {
-    float xa[GS_CARRY], xb[GS_CARRY];
-#pragma unroll
-    for (int q = 0; q < GS_CARRY; ++q) {
-      const int64_t i = at(min(j + q, j1 - 1));
-      xa[q] = a.pa[i];
-      xb[q] = a.pb[i];
-    }
-#pragma unroll
-    for (int q = 0; q < GS_CARRY; ++q)
-      if (j + q < j1) {
-        pb = fmaf(xa[q], pb, xb[q]);
-        pa *= xa[q];
+  const bool in = c0 < a.D;
+  const int64_t k = int64_t(blockIdx.x) * GS_CHAIN + wave;
+  if (threadIdx.x == 0) s_long[1] = -1;
+  __syncthreads();
+  const int64_t v = k < a.slots ? a.owner[k] : -1;
+  const float* first = BACK ? a.dh_last : a.h0;
+  if (v >= 0) {
+    int64_t b, e;
+    Piece r;
+    segment_of(a, v, b, e);
+    if (piece_in(a, b, e, k, r) && r.p == b) {
+      const int64_t pieces = (e - b) / a.piece;
+      if (pieces <= GS_ALONE) {
+        const Chain ch = {k, pieces, a, c, BACK};
+        float pa = 1.f, s = first ? first[v * a.D + c] : 0.f;
+        ch.walk<true>(0, pieces - 1, in, pa, s);          // the chain's last piece has no sums
+        if (in) a.pa[ch.at(pieces - 1)] = s;
+      } else if (lane == 0) {
+        s_long[0] = k;
+        s_long[1] = v;
       }
+    }
   }
+  __syncthreads();
+  const int64_t lv = s_long[1];
+  if (lv < 0) return;
+  int64_t b, e;
+  segment_of(a, lv, b, e);
+  const Chain ch = {s_long[0], (e - b) / a.piece, a, c, BACK};
+  const int64_t links = ch.pieces - 1, per = (links + GS_CHAIN - 1) / GS_CHAIN;
+  const int64_t j0 = min(wave * per, links), j1 = min(j0 + per, links);
+  float pa = 1.f, pb = 0.f;
+  ch.walk<false>(j0, j1, false, pa, pb);
   s_a[wave][lane] = pa;
   s_b[wave][lane] = pb;
   __syncthreads();
-  const float* first = BACK ? a.dh_last : a.h0;
-  float s = first ? first[v * a.D + c] : 0.f;
+  float s = first ? first[lv * a.D + c] : 0.f;
   for (int w = 0; w < wave; ++w) s = fmaf(s_a[w][lane], s, s_b[w][lane]);
-  for (int64_t j = j0; j < j1; j += GS_CARRY) {
-    float xa[GS_CARRY], xb[GS_CARRY];
-#pragma unroll
-    for (int q = 0; q < GS_CARRY; ++q) {
-      const int64_t i = at(min(j + q, j1 - 1));
-      xa[q] = a.pa[i];
-      xb[q] = a.pb[i];
-    }
-#pragma unroll
-    for (int q = 0; q < GS_CARRY; ++q)
-      if (j + q < j1) {
-        if (c0 < a.D) a.pa[at(j + q)] = s;
-        s = fmaf(xa[q], s, xb[q]);
-      }
-  }
-  if (j1 == links && (j0 < j1 || wave == 0) && c0 < a.D) a.pa[at(links)] = s;
+  ch.walk<true>(j0, j1, in, pa, s);
+  if (j0 < j1 && j1 == links && in) a.pa[ch.at(links)] = s;
 }
 
 template <typename T, int VE, bool SPAN, bool BACK>
@@ -548,7 +610,7 @@ static fast_status_t gs_check(const char* fn, const fast_tcsr_t* g, int D, fast_
   if (D > GS_MAX_D) return fail(FAST_ERR_UNSUPPORTED, "%s: D = %d > %lld", fn, D, (long long)GS_MAX_D);
   const int64_t big = int64_t(1) << 31;
   if (g->num_dst >= big || g->num_edges >= big) return fail(FAST_ERR_UNSUPPORTED, "%s: N or E >= 2^31", fn);
-  if (ldx >= big) return fail(FAST_ERR_UNSUPPORTED, "%s: %s >= 2^31", fn, ld_name);
+  if (ldx >= GS_MAX_LD) return fail(FAST_ERR_UNSUPPORTED, "%s: %s >= 2^26", fn, ld_name);
   if (g->num_edges * ldx >= (int64_t(1) << 56))
     return fail(FAST_ERR_UNSUPPORTED, "%s: %lld rows, %lld elements apart", fn, (long long)g->num_edges, (long long)ldx);
   if (g->num_dst > 0 && !g->dst_offsets) return fail(FAST_ERR_INVALID_ARG, "%s: NULL dst_offsets", fn);
@@ -563,8 +625,8 @@ static void gs_launch(const GsArgs& a, hipStream_t st) {
   if (a.direct + pieces > 0)
     hipLaunchKernelGGL((k_scan<T, VE, SPAN, BACK>), dim3(a.direct + pieces), dim3(GS_THREADS), 0, st, a);
   if (a.slots == 0) return;
-  hipLaunchKernelGGL((k_scan_chain<BACK>), dim3(uint32_t(a.slots), uint32_t((a.D + 63) / 64)), dim3(64 * GS_CHAIN), 0,
-                     st, a);
+  hipLaunchKernelGGL((k_scan_chain<BACK>), dim3(uint32_t((a.slots + GS_CHAIN - 1) / GS_CHAIN), uint32_t((a.D + 63) / 64)),
+                     dim3(64 * GS_CHAIN), 0, st, a);
   hipLaunchKernelGGL((k_scan_pieces<T, VE, SPAN, BACK>), dim3(pieces), dim3(GS_THREADS), 0, st, a);
 }
 template <bool BACK, typename T, int VE>
@@ -585,7 +647,7 @@ static fast_status_t gs_run(const char* fn, GsArgs& a, fast_dtype_t dtype, int64
   a.slots = p.slots;
   gs_layout(p.slots, a.D, static_cast<char*>(ws), &a);
   const int64_t direct = (a.N * a.C + GS_THREADS - 1) / GS_THREADS;
-  if (!grid_fits(direct + a.slots, GS_THREADS) || !grid_fits(a.slots, 64 * GS_CHAIN))
+  if (!grid_fits(direct + a.slots, GS_THREADS) || !grid_fits(a.slots / GS_CHAIN + 1, 64 * GS_CHAIN))
     return fail(FAST_ERR_UNSUPPORTED, "%s: 2^32 threads or more", fn);
   a.direct = uint32_t(direct);
   if (dtype == FAST_F32) {
