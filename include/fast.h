@@ -694,8 +694,7 @@ fast_status_t fast_edge_attention_fwd_cached(const fast_tcsr_t* g, int H, int dh
  * (spans of their rows that meet are refused).  Products of dtype's values are exact
  * or rounded to fp32, sums fp32.  Whatever n, ldx and the alignment, a row's result does
  * not depend on the other rows' values.
- * Limits: in, out <= 16384, n and the strides < 2^31, rows that span less than 2^56
- * elements, and fewer than 2^32 threads.
+ * Limits: in, out <= 16384, n < 2^31, strides < 2^22, and fewer than 2^32 threads.
  * ------------------------------------------------------------------------ */
 typedef enum {
   FAST_ACT_NONE = 0,

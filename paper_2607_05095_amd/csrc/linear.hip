@@ -12,15 +12,15 @@
 // Bound by HBM for narrow rows (n (in + out) elements), by the matrix units from a few
 // hundred columns on.
 #include <algorithm>
+#include <type_traits>
 
 #include "rows.h"
 
 namespace fast {
 
 constexpr int64_t LIN_MAX = 16384;        // columns
+constexpr int64_t LIN_MAX_LD = 1 << 22;   // elements from row to row: a tile's rows within 2^32 bytes
 constexpr int LIN_THREADS = 256;
-constexpr int LIN_KB = 128;               // bytes of k in a tile
-constexpr int LIN_ROW = LIN_KB + 16;      // LDS row: 16 lanes' chunks fall into different banks
 
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
@@ -35,21 +35,53 @@ __device__ __forceinline__ void lin_mma(float, const u32x4& a, const u32x4& b, f
     c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[j]), __uint_as_float(b[j]), c, 0, 0, 0);
 }
 
-// 16 bytes at p, of which n elements are in the row (zeros past them)
+// p[i] where p is the same for the whole wave and i elements are less than 2^32 bytes: the form that a
+// load takes as a scalar base and a 32-bit offset.
 template <typename T>
-__device__ __forceinline__ u32x4 lin_load(const T* p, int64_t n) {
-  if (n >= CHUNK<T>) {
-    const u32x4_e w = *reinterpret_cast<const u32x4_e*>(p);
-    return u32x4{w.x, w.y, w.z, w.w};
-  }
+__device__ __forceinline__ const T* at_offset(const T* p, uint32_t i) {
+  return reinterpret_cast<const T*>(reinterpret_cast<const char*>(p) + size_t(i * uint32_t(sizeof(T))));
+}
+
+// A row's end.  A chunk of k that reaches past it is loaded from far enough back to end with the
+// row, like all others in one instruction (a branch around a load is a wait for it), and its
+// first `skip` elements, which belong to the chunk before, are cleared in both operands.
+// Rows of less than a chunk are loaded element by element.
+template <typename T>
+__device__ __forceinline__ u32x4 lin_load(const T* p) {
+  const u32x4_e w = *reinterpret_cast<const u32x4_e*>(p);
+  return u32x4{w.x, w.y, w.z, w.w};
+}
+template <typename T>
+__device__ __forceinline__ u32x4 lin_load_short(const T* p, int n) {
   u32x4 w = {0u, 0u, 0u, 0u};
 #pragma unroll
-  for (int j = 0; j < CHUNK<T>; ++j)
+  for (int j = 0; j < CHUNK<T> - 1; ++j)
     if (j < n) {
       if constexpr (sizeof(T) == 4) w[j] = __float_as_uint(p[j]);
       else w[j / 2] |= uint32_t(p[j]) << (16 * (j & 1));
     }
   return w;
+}
+__device__ __forceinline__ void lin_unpack(float, const u32x4& w, float* x) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) x[j] = __uint_as_float(w[j]);
+}
+__device__ __forceinline__ void lin_unpack(uint16_t, const u32x4& w, float* x) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    x[2 * j] = bf16_lo(w[j]);
+    x[2 * j + 1] = bf16_hi(w[j]);
+  }
+}
+template <typename T>
+__device__ __forceinline__ u32x4 lin_mask(int skip) {
+  u32x4 m;
+#pragma unroll
+  for (int d = 0; d < 4; ++d) {
+    if constexpr (sizeof(T) == 4) m[d] = d >= skip ? ~0u : 0u;
+    else m[d] = 2 * d >= skip ? ~0u : (2 * d + 1 >= skip ? 0xffff0000u : 0u);
+  }
+  return m;
 }
 
 // ------------------------------------------------------------------ activations
@@ -92,61 +124,97 @@ struct LinArgs {
   int splits;                        // of one operand a; the same number behind them reads a2
   const void* a2;
   float* part;
+  float* sums;
 };
 
-// The epilogue of VE neighbouring columns from c on of row r.
-template <typename T, int VE>
-__device__ __forceinline__ void lin_finish(const LinArgs& p, int64_t r, int c, float* z) {
-  const int n = p.M - c;
-  if (r >= p.n || n <= 0) return;
-  if (p.bias) {
-#pragma unroll
-    for (int j = 0; j < VE; ++j)
-      if (j < n) z[j] += p.bias[c + j];
-  }
-  T* pre = p.pre ? static_cast<T*>(p.pre) + r * p.M + c : nullptr;
-  const T* res = p.res ? static_cast<const T*>(p.res) + r * p.ldres + c : nullptr;
-  T* y = static_cast<T*>(p.y) + r * p.ldy + c;
-  if constexpr (VE == CHUNK<T>) {
-    if (pre) store_chunk(pre, n, z);
-#pragma unroll
-    for (int j = 0; j < VE; ++j) z[j] = act_of(p.act, z[j]);
-    if (res) {
-      float t[VE];
-      load_chunk(res, n, t);
-#pragma unroll
-      for (int j = 0; j < VE; ++j) z[j] += t[j];
-    }
-    store_chunk(y, n, z);
-  } else {
-#pragma unroll
-    for (int j = 0; j < VE; ++j)
-      if (j < n) {
-        float t;
-        if (pre) VecIO<T, 1>::store(pre + j, &z[j]);
-        z[j] = act_of(p.act, z[j]);
-        if (res) {
-          VecIO<T, 1>::load(res + j, &t);
-          z[j] += t;
-        }
-        VecIO<T, 1>::store(y + j, &z[j]);
-      }
+// f(integral_constant) for 0 .. N-1: an array of accumulators stays in registers only if every
+// index is a constant.
+template <int N, typename F>
+__device__ __forceinline__ void lin_each(F f) {
+  if constexpr (N > 0) {
+    lin_each<N - 1>(f);
+    f(std::integral_constant<int, N - 1>());
   }
 }
 
-// A wave's part of a tile: TR x TC blocks of 32 x 32 over a tile of k in LDS.
-template <typename T, int TR, int TC>
-__device__ __forceinline__ void lin_step(const char* la, const char* lb, f32x16_t (&acc)[TR][TC]) {
-  const int lane = threadIdx.x & 63;
-  la += (lane & 31) * LIN_ROW + (lane >> 5) * 16;
-  lb += (lane & 31) * LIN_ROW + (lane >> 5) * 16;
+// The epilogue of a lane: VE neighbouring columns, the same in every row that it finishes.
+template <typename T, int VE>
+struct LinEnd {
+  const LinArgs& p;
+  int c, n;                          // first column, columns in the row
+  float bias[VE];
+  __device__ LinEnd(const LinArgs& p_, int c_) : p(p_), c(c_), n(p_.M - c_) {
 #pragma unroll
-  for (int k = 0; k < LIN_KB; k += 32) {
+    for (int j = 0; j < VE; ++j) bias[j] = p.bias && j < n ? p.bias[c + j] : 0.f;
+  }
+  __device__ void finish(int64_t r, float* z) const {
+    if (r >= p.n || n <= 0) return;
+    float t[VE];
+    const T* res = p.res ? static_cast<const T*>(p.res) + r * p.ldres + c : nullptr;
+    T* pre = p.pre ? static_cast<T*>(p.pre) + r * p.M + c : nullptr;
+    T* y = static_cast<T*>(p.y) + r * p.ldy + c;
+    if constexpr (VE == CHUNK<T>) {
+      if (res) load_chunk(res, n, t);
+    } else {
+#pragma unroll
+      for (int j = 0; j < VE; ++j) {
+        t[j] = 0.f;
+        if (res && j < n) VecIO<T, 1>::load(res + j, &t[j]);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < VE; ++j) z[j] += bias[j];
+    if (pre) put(pre, z);
+    if (p.act != FAST_ACT_NONE) {
+#pragma unroll
+      for (int j = 0; j < VE; ++j) z[j] = act_of(p.act, z[j]);
+    }
+    if (res) {
+#pragma unroll
+      for (int j = 0; j < VE; ++j) z[j] += t[j];
+    }
+    put(y, z);
+  }
+  __device__ void put(T* o, const float* z) const {
+    if constexpr (VE == CHUNK<T>) {
+      store_chunk(o, n, z);
+    } else {
+#pragma unroll
+      for (int j = 0; j < VE; ++j)
+        if (j < n) VecIO<T, 1>::store(o + j, &z[j]);
+    }
+  }
+};
+
+// The tiles of a workgroup: WR x WC waves of TR x TC blocks of 32 x 32 each, KB bytes of k.
+template <int WR_, int WC_, int TR_, int TC_, int KB_>
+struct LinTile {
+  static constexpr int WR = WR_, WC = WC_, TR = TR_, TC = TC_, KB = KB_;
+  static constexpr int THREADS = 64 * WR * WC, BR = 32 * WR * TR, BC = 32 * WC * TC;
+  static constexpr int CHUNKS = KB / 16;                       // of a row of LDS
+  static constexpr int ROW = KB + 16;                          // 16 lanes' chunks fall into different banks
+  static constexpr int BUF = (BR + BC) * ROW;                  // a tile of k of both operands
+  // (the epilogue takes 32 rows of every wave's block through it)
+  static constexpr int LDS = 2 * BUF > WR * WC * 32 * (TC * 32 + 4) * 4 ? 2 * BUF : WR * WC * 32 * (TC * 32 + 4) * 4;
+};
+typedef LinTile<2, 4, 4, 2, 128> LinBig;   // 256 x 256
+typedef LinTile<2, 2, 2, 2, 64> LinMid;    // 128 x 128
+typedef LinTile<2, 2, 2, 2, 128> LinGrad;  // 128 x 128 of weight gradients
+
+// A wave's part of a tile: TR x TC blocks of 32 x 32 over a tile of k in LDS.
+template <typename T, typename Tile>
+__device__ __forceinline__ void lin_step(const char* la, const char* lb, f32x16_t (&acc)[Tile::TR][Tile::TC]) {
+  constexpr int TR = Tile::TR, TC = Tile::TC, ROW = Tile::ROW;
+  const int lane = threadIdx.x & 63;
+  la += (lane & 31) * ROW + (lane >> 5) * 16;
+  lb += (lane & 31) * ROW + (lane >> 5) * 16;
+#pragma unroll
+  for (int k = 0; k < Tile::KB; k += 32) {
     u32x4 fa[TR], fb[TC];
 #pragma unroll
-    for (int i = 0; i < TR; ++i) fa[i] = *reinterpret_cast<const u32x4*>(la + i * 32 * LIN_ROW + k);
+    for (int i = 0; i < TR; ++i) fa[i] = *reinterpret_cast<const u32x4*>(la + i * 32 * ROW + k);
 #pragma unroll
-    for (int j = 0; j < TC; ++j) fb[j] = *reinterpret_cast<const u32x4*>(lb + j * 32 * LIN_ROW + k);
+    for (int j = 0; j < TC; ++j) fb[j] = *reinterpret_cast<const u32x4*>(lb + j * 32 * ROW + k);
 #pragma unroll
     for (int i = 0; i < TR; ++i)
 #pragma unroll
@@ -155,14 +223,14 @@ __device__ __forceinline__ void lin_step(const char* la, const char* lb, f32x16_
 }
 
 // The wave's block through LDS, 32 rows at a time, so that rows leave in whole chunks.
-// out(row of the wave's block, column, values).
+// out(row of the wave's block, values): of VE columns from (lane % (TC * 32 / VE)) * VE on.
 template <int VE, int TR, int TC, typename F>
 __device__ __forceinline__ void lin_out(char* lds, const f32x16_t (&acc)[TR][TC], F out) {
-  constexpr int W = TC * 32, LD = W + 4, PER = W / VE;
+  constexpr int W = TC * 32, LD = W + 4, PER = W / VE, ROWS = 64 / PER;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   float* buf = reinterpret_cast<float*>(lds) + wave * 32 * LD;
-#pragma unroll
-  for (int i = 0; i < TR; ++i) {
+  lin_each<TR>([&](auto I) {
+    constexpr int i = decltype(I)::value;
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < TC; ++j)
@@ -171,64 +239,74 @@ __device__ __forceinline__ void lin_out(char* lds, const f32x16_t (&acc)[TR][TC]
         *reinterpret_cast<f32x4*>(buf + (lane & 31) * LD + j * 32 + q * 8 + (lane >> 5) * 4) =
             f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
     __syncthreads();
-#pragma unroll
-    for (int t = lane; t < 32 * PER; t += 64) {
-      const int r = t / PER, c = t % PER * VE;
+#pragma unroll 2
+    for (int q = 0; q < 32 / ROWS; ++q) {
+      const int r = q * ROWS + lane / PER, c = lane % PER * VE;
       float z[VE];
 #pragma unroll
       for (int v = 0; v < VE; v += 4) {
         const f32x4 w = *reinterpret_cast<const f32x4*>(buf + r * LD + c + v);
         z[v] = w.x; z[v + 1] = w.y; z[v + 2] = w.z; z[v + 3] = w.w;
       }
-      out(i * 32 + r, c, z);
+      out(i * 32 + r, z);
     }
-  }
+  });
 }
 
-// Tiles of BR rows and BC columns, four waves of 2 x 2; the next tile of k is on its way
-// into registers while this one is multiplied from LDS.
-template <typename T, int TR, int TC>
-__global__ void __launch_bounds__(LIN_THREADS) k_linear(LinArgs p) {
-  constexpr int BR = TR * 64, BC = TC * 64, VE = CHUNK<T>, BK = LIN_KB / int(sizeof(T));
-  constexpr int NA = BR / 32, NB = BC / 32, BUF = (BR + BC) * LIN_ROW;
-  __shared__ __attribute__((aligned(16))) char lds[2 * BUF];
+// Tiles of BR rows and BC columns; the next tile of k is on its way into registers while this
+// one is multiplied from LDS.  SHORT: rows of less than a chunk.
+template <typename T, typename Tile, bool SHORT>
+__global__ void __launch_bounds__(Tile::THREADS) k_linear(LinArgs p) {
+  constexpr int TR = Tile::TR, TC = Tile::TC, BR = Tile::BR, BC = Tile::BC, BUF = Tile::BUF;
+  constexpr int VE = CHUNK<T>, BK = Tile::KB / int(sizeof(T)), STEP = Tile::THREADS / Tile::CHUNKS;
+  constexpr int NA = BR / STEP, NB = BC / STEP;
+  __shared__ __attribute__((aligned(16))) char lds[Tile::LDS];
   const uint32_t id = xcd_tile(blockIdx.x, gridDim.x);
   const int64_t r0 = int64_t(id / uint32_t(p.tiles_c)) * BR;
   const int c0 = int(id % uint32_t(p.tiles_c)) * BC;
-  const int row = threadIdx.x >> 3, chunk = threadIdx.x & 7;
-  const T* ga[NA];
-  const T* gb[NB];
+  const int row = threadIdx.x / Tile::CHUNKS, chunk = threadIdx.x % Tile::CHUNKS;
+  // places as 32-bit offsets from the tile's corner, which is the same for the whole workgroup
+  const T* A = static_cast<const T*>(p.a) + r0 * p.lda;
+  const T* B = static_cast<const T*>(p.b) + int64_t(c0) * p.ldb;
+  uint32_t oa[NA], ob[NB];
 #pragma unroll
-  for (int i = 0; i < NA; ++i) {
-    const int64_t r = r0 + i * 32 + row;
-    ga[i] = static_cast<const T*>(p.a) + (r < p.n ? r : p.n - 1) * p.lda + chunk * VE;
-  }
+  for (int i = 0; i < NA; ++i)
+    oa[i] = uint32_t(min(int64_t(i * STEP + row), p.n - 1 - r0)) * uint32_t(p.lda);
 #pragma unroll
-  for (int i = 0; i < NB; ++i) {
-    const int c = c0 + i * 32 + row;
-    gb[i] = static_cast<const T*>(p.b) + int64_t(c < p.M ? c : p.M - 1) * p.ldb + chunk * VE;
-  }
+  for (int i = 0; i < NB; ++i) ob[i] = uint32_t(min(i * STEP + row, p.M - 1 - c0)) * uint32_t(p.ldb);
+  const int K = int(p.K), full = K / BK, tiles = (K + BK - 1) / BK;
+  // this thread's chunk of the last tile, where that is not full
+  const int last = full * BK + chunk * VE, back = min(last, K - VE);
+  const u32x4 mask = lin_mask<T>(last - back);
   u32x4 ra[NA], rb[NB];
-  auto load = [&](int64_t k) {
-    if (k + BK <= p.K) {
+  auto load = [&](int t) {
+    if constexpr (SHORT) {
 #pragma unroll
-      for (int i = 0; i < NA; ++i) ra[i] = lin_load(ga[i] + k, VE);
+      for (int i = 0; i < NA; ++i) ra[i] = lin_load_short(A + oa[i], chunk == 0 ? K : 0);
 #pragma unroll
-      for (int i = 0; i < NB; ++i) rb[i] = lin_load(gb[i] + k, VE);
+      for (int i = 0; i < NB; ++i) rb[i] = lin_load_short(B + ob[i], chunk == 0 ? K : 0);
     } else {
-      const int64_t left = p.K - k - chunk * VE;
+      const uint32_t k = t < full ? chunk * VE : back;
+      const T* pa = A + (t < full ? t * BK : 0);
+      const T* pb = B + (t < full ? t * BK : 0);
 #pragma unroll
-      for (int i = 0; i < NA; ++i) ra[i] = lin_load(ga[i] + k, left);
+      for (int i = 0; i < NA; ++i) ra[i] = lin_load(at_offset(pa, oa[i] + k));
 #pragma unroll
-      for (int i = 0; i < NB; ++i) rb[i] = lin_load(gb[i] + k, left);
+      for (int i = 0; i < NB; ++i) rb[i] = lin_load(at_offset(pb, ob[i] + k));
     }
   };
-  auto put = [&](char* buf) {
-    char* at = buf + row * LIN_ROW + chunk * 16;
+  auto put = [&](int t, char* buf) {
+    char* at = buf + row * Tile::ROW + chunk * 16;
+    if (!SHORT && t >= full) {
 #pragma unroll
-    for (int i = 0; i < NA; ++i) *reinterpret_cast<u32x4*>(at + i * 32 * LIN_ROW) = ra[i];
+      for (int i = 0; i < NA; ++i) ra[i] &= mask;
 #pragma unroll
-    for (int i = 0; i < NB; ++i) *reinterpret_cast<u32x4*>(at + (BR + i * 32) * LIN_ROW) = rb[i];
+      for (int i = 0; i < NB; ++i) rb[i] &= mask;
+    }
+#pragma unroll
+    for (int i = 0; i < NA; ++i) *reinterpret_cast<u32x4*>(at + i * STEP * Tile::ROW) = ra[i];
+#pragma unroll
+    for (int i = 0; i < NB; ++i) *reinterpret_cast<u32x4*>(at + (BR + i * STEP) * Tile::ROW) = rb[i];
   };
   f32x16_t acc[TR][TC];
 #pragma unroll
@@ -237,55 +315,66 @@ __global__ void __launch_bounds__(LIN_THREADS) k_linear(LinArgs p) {
     for (int j = 0; j < TC; ++j)
 #pragma unroll
       for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.f;
-  const int wave = threadIdx.x >> 6, wr = wave >> 1, wc = wave & 1;
+  const int wave = threadIdx.x >> 6, wr = wave / Tile::WC, wc = wave % Tile::WC;
   load(0);
-  put(lds);
+  put(0, lds);
   __syncthreads();
   int cur = 0;
-  for (int64_t k = 0; k < p.K; k += BK) {
-    const bool more = k + BK < p.K;
-    if (more) load(k + BK);
+  for (int t = 0; t < tiles; ++t) {
+    const bool more = t + 1 < tiles;
+    if (more) load(t + 1);
     const char* buf = lds + cur * BUF;
-    lin_step<T, TR, TC>(buf + wr * TR * 32 * LIN_ROW, buf + (BR + wc * TC * 32) * LIN_ROW, acc);
+    lin_step<T, Tile>(buf + wr * TR * 32 * Tile::ROW, buf + (BR + wc * TC * 32) * Tile::ROW, acc);
     cur ^= 1;
-    if (more) put(lds + cur * BUF);
+    if (more) put(t + 1, lds + cur * BUF);
     __syncthreads();
   }
-  lin_out<VE>(lds, acc, [&](int r, int c, float* z) {
-    lin_finish<T, VE>(p, r0 + wr * TR * 32 + r, c0 + wc * TC * 32 + c, z);
-  });
+  const LinEnd<T, VE> end(p, c0 + wc * TC * 32 + (threadIdx.x & 63) % (TC * 32 / VE) * VE);
+  lin_out<VE>(lds, acc, [&](int r, float* z) { end.finish(r0 + wr * TR * 32 + r, z); });
 }
 
 // Few rows: 32 x 32 results a workgroup, its waves share k, each feeding the matrix unit from
 // global memory; their sums are added in order in LDS.
-template <typename T, int WAVES>
+template <typename T, int WAVES, bool SHORT>
 __global__ void __launch_bounds__(64 * WAVES) k_linear_few(LinArgs p) {
-  constexpr int VE = CHUNK<T>, STEP = 2 * VE, LD = 36, AHEAD = 4;
+  constexpr int VE = CHUNK<T>, STEP = 2 * VE, LD = 36, AHEAD = 4, ROUND = AHEAD * WAVES * STEP;
   __shared__ float buf[WAVES][32 * LD];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
   const int64_t r0 = int64_t(blockIdx.x / uint32_t(p.tiles_c)) * 32;
-  const int c0 = int(blockIdx.x % uint32_t(p.tiles_c)) * 32;
+  const int c0 = int(blockIdx.x % uint32_t(p.tiles_c)) * 32, K = int(p.K);
   const int64_t r = min(r0 + (lane & 31), p.n - 1);
   const int c = min(c0 + (lane & 31), p.M - 1);
-  const T* ga = static_cast<const T*>(p.a) + r * p.lda + (lane >> 5) * VE;
-  const T* gb = static_cast<const T*>(p.b) + int64_t(c) * p.ldb + (lane >> 5) * VE;
+  const T* ga = static_cast<const T*>(p.a) + r * p.lda;
+  const T* gb = static_cast<const T*>(p.b) + int64_t(c) * p.ldb;
   f32x16_t acc;
 #pragma unroll
   for (int q = 0; q < 16; ++q) acc[q] = 0.f;
-  for (int64_t k = int64_t(wave) * STEP; k < p.K; k += int64_t(AHEAD) * WAVES * STEP) {
-    u32x4 fa[AHEAD], fb[AHEAD];
+  if constexpr (SHORT) {
+    if (wave == 0) lin_mma(T(), lin_load_short(gb, half ? 0 : K), lin_load_short(ga, half ? 0 : K), acc);
+  } else {
+    for (int k = wave * STEP + half * VE; k - half * VE < K; k += ROUND) {
+      u32x4 fa[AHEAD], fb[AHEAD];
 #pragma unroll
-    for (int s = 0; s < AHEAD; ++s) {
-      const int64_t at = k + int64_t(s) * WAVES * STEP, left = p.K - at - (lane >> 5) * VE;
-      fa[s] = lin_load(ga + at, left);
-      fb[s] = lin_load(gb + at, left);
+      for (int s = 0; s < AHEAD; ++s) {
+        const int at = min(k + s * WAVES * STEP, K - VE);
+        fa[s] = lin_load(ga + at);
+        fb[s] = lin_load(gb + at);
+      }
+#pragma unroll
+      for (int s = 0; s < AHEAD; ++s) {
+        const int at = k + s * WAVES * STEP;
+        if (at - half * VE + STEP > K) {                   // (the same for the whole wave)
+          const u32x4 m = lin_mask<T>(at - min(at, K - VE));
+          fa[s] &= m;
+          fb[s] &= m;
+        }
+        lin_mma(T(), fb[s], fa[s], acc);
+      }
     }
-#pragma unroll
-    for (int s = 0; s < AHEAD; ++s) lin_mma(T(), fb[s], fa[s], acc);
   }
 #pragma unroll
   for (int q = 0; q < 4; ++q)
-    *reinterpret_cast<f32x4*>(&buf[wave][(lane & 31) * LD + q * 8 + (lane >> 5) * 4]) =
+    *reinterpret_cast<f32x4*>(&buf[wave][(lane & 31) * LD + q * 8 + half * 4]) =
         f32x4{acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]};
   __syncthreads();
   constexpr int VO = 16 / WAVES;
@@ -293,10 +382,12 @@ __global__ void __launch_bounds__(64 * WAVES) k_linear_few(LinArgs p) {
   float z[VO];
 #pragma unroll
   for (int v = 0; v < VO; ++v) z[v] = 0.f;
+#pragma unroll
   for (int w = 0; w < WAVES; ++w)
 #pragma unroll
     for (int v = 0; v < VO; ++v) z[v] += buf[w][t / 32 * LD + t % 32 + v];
-  lin_finish<T, VO>(p, r0 + t / 32, c0 + t % 32, z);
+  const LinEnd<T, VO> end(p, c0 + t % 32);
+  end.finish(r0 + t / 32, z);
 }
 
 // ------------------------------------------------------------------ weight gradients
@@ -306,43 +397,84 @@ template <typename T> struct LinTurn;
 template <> struct LinTurn<uint16_t> {        // 2 columns of 8 rows
   static constexpr int COLS = 2, ROWS = 8;
   uint32_t w[8];
-  __device__ void load(const uint16_t* p, int64_t ld, bool pair, int64_t rows) {
+  // Of an odd width the last column is loaded with the one before; width 1: alone.
+  uint32_t at;
+  int shift;
+  __device__ void place(int col, int width) {
+    const int c = min(col, width - 1);
+    shift = c + 1 < width || width == 1 ? 0 : 16;
+    at = uint32_t(c - (shift ? 1 : 0));
+  }
+  // rows row, row + 1, ... of p; END: row `last` again from there on; ONE: width 1
+  template <bool END, bool ONE>
+  __device__ void load(const uint16_t* p, uint32_t ld, int row, int last) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      w[j] = 0u;
-      if (j < rows) w[j] = pair ? *reinterpret_cast<const u32_e*>(p + j * ld) : uint32_t(p[j * ld]);
+      const uint16_t* q = END ? at_offset(p, at + uint32_t(min(row + j, last)) * ld) : at_offset(p + j * size_t(ld), at + row * ld);
+      if constexpr (ONE) w[j] = *q;
+      else w[j] = *reinterpret_cast<const u32_e*>(q);
     }
   }
-  __device__ void put(char* at) const {
+  // rows past the end count nothing
+  __device__ void trim(int64_t rows) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) w[j] = j < rows ? w[j] >> shift : 0u;
+  }
+  template <int ROW>
+  __device__ void put(char* o) const {
     u32x4 lo, hi;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       lo[j] = __builtin_amdgcn_perm(w[2 * j + 1], w[2 * j], 0x05040100u);
       hi[j] = __builtin_amdgcn_perm(w[2 * j + 1], w[2 * j], 0x07060302u);
     }
-    *reinterpret_cast<u32x4*>(at) = lo;
-    *reinterpret_cast<u32x4*>(at + LIN_ROW) = hi;
+    *reinterpret_cast<u32x4*>(o) = lo;
+    *reinterpret_cast<u32x4*>(o + ROW) = hi;
+  }
+  __device__ void add(float* s) const {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      s[0] += bf16_lo(w[j]);
+      s[1] += bf16_hi(w[j]);
+    }
   }
 };
 template <> struct LinTurn<float> {           // a column of 4 rows
   static constexpr int COLS = 1, ROWS = 4;
-  uint32_t w[4];
-  __device__ void load(const float* p, int64_t ld, bool, int64_t rows) {
+  float w[4];
+  uint32_t at;
+  __device__ void place(int col, int width) { at = uint32_t(min(col, width - 1)); }
+  template <bool END, bool ONE>
+  __device__ void load(const float* p, uint32_t ld, int row, int last) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) w[j] = j < rows ? __float_as_uint(p[j * ld]) : 0u;
+    for (int j = 0; j < 4; ++j)
+      w[j] = END ? *at_offset(p, at + uint32_t(min(row + j, last)) * ld) : *at_offset(p + j * size_t(ld), at + row * ld);
   }
-  __device__ void put(char* at) const { *reinterpret_cast<u32x4*>(at) = u32x4{w[0], w[1], w[2], w[3]}; }
+  __device__ void trim(int64_t rows) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = j < rows ? w[j] : 0.f;
+  }
+  template <int ROW>
+  __device__ void put(char* o) const { *reinterpret_cast<f32x4*>(o) = f32x4{w[0], w[1], w[2], w[3]}; }
+  __device__ void add(float* s) const {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) s[0] += w[j];
+  }
 };
 
-// p.a: dz [K, n] (n columns, lda apart), p.b: x [K, M]; part[split][n][M].
-template <typename T>
-__global__ void __launch_bounds__(LIN_THREADS) k_linear_wgrad(LinArgs p) {
-  constexpr int TR = 2, TC = 2, BR = TR * 64, BC = TC * 64, BK = LIN_KB / int(sizeof(T));
+// p.a: dz [K, n] (n columns, lda apart), p.b: x [K, M]; PRODUCT: part[split][n][M]; sums (NULL for
+// none): from the workgroups of the first tile of columns, sums[split][n] of dz's columns.
+// ONE: n or M is 1.
+template <typename T, typename Tile, bool PRODUCT, bool ONE>
+__global__ void __launch_bounds__(Tile::THREADS) k_linear_wgrad(LinArgs p) {
+  constexpr int TR = Tile::TR, TC = Tile::TC, BR = Tile::BR, BC = Tile::BC, BUF = Tile::BUF;
+  constexpr int BK = Tile::KB / int(sizeof(T));
   typedef LinTurn<T> Turn;
-  constexpr int GRP = BR / Turn::COLS;                  // column groups of an operand's tile
-  constexpr int NT = GRP * 8 / LIN_THREADS;             // pieces per thread and operand
-  constexpr int BUF = (BR + BC) * LIN_ROW;
-  __shared__ __attribute__((aligned(16))) char lds[2 * BUF];
+    // an operand's tile: column groups, pieces per thread, chunks between a thread's pieces
+  constexpr int GA = BR / Turn::COLS, NTA = GA * Tile::CHUNKS / Tile::THREADS, NEXTA = Tile::THREADS / GA;
+  constexpr int GB = BC / Turn::COLS, NTB = GB * Tile::CHUNKS / Tile::THREADS, NEXTB = Tile::THREADS / GB;
+  static_assert(NTA * NEXTA == Tile::CHUNKS && NTB * NEXTB == Tile::CHUNKS, "whole pieces");
+  __shared__ __attribute__((aligned(16))) char lds[Tile::LDS];
   const uint32_t id = xcd_tile(blockIdx.x, gridDim.x);
   const uint32_t tiles_r = uint32_t((p.n + BR - 1) / BR), tiles = tiles_r * uint32_t(p.tiles_c);
   const uint32_t split = id / tiles, tile = id % tiles;
@@ -351,26 +483,65 @@ __global__ void __launch_bounds__(LIN_THREADS) k_linear_wgrad(LinArgs p) {
   const T* A = static_cast<const T*>(second ? p.a2 : p.a);
   const T* B = static_cast<const T*>(p.b);
   const int64_t k0 = int64_t(second ? split - p.splits : split) * p.rows, k1 = min(k0 + p.rows, p.K);
-  const int grp = threadIdx.x % GRP, first = threadIdx.x / GRP;
-  constexpr int NEXT = LIN_THREADS / GRP;               // chunks between a thread's pieces
-  const int width = int(p.n);
-  const int ca = min(r0 + grp * Turn::COLS, width - 1), cb = min(c0 + grp * Turn::COLS, p.M - 1);
-  const bool pa = ca + 1 < width, pb = cb + 1 < p.M;
-  Turn ta[NT], tb[NT];
-  auto load = [&](int64_t k) {
+  const int grpa = threadIdx.x % GA, firsta = threadIdx.x / GA, grpb = threadIdx.x % GB, firstb = threadIdx.x / GB;
+  const bool sums = p.sums && c0 == 0;
+  Turn ta[NTA], tb[NTB];
 #pragma unroll
-    for (int i = 0; i < NT; ++i) {
-      const int64_t at = k + (first + i * NEXT) * Turn::ROWS;
-      ta[i].load(A + at * p.lda + ca, p.lda, pa, k1 - at);
-      tb[i].load(B + at * p.ldb + cb, p.ldb, pb, k1 - at);
+  for (int i = 0; i < NTA; ++i) ta[i].place(r0 + grpa * Turn::COLS, int(p.n));
+  if (PRODUCT) {
+#pragma unroll
+    for (int i = 0; i < NTB; ++i) tb[i].place(c0 + grpb * Turn::COLS, p.M);
+  }
+  // END: the tile that the split ends in
+  auto load = [&](int64_t k, auto end) {
+    constexpr bool END = decltype(end)::value;
+    const int last = int(k1 - 1 - k);
+    const T* a = A + k * p.lda;
+    const T* b = PRODUCT ? B + k * p.ldb : nullptr;
+#pragma unroll
+    for (int i = 0; i < NTA; ++i) {
+      const int row = (firsta + i * NEXTA) * Turn::ROWS;
+      if (ONE && p.n == 1) ta[i].template load<END, true>(a, uint32_t(p.lda), row, last);
+      else ta[i].template load<END, false>(a, uint32_t(p.lda), row, last);
+    }
+    if constexpr (PRODUCT) {
+#pragma unroll
+      for (int i = 0; i < NTB; ++i) {
+        const int row = (firstb + i * NEXTB) * Turn::ROWS;
+        if (ONE && p.M == 1) tb[i].template load<END, true>(b, uint32_t(p.ldb), row, last);
+        else tb[i].template load<END, false>(b, uint32_t(p.ldb), row, last);
+      }
     }
   };
-  auto put = [&](char* buf) {
+  double sum[Turn::COLS];                               // (a tile's in fp32)
 #pragma unroll
-    for (int i = 0; i < NT; ++i) {
-      char* at = buf + grp * Turn::COLS * LIN_ROW + (first + i * NEXT) * 16;
-      ta[i].put(at);
-      tb[i].put(at + BR * LIN_ROW);
+  for (int j = 0; j < Turn::COLS; ++j) sum[j] = 0.0;
+  const bool odd = sizeof(T) == 2 && ((p.n | p.M) & 1);  // a last column to be shifted into place
+  auto put = [&](int64_t k, char* buf) {
+    if (odd || k + BK > k1) {
+#pragma unroll
+      for (int i = 0; i < NTA; ++i) ta[i].trim(k1 - k - (firsta + i * NEXTA) * Turn::ROWS);
+      if (PRODUCT) {
+#pragma unroll
+        for (int i = 0; i < NTB; ++i) tb[i].trim(k1 - k - (firstb + i * NEXTB) * Turn::ROWS);
+      }
+    }
+    if (sums) {
+      float s[Turn::COLS];
+#pragma unroll
+      for (int j = 0; j < Turn::COLS; ++j) s[j] = 0.f;
+#pragma unroll
+      for (int i = 0; i < NTA; ++i) ta[i].add(s);
+#pragma unroll
+      for (int j = 0; j < Turn::COLS; ++j) sum[j] += s[j];
+    }
+    if constexpr (PRODUCT) {
+#pragma unroll
+      for (int i = 0; i < NTA; ++i)
+        ta[i].template put<Tile::ROW>(buf + grpa * Turn::COLS * Tile::ROW + (firsta + i * NEXTA) * 16);
+#pragma unroll
+      for (int i = 0; i < NTB; ++i)
+        tb[i].template put<Tile::ROW>(buf + (BR + grpb * Turn::COLS) * Tile::ROW + (firstb + i * NEXTB) * 16);
     }
   };
   f32x16_t acc[TR][TC];
@@ -380,85 +551,141 @@ __global__ void __launch_bounds__(LIN_THREADS) k_linear_wgrad(LinArgs p) {
     for (int j = 0; j < TC; ++j)
 #pragma unroll
       for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.f;
-  const int wave = threadIdx.x >> 6, wr = wave >> 1, wc = wave & 1;
-  load(k0);
-  put(lds);
-  __syncthreads();
+  const int wave = threadIdx.x >> 6, wr = wave / Tile::WC, wc = wave % Tile::WC;
+  auto multiply = [&](const char* buf) {
+    if constexpr (PRODUCT)
+      lin_step<T, Tile>(buf + wr * TR * 32 * Tile::ROW, buf + (BR + wc * TC * 32) * Tile::ROW, acc);
+  };
+  typedef std::integral_constant<bool, false> Whole;
+  typedef std::integral_constant<bool, true> End;
+  const int64_t full = k1 > k0 ? (k1 - k0) / BK : 0;    // (a split past the end adds zeros)
+  int64_t k = k0;
   int cur = 0;
-  for (int64_t k = k0; k < k1; k += BK) {
-    const bool more = k + BK < k1;
-    if (more) load(k + BK);
-    const char* buf = lds + cur * BUF;
-    lin_step<T, TR, TC>(buf + wr * TR * 32 * LIN_ROW, buf + (BR + wc * TC * 32) * LIN_ROW, acc);
-    cur ^= 1;
-    if (more) put(lds + cur * BUF);
+  if (full > 0) {
+    load(k, Whole());
+    put(k, lds);
+    __syncthreads();
+    for (int64_t t = 0; t < full; ++t, k += BK) {
+      const bool more = t + 1 < full;
+      if (more) load(k + BK, Whole());
+      multiply(lds + cur * BUF);
+      cur ^= 1;
+      if (more) put(k + BK, lds + cur * BUF);
+      __syncthreads();
+    }
+  }
+  if (k < k1) {
+    load(k, End());
+    put(k, lds + cur * BUF);
+    __syncthreads();
+    multiply(lds + cur * BUF);
     __syncthreads();
   }
-  float* part = p.part + int64_t(split) * p.n * p.M;
-  lin_out<4>(lds, acc, [&](int r, int c, float* z) {
-    const int64_t row = r0 + wr * TR * 32 + r;
-    const int col = c0 + wc * TC * 32 + c;
-    if (row < p.n && col < p.M) store_chunk_of(part + row * p.M + col, p.M - col, z);
-  });
+  if constexpr (PRODUCT) {
+    float* part = p.part + int64_t(split) * p.n * p.M;
+    const int col = c0 + wc * TC * 32 + (threadIdx.x & 63) % (TC * 8) * 4;
+    lin_out<4>(lds, acc, [&](int r, float* z) {
+      const int64_t row = r0 + wr * TR * 32 + r;
+      if (row < p.n && col < p.M) store_chunk_of(part + row * p.M + col, p.M - col, z);
+    });
+  }
+  if (sums) {                                           // the threads of a column group, in order
+    __syncthreads();
+    double* s = reinterpret_cast<double*>(lds);
+#pragma unroll
+    for (int j = 0; j < Turn::COLS; ++j) s[firsta * BR + grpa * Turn::COLS + j] = sum[j];
+    __syncthreads();
+    for (int c = threadIdx.x; c < BR && r0 + c < p.n; c += Tile::THREADS) {
+      double x = 0.0;
+      for (int f = 0; f < NEXTA; ++f) x += s[f * BR + c];
+      p.sums[int64_t(split) * p.n + r0 + c] = float(x);
+    }
+  }
 }
 
-// dz = dy act'(pre) (bf16: the nearest value and what is left, 16 bits of it together),
-// and the sums of its columns over the workgroup's rows.
-constexpr int DZ_ROWS = 256, DZ_COLS = 64;             // rows and 16-byte chunks of a workgroup
+// dz = dy act'(pre) (bf16: the nearest value and what is left, 16 bits of it together) and its
+// columns' sums: a workgroup takes DZ_ROWS rows and up to 256 chunks of columns, a thread one chunk
+// of every `groups`-th row, DZ_AHEAD of them loaded together.  A row's last chunk starts early
+// enough to end with it (both writers of an element write the same value; one counts it).
+// SHORT: rows of less than a chunk.
+constexpr int DZ_AHEAD = 4, DZ_ROWS = 64;
 struct DzArgs {
   int64_t n, lddy;
   int M, act;
+  int chunks, lanes;                                    // of a row; of them in a workgroup
   const void* dy;
   const void* pre;
   void* dz;
   void* rest;
   float* sums;                                          // [row blocks][M], or NULL
 };
-template <typename T>
+template <typename T, bool SHORT>
 __global__ void __launch_bounds__(LIN_THREADS) k_linear_dz(DzArgs p) {
-  constexpr int VE = CHUNK<T>, WAVES = LIN_THREADS / 64;
-  __shared__ float s[WAVES][DZ_COLS * VE];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int c = (blockIdx.y * DZ_COLS + lane) * VE, n = p.M - c;
+  constexpr int VE = CHUNK<T>;
+  __shared__ float s[LIN_THREADS * VE];
+  const int groups = LIN_THREADS / p.lanes, lane = threadIdx.x % p.lanes, g = threadIdx.x / p.lanes;
+  const int chunk = blockIdx.y * p.lanes + lane;
+  const bool in = g < groups && chunk < p.chunks;
+  const int c = SHORT ? 0 : min(chunk * VE, p.M - VE), skip = SHORT ? 0 : chunk * VE - c, n = SHORT ? p.M : VE;
   const int64_t r0 = int64_t(blockIdx.x) * DZ_ROWS, r1 = min(r0 + DZ_ROWS, p.n);
   float sum[VE];
 #pragma unroll
   for (int j = 0; j < VE; ++j) sum[j] = 0.f;
-  if (n > 0) {
-#pragma unroll 4
-    for (int64_t r = r0 + wave; r < r1; r += WAVES) {
-      float d[VE];
-      load_chunk(static_cast<const T*>(p.dy) + r * p.lddy + c, n, d);
-      if (p.act != FAST_ACT_NONE) {
-        float z[VE], t[VE];
-        load_chunk(static_cast<const T*>(p.pre) + r * p.M + c, n, z);
+  if (in) {
+    const T* dy = static_cast<const T*>(p.dy) + r0 * p.lddy + c;
+    const T* pre = static_cast<const T*>(p.pre) + r0 * p.M + c;
+    T* dz = static_cast<T*>(p.dz) + r0 * p.M + c;
+    T* rest = static_cast<T*>(p.rest) + r0 * p.M + c;
+    const int rows = int(r1 - r0);
+    for (int r = g; r < rows; r += DZ_AHEAD * groups) {
+      u32x4 d[DZ_AHEAD], z[DZ_AHEAD];
 #pragma unroll
-        for (int j = 0; j < VE; ++j) d[j] *= slope_of(p.act, z[j]);
-        store_chunk(static_cast<T*>(p.dz) + r * p.M + c, n, d);
-        if constexpr (sizeof(T) == 2) {
-#pragma unroll
-          for (int j = 0; j < VE; ++j) {
-            const float near = __uint_as_float(bf16_rne(d[j]) << 16);
-            t[j] = fabsf(near) < INFINITY ? d[j] - near : 0.f;
-          }
-          store_chunk(static_cast<T*>(p.rest) + r * p.M + c, n, t);
+      for (int i = 0; i < DZ_AHEAD; ++i) {
+        const int64_t q = min(r + i * groups, rows - 1);
+        if constexpr (SHORT) {
+          d[i] = lin_load_short(dy + q * p.lddy, n);
+          z[i] = lin_load_short(pre + q * p.M, n);
+        } else {
+          d[i] = lin_load(dy + q * p.lddy);
+          z[i] = lin_load(pre + q * p.M);
         }
       }
 #pragma unroll
-      for (int j = 0; j < VE; ++j) sum[j] += d[j];
+      for (int i = 0; i < DZ_AHEAD; ++i)
+        if (r + i * groups < rows) {
+          const int64_t o = int64_t(r + i * groups) * p.M;
+          float x[VE], y[VE];
+          lin_unpack(T(), d[i], x);
+          lin_unpack(T(), z[i], y);
+#pragma unroll
+          for (int j = 0; j < VE; ++j) {
+            x[j] *= slope_of(p.act, y[j]);
+            sum[j] += x[j];
+          }
+          store_chunk(dz + o, n, x);
+          if constexpr (sizeof(T) == 2) {
+#pragma unroll
+            for (int j = 0; j < VE; ++j) {
+              const float near = __uint_as_float(bf16_rne(x[j]) << 16);
+              x[j] = fabsf(near) < INFINITY ? x[j] - near : 0.f;
+            }
+            store_chunk(rest + o, n, x);
+          }
+        }
     }
   }
   if (!p.sums) return;
 #pragma unroll
-  for (int j = 0; j < VE; ++j) s[wave][lane * VE + j] = sum[j];
+  for (int j = 0; j < VE; ++j) s[threadIdx.x * VE + j] = sum[j];
   __syncthreads();
-  for (int t = threadIdx.x; t < DZ_COLS * VE; t += LIN_THREADS) {
-    const int col = blockIdx.y * DZ_COLS * VE + t;
-    if (col < p.M) {
-      double x = 0.0;
-      for (int w = 0; w < WAVES; ++w) x += s[w][t];
-      p.sums[int64_t(blockIdx.x) * p.M + col] = float(x);
-    }
+  if (in && g == 0) {
+#pragma unroll
+    for (int j = 0; j < VE; ++j)
+      if (j >= skip && j < n) {
+        double x = 0.0;
+        for (int q = 0; q < groups; ++q) x += s[(q * p.lanes + lane) * VE + j];
+        p.sums[int64_t(blockIdx.x) * p.M + c + j] = float(x);
+      }
   }
 }
 
@@ -495,18 +722,40 @@ __global__ void __launch_bounds__(LIN_THREADS) k_linear_turn(const T* __restrict
 }
 
 // ------------------------------------------------------------------ host side
+// Long products into wide rows take 256 x 256: a tile of 128 x 128 reads twice the operands
+// from L2 (40,000 x 2048 x 2048 bf16 457 against 548 us, 8192^3 1068 / 1697; the library 349 / 728).
+// Otherwise several workgroups per CU count for more: 264,000 x 272 x 256 bf16 105 / 96,
+// x 256 x 272 146 / 93 (the library 148 / 155), x 372 x 200 fp32 538 / 469 (564).
+static bool lin_big(int64_t n, int M, int64_t K) {
+  return K >= 1024 && M >= 512 && ((n + 255) / 256) * ((M + 255) / 256) >= 256;
+}
+template <typename T, typename Tile>
+static void lin_tiled(LinArgs& a, hipStream_t st) {
+  a.tiles_c = (a.M + Tile::BC - 1) / Tile::BC;
+  const dim3 grid(uint32_t((a.n + Tile::BR - 1) / Tile::BR * a.tiles_c));
+  if constexpr (std::is_same<Tile, LinMid>::value) {
+    if (a.K < CHUNK<T>) {
+      hipLaunchKernelGGL((k_linear<T, Tile, true>), grid, dim3(Tile::THREADS), 0, st, a);
+      return;
+    }
+  }
+  hipLaunchKernelGGL((k_linear<T, Tile, false>), grid, dim3(Tile::THREADS), 0, st, a);
+}
 template <typename T>
 static void lin_product(LinArgs a, hipStream_t st) {
-  const int64_t tr = (a.n + 127) / 128, tc = (a.M + 127) / 128;
-  if (tr * tc >= 256) {
-    a.tiles_c = int(tc);
-    hipLaunchKernelGGL((k_linear<T, 2, 2>), dim3(uint32_t(tr * tc)), dim3(LIN_THREADS), 0, st, a);
+  if (lin_big(a.n, a.M, a.K)) {
+    lin_tiled<T, LinBig>(a, st);
+    return;
+  }
+  if ((a.n + 127) / 128 * ((a.M + 127) / 128) >= 256) {
+    lin_tiled<T, LinMid>(a, st);
     return;
   }
   a.tiles_c = (a.M + 31) / 32;
   const dim3 grid(uint32_t((a.n + 31) / 32 * a.tiles_c));
-  if (a.K * int64_t(sizeof(T)) <= 1024) hipLaunchKernelGGL((k_linear_few<T, 4>), grid, dim3(256), 0, st, a);
-  else hipLaunchKernelGGL((k_linear_few<T, 16>), grid, dim3(1024), 0, st, a);
+  if (a.K < CHUNK<T>) hipLaunchKernelGGL((k_linear_few<T, 4, true>), grid, dim3(256), 0, st, a);
+  else if (a.K * int64_t(sizeof(T)) <= 1024) hipLaunchKernelGGL((k_linear_few<T, 4, false>), grid, dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((k_linear_few<T, 16, false>), grid, dim3(1024), 0, st, a);
 }
 // Workgroups of lin_product times its threads, at most
 static bool lin_fits(int64_t n, int M) {
@@ -521,14 +770,14 @@ struct LinPlan {
 constexpr int64_t LIN_SPLIT_MAX = 16384;     // rows whose products are added in fp32, at most
 static LinPlan lin_plan(int64_t n, int K, int M, fast_dtype_t dtype, fast_act_t act) {
   LinPlan p = {};
+  p.planes = dtype == FAST_BF16 && act != FAST_ACT_NONE ? 2 : 1;
+  p.dz_blocks = (n + DZ_ROWS - 1) / DZ_ROWS;
   const int64_t tiles = int64_t((M + 127) / 128) * ((K + 127) / 128);
-  int64_t s = std::max<int64_t>(1, 512 / tiles);
+  int64_t s = std::max<int64_t>(1, 512 / (tiles * p.planes));
   s = std::min<int64_t>(s, (n + 255) / 256);
   s = std::max<int64_t>({s, (n + LIN_SPLIT_MAX - 1) / LIN_SPLIT_MAX, 1});
   p.rows = ((n + s - 1) / s + 63) / 64 * 64;
   p.splits = int(s);                 // (trailing ones may be empty)
-  p.planes = dtype == FAST_BF16 && act != FAST_ACT_NONE ? 2 : 1;
-  p.dz_blocks = (n + DZ_ROWS - 1) / DZ_ROWS;
   return p;
 }
 
@@ -554,7 +803,7 @@ static size_t lin_layout(int64_t n, int K, int M, fast_dtype_t dtype, fast_act_t
   t.dz = act != FAST_ACT_NONE ? take(n * M * es) : nullptr;
   t.rest = p.planes == 2 ? take(n * M * es) : nullptr;
   t.part = reinterpret_cast<float*>(take(int64_t(p.splits) * p.planes * M * K * 4));
-  t.sums = reinterpret_cast<float*>(take(p.dz_blocks * M * 4));
+  t.sums = reinterpret_cast<float*>(take((act != FAST_ACT_NONE ? p.dz_blocks : p.splits) * M * 4));
   if (w) *w = t;
   return at;
 }
@@ -573,9 +822,7 @@ static fast_status_t lin_check(const char* fn, int64_t n, int K, int M, fast_dty
 static fast_status_t lin_rows(const char* fn, const char* name, const void* p, int64_t n, int F, int64_t ld,
                               int64_t es) {
   if (ld < F) return fail(FAST_ERR_INVALID_ARG, "%s: %s: rows of %d elements, %lld apart", fn, name, F, (long long)ld);
-  if (ld >= (int64_t(1) << 31)) return fail(FAST_ERR_UNSUPPORTED, "%s: %s: row stride >= 2^31", fn, name);
-  if (n * ld >= (int64_t(1) << 56))
-    return fail(FAST_ERR_UNSUPPORTED, "%s: %s: %lld rows, %lld elements apart", fn, name, (long long)n, (long long)ld);
+  if (ld >= LIN_MAX_LD) return fail(FAST_ERR_UNSUPPORTED, "%s: %s: row stride >= 2^22", fn, name);
   if (n > 0 && !p) return fail(FAST_ERR_INVALID_ARG, "%s: NULL %s", fn, name);
   if (!aligned(p, es)) return fail(FAST_ERR_UNSUPPORTED, "%s: %s not %d-byte aligned", fn, name, int(es));
   return FAST_OK;
@@ -589,15 +836,13 @@ static void lin_bwd(int64_t n, int K, int M, fast_dtype_t dtype, const void* x, 
   LinWork m;
   lin_layout(n, K, M, dtype, act, ws, &m);
   const bool acts = act != FAST_ACT_NONE;
-  if (n > 0 && (dbias || acts)) {
-    const DzArgs d = {n, lddy, M, act, dy, pre, m.dz, m.rest, dbias ? m.sums : nullptr};
-    const int per = DZ_COLS * CHUNK<T>;
-    hipLaunchKernelGGL(k_linear_dz<T>, dim3(uint32_t(p.dz_blocks), uint32_t((M + per - 1) / per)), dim3(LIN_THREADS), 0,
-                       st, d);
+  if (n > 0 && acts) {
+    DzArgs d = {n, lddy, M, act, (M + CHUNK<T> - 1) / CHUNK<T>, 0, dy, pre, m.dz, m.rest, dbias ? m.sums : nullptr};
+    d.lanes = std::min(d.chunks, LIN_THREADS);
+    const dim3 grid(uint32_t(p.dz_blocks), uint32_t((d.chunks + d.lanes - 1) / d.lanes));
+    if (M < CHUNK<T>) hipLaunchKernelGGL((k_linear_dz<T, true>), grid, dim3(LIN_THREADS), 0, st, d);
+    else hipLaunchKernelGGL((k_linear_dz<T, false>), grid, dim3(LIN_THREADS), 0, st, d);
   }
-  if (dbias)
-    hipLaunchKernelGGL(k_linear_join, dim3(uint32_t((M + LJ_COLS - 1) / LJ_COLS)), dim3(LIN_THREADS), 0, st, m.sums,
-                       p.dz_blocks, int64_t(M), dbias);
   const void* dz = acts ? m.dz : dy;
   const int64_t lddz = acts ? M : lddy;
   if (dx && n > 0) {
@@ -616,7 +861,13 @@ static void lin_bwd(int64_t n, int K, int M, fast_dtype_t dtype, const void* x, 
     a.ldy = lddx;
     lin_product<T>(a, st);
   }
-  if (dw) {
+  auto join = [&](const float* part, int64_t parts, int64_t size, float* out) {
+    if (parts != 1)
+      hipLaunchKernelGGL(k_linear_join, dim3(uint32_t((size + LJ_COLS - 1) / LJ_COLS)), dim3(LIN_THREADS), 0, st, part,
+                         parts, size, out);
+  };
+  const int64_t parts = n > 0 ? int64_t(p.splits) * p.planes : 0;
+  if (n > 0 && (dw || (dbias && !acts))) {
     LinArgs a = {};
     a.a = dz;
     a.a2 = m.rest;
@@ -624,21 +875,31 @@ static void lin_bwd(int64_t n, int K, int M, fast_dtype_t dtype, const void* x, 
     a.b = x;
     a.ldb = ldx;
     a.n = M;
-    a.M = K;
+    a.M = dw ? K : 1;                                   // (dbias alone: one tile of columns)
     a.K = n;
     a.rows = p.rows;
     a.splits = p.splits;
-    a.tiles_c = (K + 127) / 128;
-    const int64_t parts = n > 0 ? int64_t(p.splits) * p.planes : 0;
     a.part = parts == 1 ? dw : m.part;
-    if (parts > 0)
-      hipLaunchKernelGGL(k_linear_wgrad<T>, dim3(uint32_t(parts * ((M + 127) / 128) * a.tiles_c)), dim3(LIN_THREADS),
-                         0, st, a);
-    if (parts != 1) {
-      const int64_t size = int64_t(M) * K;
-      hipLaunchKernelGGL(k_linear_join, dim3(uint32_t((size + LJ_COLS - 1) / LJ_COLS)), dim3(LIN_THREADS), 0, st, m.part,
-                         parts, size, dw);
-    }
+    a.sums = !dbias || acts ? nullptr : (parts == 1 ? dbias : m.sums);
+    auto launch = [&](auto product, auto one) {
+      typedef LinGrad Tile;
+      a.tiles_c = (a.M + Tile::BC - 1) / Tile::BC;
+      hipLaunchKernelGGL((k_linear_wgrad<T, Tile, decltype(product)::value, decltype(one)::value>),
+                         dim3(uint32_t(parts * ((M + Tile::BR - 1) / Tile::BR) * a.tiles_c)), dim3(Tile::THREADS), 0, st, a);
+    };
+    const std::integral_constant<bool, true> yes;
+    const std::integral_constant<bool, false> no;
+    if (dw && M > 1 && K > 1) launch(yes, no);
+    else if (dw) launch(yes, yes);
+    else if (M > 1) launch(no, no);
+    else launch(no, yes);
+  }
+  if (dw) join(m.part, parts, int64_t(M) * K, dw);
+  if (dbias && acts) {                                  // a part per block of rows
+    hipLaunchKernelGGL(k_linear_join, dim3(uint32_t((M + LJ_COLS - 1) / LJ_COLS)), dim3(LIN_THREADS), 0, st, m.sums,
+                       p.dz_blocks, int64_t(M), dbias);
+  } else if (dbias) {
+    join(m.sums, parts, M, dbias);
   }
 }
 
