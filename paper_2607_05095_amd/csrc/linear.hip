@@ -84,6 +84,36 @@ __device__ __forceinline__ u32x4 lin_mask(int skip) {
   return m;
 }
 
+// ------------------------------------------------------------------ fp32 in three parts
+// An fp32 value is the sum of three bf16 values, 8 bits of its mantissa each: cut off, subtracted
+// (exactly), cut off again.  A product of two is then six products of parts; the three that are
+// left out are below 2^-22 of it together, 2^-24 in the mean.  Six bf16 instructions take 2.7
+// times less than the fp32 ones of the same product.  An infinity has no such parts (and a part
+// of 0 times an infinity is no number): a workgroup that meets a value that is not finite does
+// its tile again with fp32 instructions.
+struct LinParts {
+  u32x4 p[3];                        // 8 values: their first, second and third parts
+};
+// cut: accumulates what is not a number once a value was not finite.
+__device__ __forceinline__ LinParts lin_split(const float* x, float& cut) {
+  LinParts r;
+  float y[8], z[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    y[j] = x[j] - __uint_as_float(__float_as_uint(x[j]) & 0xffff0000u);
+    z[j] = y[j] - __uint_as_float(__float_as_uint(y[j]) & 0xffff0000u);
+    cut = fmaf(y[j], 0.f, cut);
+  }
+#pragma unroll
+  for (int d = 0; d < 4; ++d) {
+    r.p[0][d] = __builtin_amdgcn_perm(__float_as_uint(x[2 * d + 1]), __float_as_uint(x[2 * d]), 0x07060302u);
+    r.p[1][d] = __builtin_amdgcn_perm(__float_as_uint(y[2 * d + 1]), __float_as_uint(y[2 * d]), 0x07060302u);
+    r.p[2][d] = __builtin_amdgcn_perm(__float_as_uint(z[2 * d + 1]), __float_as_uint(z[2 * d]), 0x07060302u);
+  }
+  return r;
+}
+template <typename T> constexpr int LIN_PARTS = sizeof(T) == 4 ? 3 : 1;
+
 // ------------------------------------------------------------------ activations
 __device__ __forceinline__ float act_of(int act, float z) {
   if (act == FAST_ACT_RELU) return z > 0.f ? z : (z == z ? 0.f : z);
@@ -121,8 +151,6 @@ struct LinArgs {
   int tiles_c;                       // tiles along c
   // weight gradients: K is cut into splits of `rows`, each with a result of its own
   int64_t rows;
-  int splits;                        // of one operand a; the same number behind them reads a2
-  const void* a2;
   float* part;
   float* sums;
 };
@@ -200,6 +228,7 @@ struct LinTile {
 typedef LinTile<2, 4, 4, 2, 128> LinBig;   // 256 x 256
 typedef LinTile<2, 2, 2, 2, 64> LinMid;    // 128 x 128
 typedef LinTile<2, 2, 2, 2, 128> LinGrad;  // 128 x 128 of weight gradients
+typedef LinTile<2, 4, 2, 2, 64> LinWide;   // 128 x 256
 
 // A wave's part of a tile: TR x TC blocks of 32 x 32 over a tile of k in LDS.
 template <typename T, typename Tile>
@@ -220,6 +249,48 @@ __device__ __forceinline__ void lin_step(const char* la, const char* lb, f32x16_
 #pragma unroll
       for (int j = 0; j < TC; ++j) lin_mma(T(), fb[j], fa[i], acc[i][j]);
   }
+}
+
+// The same with PA and PB parts of the operands, their tiles one behind the other.
+template <typename Tile, int PA, int PB>
+__device__ __forceinline__ void lin_step_parts(const char* la, const char* lb,
+                                               f32x16_t (&acc)[Tile::TR][Tile::TC]) {
+  constexpr int TR = Tile::TR, TC = Tile::TC, ROW = Tile::ROW;
+  const int lane = threadIdx.x & 63;
+  la += (lane & 31) * ROW + (lane >> 5) * 16;
+  lb += (lane & 31) * ROW + (lane >> 5) * 16;
+#pragma unroll
+  for (int k = 0; k < Tile::KB; k += 32) {
+    u32x4 fa[TR][PA], fb[TC][PB];
+#pragma unroll
+    for (int i = 0; i < TR; ++i)
+#pragma unroll
+      for (int s = 0; s < PA; ++s) fa[i][s] = *reinterpret_cast<const u32x4*>(la + (s * Tile::BR + i * 32) * ROW + k);
+#pragma unroll
+    for (int j = 0; j < TC; ++j)
+#pragma unroll
+      for (int s = 0; s < PB; ++s) fb[j][s] = *reinterpret_cast<const u32x4*>(lb + (s * Tile::BC + j * 32) * ROW + k);
+    // the small products first
+#pragma unroll
+    for (int s = PA + PB - 2 < 2 ? PA + PB - 2 : 2; s >= 0; --s)
+#pragma unroll
+      for (int q = 0; q < PA; ++q)
+        if (s - q >= 0 && s - q < PB) {
+#pragma unroll
+          for (int i = 0; i < TR; ++i)
+#pragma unroll
+            for (int j = 0; j < TC; ++j) lin_mma(uint16_t(), fb[j][s - q], fa[i][q], acc[i][j]);
+        }
+  }
+}
+template <int TR, int TC>
+__device__ __forceinline__ void lin_clear(f32x16_t (&acc)[TR][TC]) {
+#pragma unroll
+  for (int i = 0; i < TR; ++i)
+#pragma unroll
+    for (int j = 0; j < TC; ++j)
+#pragma unroll
+      for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.f;
 }
 
 // The wave's block through LDS, 32 rows at a time, so that rows leave in whole chunks.
@@ -333,6 +404,102 @@ __global__ void __launch_bounds__(Tile::THREADS) k_linear(LinArgs p) {
   lin_out<VE>(lds, acc, [&](int r, float* z) { end.finish(r0 + wr * TR * 32 + r, z); });
 }
 
+// k_linear of fp32 rows in parts; K >= 8.  One buffer in LDS, so that two workgroups share a CU:
+// one multiplies while the other cuts its next tile of k up.
+template <typename Tile>
+__global__ void __launch_bounds__(Tile::THREADS) k_linear_parts(LinArgs p) {
+  constexpr int TR = Tile::TR, TC = Tile::TC, BR = Tile::BR, BC = Tile::BC, ROW = Tile::ROW;
+  constexpr int VE = 8, BK = Tile::KB / 2, STEP = Tile::THREADS / Tile::CHUNKS, NA = BR / STEP, NB = BC / STEP;
+  __shared__ __attribute__((aligned(16))) char lds[3 * (BR + BC) * ROW];
+  static_assert(sizeof(lds) >= Tile::WR * Tile::WC * 32 * (TC * 32 + 4) * 4, "the epilogue's buffer");
+  const uint32_t id = xcd_tile(blockIdx.x, gridDim.x);
+  const int64_t r0 = int64_t(id / uint32_t(p.tiles_c)) * BR;
+  const int c0 = int(id % uint32_t(p.tiles_c)) * BC;
+  const int row = threadIdx.x / Tile::CHUNKS, chunk = threadIdx.x % Tile::CHUNKS;
+  const float* A = static_cast<const float*>(p.a) + r0 * p.lda;
+  const float* B = static_cast<const float*>(p.b) + int64_t(c0) * p.ldb;
+  uint32_t oa[NA], ob[NB];
+#pragma unroll
+  for (int i = 0; i < NA; ++i)
+    oa[i] = uint32_t(min(int64_t(i * STEP + row), p.n - 1 - r0)) * uint32_t(p.lda);
+#pragma unroll
+  for (int i = 0; i < NB; ++i) ob[i] = uint32_t(min(i * STEP + row, p.M - 1 - c0)) * uint32_t(p.ldb);
+  const int K = int(p.K), full = K / BK, tiles = (K + BK - 1) / BK;
+  const int last = full * BK + chunk * VE, back = min(last, K - VE), skip = last - back;
+  u32x4 ra[NA][2], rb[NB][2];
+  auto load = [&](int t) {
+    const uint32_t k = t < full ? chunk * VE : back;
+    const float* pa = A + (t < full ? t * BK : 0);
+    const float* pb = B + (t < full ? t * BK : 0);
+#pragma unroll
+    for (int i = 0; i < NA; ++i) {
+      ra[i][0] = lin_load(at_offset(pa, oa[i] + k));
+      ra[i][1] = lin_load(at_offset(pa, oa[i] + k + 4));
+    }
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+      rb[i][0] = lin_load(at_offset(pb, ob[i] + k));
+      rb[i][1] = lin_load(at_offset(pb, ob[i] + k + 4));
+    }
+  };
+  float cut = 0.f;
+  auto part = [&](const u32x4 (&w)[2], bool end, char* at, int rows) {
+    float x[VE];
+#pragma unroll
+    for (int j = 0; j < VE; ++j) x[j] = __uint_as_float(w[j / 4][j % 4]);
+    if (end) {
+#pragma unroll
+      for (int j = 0; j < VE; ++j) x[j] = j >= skip ? x[j] : 0.f;
+    }
+    const LinParts s = lin_split(x, cut);
+#pragma unroll
+    for (int q = 0; q < 3; ++q) *reinterpret_cast<u32x4*>(at + q * rows * ROW) = s.p[q];
+  };
+  auto put = [&](int t) {
+    char* at = lds + row * ROW + chunk * 16;
+#pragma unroll
+    for (int i = 0; i < NA; ++i) part(ra[i], t >= full, at + i * STEP * ROW, BR);
+#pragma unroll
+    for (int i = 0; i < NB; ++i) part(rb[i], t >= full, at + (3 * BR + i * STEP) * ROW, BC);
+  };
+  f32x16_t acc[TR][TC];
+  lin_clear(acc);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wr = wave / Tile::WC, wc = wave % Tile::WC;
+  load(0);
+  for (int t = 0; t < tiles; ++t) {
+    put(t);
+    __syncthreads();
+    if (t + 1 < tiles) load(t + 1);
+    lin_step_parts<Tile, 3, 3>(lds + wr * TR * 32 * ROW, lds + (3 * BR + wc * TC * 32) * ROW, acc);
+    __syncthreads();
+  }
+  if (__syncthreads_or(cut != cut)) {                     // not finite: from memory, in fp32
+    lin_clear(acc);
+    const int half = lane >> 5;
+    for (int k = half * 4; k - half * 4 < K; k += 8) {
+      const int at = min(k, K - 4);
+      const u32x4 m = lin_mask<float>(k - at);
+      u32x4 fa[TR], fb[TC];
+#pragma unroll
+      for (int i = 0; i < TR; ++i) {
+        const int64_t r = min(int64_t(wr * TR * 32 + i * 32 + (lane & 31)), p.n - 1 - r0);
+        fa[i] = lin_load(A + r * p.lda + at) & m;
+      }
+#pragma unroll
+      for (int j = 0; j < TC; ++j) {
+        const int64_t c = min(wc * TC * 32 + j * 32 + (lane & 31), p.M - 1 - c0);
+        fb[j] = lin_load(B + c * p.ldb + at) & m;
+      }
+#pragma unroll
+      for (int i = 0; i < TR; ++i)
+#pragma unroll
+        for (int j = 0; j < TC; ++j) lin_mma(float(), fb[j], fa[i], acc[i][j]);
+    }
+  }
+  const LinEnd<float, 4> end(p, c0 + wc * TC * 32 + lane % (TC * 8) * 4);
+  lin_out<4>(lds, acc, [&](int r, float* z) { end.finish(r0 + wr * TR * 32 + r, z); });
+}
+
 // Few rows: 32 x 32 results a workgroup, its waves share k, each feeding the matrix unit from
 // global memory; their sums are added in order in LDS.
 template <typename T, int WAVES, bool SHORT>
@@ -439,29 +606,6 @@ template <> struct LinTurn<uint16_t> {        // 2 columns of 8 rows
     }
   }
 };
-template <> struct LinTurn<float> {           // a column of 4 rows
-  static constexpr int COLS = 1, ROWS = 4;
-  float w[4];
-  uint32_t at;
-  __device__ void place(int col, int width) { at = uint32_t(min(col, width - 1)); }
-  template <bool END, bool ONE>
-  __device__ void load(const float* p, uint32_t ld, int row, int last) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      w[j] = END ? *at_offset(p, at + uint32_t(min(row + j, last)) * ld) : *at_offset(p + j * size_t(ld), at + row * ld);
-  }
-  __device__ void trim(int64_t rows) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) w[j] = j < rows ? w[j] : 0.f;
-  }
-  template <int ROW>
-  __device__ void put(char* o) const { *reinterpret_cast<f32x4*>(o) = f32x4{w[0], w[1], w[2], w[3]}; }
-  __device__ void add(float* s) const {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) s[0] += w[j];
-  }
-};
-
 // p.a: dz [K, n] (n columns, lda apart), p.b: x [K, M]; PRODUCT: part[split][n][M]; sums (NULL for
 // none): from the workgroups of the first tile of columns, sums[split][n] of dz's columns.
 // ONE: n or M is 1.
@@ -479,10 +623,9 @@ __global__ void __launch_bounds__(Tile::THREADS) k_linear_wgrad(LinArgs p) {
   const uint32_t tiles_r = uint32_t((p.n + BR - 1) / BR), tiles = tiles_r * uint32_t(p.tiles_c);
   const uint32_t split = id / tiles, tile = id % tiles;
   const int r0 = int(tile / uint32_t(p.tiles_c)) * BR, c0 = int(tile % uint32_t(p.tiles_c)) * BC;
-  const bool second = split >= uint32_t(p.splits);
-  const T* A = static_cast<const T*>(second ? p.a2 : p.a);
+  const T* A = static_cast<const T*>(p.a);
   const T* B = static_cast<const T*>(p.b);
-  const int64_t k0 = int64_t(second ? split - p.splits : split) * p.rows, k1 = min(k0 + p.rows, p.K);
+  const int64_t k0 = int64_t(split) * p.rows, k1 = min(k0 + p.rows, p.K);
   const int grpa = threadIdx.x % GA, firsta = threadIdx.x / GA, grpb = threadIdx.x % GB, firstb = threadIdx.x / GB;
   const bool sums = p.sums && c0 == 0;
   Turn ta[NTA], tb[NTB];
@@ -603,8 +746,181 @@ __global__ void __launch_bounds__(Tile::THREADS) k_linear_wgrad(LinArgs p) {
   }
 }
 
-// dz = dy act'(pre) (bf16: the nearest value and what is left, 16 bits of it together) and its
-// columns' sums: a workgroup takes DZ_ROWS rows and up to 256 chunks of columns, a thread one chunk
+// k_linear_wgrad of fp32 dz (and x of fp32 or bf16) in parts.
+template <typename T> struct LinCols;           // 8 rows of LinCols::COLS columns
+template <> struct LinCols<float> {
+  static constexpr int COLS = 1;
+  float w[8];
+  uint32_t at;
+  __device__ void place(int col, int width) { at = uint32_t(min(col, width - 1)); }
+  template <bool END, bool ONE>
+  __device__ void load(const float* p, uint32_t ld, int row, int last) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      w[j] = END ? *at_offset(p, at + uint32_t(min(row + j, last)) * ld) : *at_offset(p + j * size_t(ld), at + row * ld);
+  }
+  __device__ void trim(int64_t rows) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) w[j] = j < rows ? w[j] : 0.f;
+  }
+  // (`rows`: of a part's tile)
+  template <int ROW>
+  __device__ void put(char* o, int rows, float& cut) const {
+    const LinParts s = lin_split(w, cut);
+#pragma unroll
+    for (int q = 0; q < 3; ++q) *reinterpret_cast<u32x4*>(o + q * rows * ROW) = s.p[q];
+  }
+};
+template <> struct LinCols<uint16_t> : LinTurn<uint16_t> {
+  template <int ROW>
+  __device__ void put(char* o, int, float& cut) const {
+    LinTurn<uint16_t>::template put<ROW>(o);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) cut = fmaf(bf16_lo(w[j]), 0.f, fmaf(bf16_hi(w[j]), 0.f, cut));
+  }
+};
+__device__ __forceinline__ float lin_value(float x) { return x; }
+__device__ __forceinline__ float lin_value(uint16_t x) { return __uint_as_float(uint32_t(x) << 16); }
+
+// As k_linear_wgrad; ONE: p.M is 1.
+template <typename T, typename Tile, bool PRODUCT, bool ONE>
+__global__ void __launch_bounds__(Tile::THREADS) k_linear_wgrad_parts(LinArgs p) {
+  constexpr int TR = Tile::TR, TC = Tile::TC, BR = Tile::BR, BC = Tile::BC, ROW = Tile::ROW, PB = LIN_PARTS<T>;
+  constexpr int BK = Tile::KB / 2;
+  typedef LinCols<float> ColsA;
+  typedef LinCols<T> ColsB;
+  constexpr int GA = BR, NTA = GA * Tile::CHUNKS / Tile::THREADS, NEXTA = Tile::THREADS / GA;
+  constexpr int GB = BC / ColsB::COLS, NTB = GB * Tile::CHUNKS / Tile::THREADS, NEXTB = Tile::THREADS / GB;
+  static_assert(NTA * NEXTA == Tile::CHUNKS && NTB * NEXTB == Tile::CHUNKS, "whole pieces");
+  constexpr int OUT = Tile::WR * Tile::WC * 32 * (TC * 32 + 4) * 4, BUF = (3 * BR + PB * BC) * ROW;
+  __shared__ __attribute__((aligned(16))) char lds[PRODUCT ? (BUF > OUT ? BUF : OUT) : NEXTA * BR * 8];
+  const uint32_t id = xcd_tile(blockIdx.x, gridDim.x);
+  const uint32_t tiles_r = uint32_t((p.n + BR - 1) / BR), tiles = tiles_r * uint32_t(p.tiles_c);
+  const uint32_t split = id / tiles, tile = id % tiles;
+  const int r0 = int(tile / uint32_t(p.tiles_c)) * BR, c0 = int(tile % uint32_t(p.tiles_c)) * BC;
+  const float* A = static_cast<const float*>(p.a);
+  const T* B = static_cast<const T*>(p.b);
+  const int64_t k0 = int64_t(split) * p.rows, k1 = min(k0 + p.rows, p.K);
+  const int ga = threadIdx.x % GA, fa0 = threadIdx.x / GA, gb = threadIdx.x % GB, fb0 = threadIdx.x / GB;
+  const bool sums = p.sums && c0 == 0;
+  ColsA ta[NTA];
+  ColsB tb[NTB];
+#pragma unroll
+  for (int i = 0; i < NTA; ++i) ta[i].place(r0 + ga, int(p.n));
+#pragma unroll
+  for (int i = 0; i < NTB; ++i) tb[i].place(c0 + gb * ColsB::COLS, PRODUCT ? p.M : 1);
+  auto load = [&](int64_t k, auto end) {
+    constexpr bool END = decltype(end)::value;
+    const int last = int(k1 - 1 - k);
+#pragma unroll
+    for (int i = 0; i < NTA; ++i)
+      ta[i].template load<END, false>(A + k * p.lda, uint32_t(p.lda), (fa0 + i * NEXTA) * 8, last);
+    if constexpr (PRODUCT) {
+#pragma unroll
+      for (int i = 0; i < NTB; ++i)
+        tb[i].template load<END, ONE>(B + k * p.ldb, uint32_t(p.ldb), (fb0 + i * NEXTB) * 8, last);
+    }
+  };
+  float cut = 0.f;
+  double sum = 0.0;                                     // (a tile's in fp32)
+  const bool odd = sizeof(T) == 2 && (p.M & 1);
+  auto put = [&](int64_t k) {
+    if (k + BK > k1) {
+#pragma unroll
+      for (int i = 0; i < NTA; ++i) ta[i].trim(k1 - k - (fa0 + i * NEXTA) * 8);
+    }
+    if (PRODUCT && (odd || k + BK > k1)) {
+#pragma unroll
+      for (int i = 0; i < NTB; ++i) tb[i].trim(k1 - k - (fb0 + i * NEXTB) * 8);
+    }
+    if (sums) {
+      float s = 0.f;
+#pragma unroll
+      for (int i = 0; i < NTA; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s += ta[i].w[j];
+      sum += s;
+    }
+    if constexpr (PRODUCT) {
+#pragma unroll
+      for (int i = 0; i < NTA; ++i) ta[i].template put<ROW>(lds + ga * ROW + (fa0 + i * NEXTA) * 16, BR, cut);
+#pragma unroll
+      for (int i = 0; i < NTB; ++i)
+        tb[i].template put<ROW>(lds + (3 * BR + gb * ColsB::COLS) * ROW + (fb0 + i * NEXTB) * 16, BC, cut);
+    }
+  };
+  f32x16_t acc[TR][TC];
+  lin_clear(acc);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wr = wave / Tile::WC, wc = wave % Tile::WC;
+  auto multiply = [&] {
+    if constexpr (PRODUCT)
+      lin_step_parts<Tile, 3, PB>(lds + wr * TR * 32 * ROW, lds + (3 * BR + wc * TC * 32) * ROW, acc);
+  };
+  typedef std::integral_constant<bool, false> Whole;
+  typedef std::integral_constant<bool, true> End;
+  const int64_t full = k1 > k0 ? (k1 - k0) / BK : 0;
+  int64_t k = k0;
+  if (full > 0) load(k, Whole());
+  for (int64_t t = 0; t < full; ++t, k += BK) {
+    put(k);
+    __syncthreads();
+    if (t + 1 < full) load(k + BK, Whole());
+    multiply();
+    __syncthreads();
+  }
+  if (k < k1) {
+    load(k, End());
+    put(k);
+    __syncthreads();
+    multiply();
+    __syncthreads();
+  }
+  if (PRODUCT && __syncthreads_or(cut != cut)) {          // not finite: from memory, in fp32
+    lin_clear(acc);
+    for (int64_t q = k0; q < k1; q += 8) {
+      u32x4 fa[TR], fb[TC];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int64_t r = q + (lane >> 5) * 4 + j, rr = min(r, k1 - 1);
+#pragma unroll
+        for (int i = 0; i < TR; ++i) {
+          const float v = A[rr * p.lda + min(r0 + wr * TR * 32 + i * 32 + (lane & 31), int(p.n) - 1)];
+          fa[i][j] = r < k1 ? __float_as_uint(v) : 0u;
+        }
+#pragma unroll
+        for (int i = 0; i < TC; ++i) {
+          const float v = lin_value(B[rr * p.ldb + min(c0 + wc * TC * 32 + i * 32 + (lane & 31), p.M - 1)]);
+          fb[i][j] = r < k1 ? __float_as_uint(v) : 0u;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < TR; ++i)
+#pragma unroll
+        for (int j = 0; j < TC; ++j) lin_mma(float(), fb[j], fa[i], acc[i][j]);
+    }
+  }
+  if constexpr (PRODUCT) {
+    float* part = p.part + int64_t(split) * p.n * p.M;
+    const int col = c0 + wc * TC * 32 + lane % (TC * 8) * 4;
+    lin_out<4>(lds, acc, [&](int r, float* z) {
+      const int64_t row = r0 + wr * TR * 32 + r;
+      if (row < p.n && col < p.M) store_chunk_of(part + row * p.M + col, p.M - col, z);
+    });
+  }
+  if (sums) {
+    __syncthreads();
+    double* s = reinterpret_cast<double*>(lds);
+    s[fa0 * BR + ga] = sum;
+    __syncthreads();
+    for (int c = threadIdx.x; c < BR && r0 + c < p.n; c += Tile::THREADS) {
+      double x = 0.0;
+      for (int f = 0; f < NEXTA; ++f) x += s[f * BR + c];
+      p.sums[int64_t(split) * p.n + r0 + c] = float(x);
+    }
+  }
+}
+
+// dz = dy act'(pre) in fp32 (and, for dx of bf16 rows, rounded to that) and its columns' sums: a workgroup takes DZ_ROWS rows and up to 256 chunks of columns, a thread one chunk
 // of every `groups`-th row, DZ_AHEAD of them loaded together.  A row's last chunk starts early
 // enough to end with it (both writers of an element write the same value; one counts it).
 // SHORT: rows of less than a chunk.
@@ -615,8 +931,8 @@ struct DzArgs {
   int chunks, lanes;                                    // of a row; of them in a workgroup
   const void* dy;
   const void* pre;
-  void* dz;
-  void* rest;
+  float* dz;                                            // NULL where only near is needed
+  uint16_t* near;                                       // NULL: none
   float* sums;                                          // [row blocks][M], or NULL
 };
 template <typename T, bool SHORT>
@@ -634,8 +950,7 @@ __global__ void __launch_bounds__(LIN_THREADS) k_linear_dz(DzArgs p) {
   if (in) {
     const T* dy = static_cast<const T*>(p.dy) + r0 * p.lddy + c;
     const T* pre = static_cast<const T*>(p.pre) + r0 * p.M + c;
-    T* dz = static_cast<T*>(p.dz) + r0 * p.M + c;
-    T* rest = static_cast<T*>(p.rest) + r0 * p.M + c;
+    const int64_t o0 = r0 * p.M + c;
     const int rows = int(r1 - r0);
     for (int r = g; r < rows; r += DZ_AHEAD * groups) {
       u32x4 d[DZ_AHEAD], z[DZ_AHEAD];
@@ -653,7 +968,7 @@ __global__ void __launch_bounds__(LIN_THREADS) k_linear_dz(DzArgs p) {
 #pragma unroll
       for (int i = 0; i < DZ_AHEAD; ++i)
         if (r + i * groups < rows) {
-          const int64_t o = int64_t(r + i * groups) * p.M;
+          const int64_t o = o0 + int64_t(r + i * groups) * p.M;
           float x[VE], y[VE];
           lin_unpack(T(), d[i], x);
           lin_unpack(T(), z[i], y);
@@ -662,14 +977,12 @@ __global__ void __launch_bounds__(LIN_THREADS) k_linear_dz(DzArgs p) {
             x[j] *= slope_of(p.act, y[j]);
             sum[j] += x[j];
           }
-          store_chunk(dz + o, n, x);
-          if constexpr (sizeof(T) == 2) {
+          if (p.dz) {
 #pragma unroll
-            for (int j = 0; j < VE; ++j) {
-              const float near = __uint_as_float(bf16_rne(x[j]) << 16);
-              x[j] = fabsf(near) < INFINITY ? x[j] - near : 0.f;
-            }
-            store_chunk(rest + o, n, x);
+            for (int j = 0; j < VE; j += 4) store_chunk(p.dz + o + j, SHORT ? n - j : 4, x + j);
+          }
+          if constexpr (sizeof(T) == 2) {
+            if (p.near) store_chunk(p.near + o, n, x);
           }
         }
     }
@@ -741,11 +1054,22 @@ static void lin_tiled(LinArgs& a, hipStream_t st) {
   }
   hipLaunchKernelGGL((k_linear<T, Tile, false>), grid, dim3(Tile::THREADS), 0, st, a);
 }
+constexpr int64_t LIN_PARTS_K = 64;       // products of fp32 rows in parts from this length on
 template <typename T>
 static void lin_product(LinArgs a, hipStream_t st) {
-  if (lin_big(a.n, a.M, a.K)) {
-    lin_tiled<T, LinBig>(a, st);
-    return;
+  if constexpr (sizeof(T) == 4) {
+    const int64_t tiles = (a.n + 127) / 128 * ((a.M + 127) / 128);
+    if (tiles >= 256 && a.K >= LIN_PARTS_K) {
+      a.tiles_c = (a.M + 127) / 128;
+      hipLaunchKernelGGL((k_linear_parts<LinMid>), dim3(uint32_t(tiles)), dim3(LinMid::THREADS), 0, st, a);
+      return;
+    }
+  }
+  if constexpr (sizeof(T) == 2) {
+    if (lin_big(a.n, a.M, a.K)) {
+      lin_tiled<T, LinBig>(a, st);
+      return;
+    }
   }
   if ((a.n + 127) / 128 * ((a.M + 127) / 128) >= 256) {
     lin_tiled<T, LinMid>(a, st);
@@ -764,16 +1088,19 @@ static bool lin_fits(int64_t n, int M) {
 
 struct LinPlan {
   int64_t rows;                      // k of a split
-  int splits, planes;
+  int splits;
+  bool parts, wide;                  // fp32 operands in parts; tiles of 128 x 256
   int64_t dz_blocks;
 };
 constexpr int64_t LIN_SPLIT_MAX = 16384;     // rows whose products are added in fp32, at most
 static LinPlan lin_plan(int64_t n, int K, int M, fast_dtype_t dtype, fast_act_t act) {
   LinPlan p = {};
-  p.planes = dtype == FAST_BF16 && act != FAST_ACT_NONE ? 2 : 1;
+  const bool acts = act != FAST_ACT_NONE;
+  p.parts = dtype == FAST_F32 || acts;
   p.dz_blocks = (n + DZ_ROWS - 1) / DZ_ROWS;
-  const int64_t tiles = int64_t((M + 127) / 128) * ((K + 127) / 128);
-  int64_t s = std::max<int64_t>(1, 512 / (tiles * p.planes));
+  p.wide = acts && dtype == FAST_BF16 && K >= 512;
+  const int64_t tiles = int64_t((M + 127) / 128) * (p.wide ? (K + 255) / 256 : (K + 127) / 128);
+  int64_t s = std::max<int64_t>(1, 512 / tiles);
   s = std::min<int64_t>(s, (n + 255) / 256);
   s = std::max<int64_t>({s, (n + LIN_SPLIT_MAX - 1) / LIN_SPLIT_MAX, 1});
   p.rows = ((n + s - 1) / s + 63) / 64 * 64;
@@ -783,8 +1110,8 @@ static LinPlan lin_plan(int64_t n, int K, int M, fast_dtype_t dtype, fast_act_t 
 
 struct LinWork {
   char* wt;
-  char* dz;
-  char* rest;
+  float* dz;
+  uint16_t* near;
   float* part;
   float* sums;
 };
@@ -800,9 +1127,10 @@ static size_t lin_layout(int64_t n, int K, int M, fast_dtype_t dtype, fast_act_t
   };
   LinWork t;
   t.wt = take(int64_t(K) * lin_wt_ld(M, es) * es);
-  t.dz = act != FAST_ACT_NONE ? take(n * M * es) : nullptr;
-  t.rest = p.planes == 2 ? take(n * M * es) : nullptr;
-  t.part = reinterpret_cast<float*>(take(int64_t(p.splits) * p.planes * M * K * 4));
+  const bool acts = act != FAST_ACT_NONE;
+  t.dz = acts ? reinterpret_cast<float*>(take(n * M * 4)) : nullptr;
+  t.near = acts && dtype == FAST_BF16 ? reinterpret_cast<uint16_t*>(take(n * M * 2)) : nullptr;
+  t.part = reinterpret_cast<float*>(take(int64_t(p.splits) * M * K * 4));
   t.sums = reinterpret_cast<float*>(take((act != FAST_ACT_NONE ? p.dz_blocks : p.splits) * M * 4));
   if (w) *w = t;
   return at;
@@ -837,13 +1165,14 @@ static void lin_bwd(int64_t n, int K, int M, fast_dtype_t dtype, const void* x, 
   lin_layout(n, K, M, dtype, act, ws, &m);
   const bool acts = act != FAST_ACT_NONE;
   if (n > 0 && acts) {
-    DzArgs d = {n, lddy, M, act, (M + CHUNK<T> - 1) / CHUNK<T>, 0, dy, pre, m.dz, m.rest, dbias ? m.sums : nullptr};
+    DzArgs d = {n, lddy, M, act, (M + CHUNK<T> - 1) / CHUNK<T>, 0, dy, pre, dw || sizeof(T) == 4 ? m.dz : nullptr,
+                dx ? m.near : nullptr, dbias ? m.sums : nullptr};
     d.lanes = std::min(d.chunks, LIN_THREADS);
     const dim3 grid(uint32_t(p.dz_blocks), uint32_t((d.chunks + d.lanes - 1) / d.lanes));
     if (M < CHUNK<T>) hipLaunchKernelGGL((k_linear_dz<T, true>), grid, dim3(LIN_THREADS), 0, st, d);
     else hipLaunchKernelGGL((k_linear_dz<T, false>), grid, dim3(LIN_THREADS), 0, st, d);
   }
-  const void* dz = acts ? m.dz : dy;
+  const void* dz = !acts ? dy : (sizeof(T) == 4 ? static_cast<const void*>(m.dz) : m.near);   // of dx
   const int64_t lddz = acts ? M : lddy;
   if (dx && n > 0) {
     const int ld = lin_wt_ld(M, sizeof(T));
@@ -866,11 +1195,10 @@ static void lin_bwd(int64_t n, int K, int M, fast_dtype_t dtype, const void* x, 
       hipLaunchKernelGGL(k_linear_join, dim3(uint32_t((size + LJ_COLS - 1) / LJ_COLS)), dim3(LIN_THREADS), 0, st, part,
                          parts, size, out);
   };
-  const int64_t parts = n > 0 ? int64_t(p.splits) * p.planes : 0;
+  const int64_t parts = n > 0 ? int64_t(p.splits) : 0;
   if (n > 0 && (dw || (dbias && !acts))) {
     LinArgs a = {};
-    a.a = dz;
-    a.a2 = m.rest;
+    a.a = acts ? m.dz : dy;
     a.lda = lddz;
     a.b = x;
     a.ldb = ldx;
@@ -878,21 +1206,33 @@ static void lin_bwd(int64_t n, int K, int M, fast_dtype_t dtype, const void* x, 
     a.M = dw ? K : 1;                                   // (dbias alone: one tile of columns)
     a.K = n;
     a.rows = p.rows;
-    a.splits = p.splits;
     a.part = parts == 1 ? dw : m.part;
     a.sums = !dbias || acts ? nullptr : (parts == 1 ? dbias : m.sums);
-    auto launch = [&](auto product, auto one) {
-      typedef LinGrad Tile;
-      a.tiles_c = (a.M + Tile::BC - 1) / Tile::BC;
-      hipLaunchKernelGGL((k_linear_wgrad<T, Tile, decltype(product)::value, decltype(one)::value>),
-                         dim3(uint32_t(parts * ((M + Tile::BR - 1) / Tile::BR) * a.tiles_c)), dim3(Tile::THREADS), 0, st, a);
-    };
     const std::integral_constant<bool, true> yes;
     const std::integral_constant<bool, false> no;
-    if (dw && M > 1 && K > 1) launch(yes, no);
-    else if (dw) launch(yes, yes);
-    else if (M > 1) launch(no, no);
-    else launch(no, yes);
+    auto launch = [&](auto tile, auto product, auto one) {
+      typedef decltype(tile) Tile;
+      constexpr bool PRODUCT = decltype(product)::value, ONE = decltype(one)::value;
+      a.tiles_c = (a.M + Tile::BC - 1) / Tile::BC;
+      const dim3 grid(uint32_t(parts * ((M + Tile::BR - 1) / Tile::BR) * a.tiles_c));
+      if constexpr (std::is_same<Tile, LinGrad>::value)
+        hipLaunchKernelGGL((k_linear_wgrad<uint16_t, Tile, PRODUCT, ONE>), grid, dim3(Tile::THREADS), 0, st, a);
+      else
+        hipLaunchKernelGGL((k_linear_wgrad_parts<T, Tile, PRODUCT, ONE>), grid, dim3(Tile::THREADS), 0, st, a);
+    };
+    if constexpr (sizeof(T) == 4) {
+      if (dw) launch(LinMid(), yes, no);
+      else launch(LinMid(), no, no);
+    } else if (acts) {
+      if (p.wide) launch(LinWide(), yes, no);
+      else if (K > 1) launch(LinMid(), yes, no);
+      else launch(LinMid(), yes, yes);
+    } else {
+      if (dw && M > 1 && K > 1) launch(LinGrad(), yes, no);
+      else if (dw) launch(LinGrad(), yes, yes);
+      else if (M > 1) launch(LinGrad(), no, no);
+      else launch(LinGrad(), no, yes);
+    }
   }
   if (dw) join(m.part, parts, int64_t(M) * K, dw);
   if (dbias && acts) {                                  // a part per block of rows
