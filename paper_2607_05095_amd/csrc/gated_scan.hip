@@ -34,28 +34,20 @@ struct Gate {
   float a, u, k;                     // k: the slope of u over the gate, a dt sigmoid(gate)
 };
 
-// An event's time.  Where it is long, e^gate is formed 2^64 times as large and the time as much
-// smaller: a rate too small for fp32 counts over such a time.
-struct Span {
-  float dt, up, part, down;          // 2^up e^gate part = e^gate dt; 2^up e^gate down = e^gate
-};
-__device__ __forceinline__ Span span_of(float dt) {
-  dt = dt < 0.f ? 0.f : dt;
-  const bool l = dt > 0x1p20f;
-  return Span{dt, l ? 64.f : 0.f, l ? dt * 0x1p-64f : dt, l ? 0x1p-64f : 1.f};
-}
-
 // u = 1 - a keeps its relative accuracy for slow gates and a for fast ones.  No branches: the
 // evaluations of several events and columns interleave.
-template <bool SPAN>
-__device__ __forceinline__ Gate gate_of(float g, const Span& w) {
+// FAR: some gate is so low that e^gate, at most 2^-100 then, may lie below what fp32 holds; over a
+// long time it counts all the same, so it is formed 2^100 times as large and the time as much smaller.
+template <bool SPAN, bool FAR>
+__device__ __forceinline__ Gate gate_of(float g, float dt) {
   Gate q;
-  // t = e^-|g| 2^up within 3 U: the product with log2(e) in two parts (the second is no number
-  // where g is infinite, and 0 or close to it otherwise)
+  // t = e^-|g| within 3 U: the product with log2(e) in two parts (the second is no number where g is
+  // infinite, and 0 or close to it otherwise)
   const float x = fabsf(g), h = -x * 0x1.715476p+0f;
   float l = fmaf(-x, 0x1.715476p+0f, -h);
   l = __builtin_amdgcn_fmed3f(fmaf(-x, 0x1.4ae0cp-26f, l), -1.f, 1.f);
-  float ts = __builtin_amdgcn_exp2f(SPAN ? h + w.up : h);
+  const bool far = FAR && h < -100.f;
+  float ts = __builtin_amdgcn_exp2f(far ? h + 100.f : h);
   ts = fmaf(ts, l * 0x1.62e43p-1f, ts);
   const bool pos = g >= 0.f;
   if constexpr (!SPAN) {
@@ -65,7 +57,7 @@ __device__ __forceinline__ Gate gate_of(float g, const Span& w) {
     q.k = q.a * q.u;
     return q;
   }
-  const float t = ts * w.down;
+  const float t = far ? ts * 0x1p-100f : ts, part = far ? dt * 0x1p-100f : dt;
   // log(1 + t) / t on (0, 1], within 2^-27 (a weighted least-squares fit)
   float p = -0x1.a9330cp-9f;
   p = fmaf(p, t, 0x1.453edcp-6f);
@@ -77,7 +69,8 @@ __device__ __forceinline__ Gate gate_of(float g, const Span& w) {
   p = fmaf(p, t, 0x1.554c80p-2f);
   p = fmaf(p, t, -0x1.ffffbep-2f);
   p = fmaf(p, t, 1.f);
-  const float y = fmaf(p * ts, w.part, fmaxf(g, 0.f) * w.dt);          // rate dt
+  // rate dt
+  const float y = FAR ? fmaf(p * ts, part, fmaxf(g, 0.f) * dt) : fmaf(p, t, fmaxf(g, 0.f)) * dt;
   // (1 - e^-y) / y below log 2, within 2^-26; the difference above
   const float e = __builtin_amdgcn_exp2f(y * -0x1.715476p+0f);
   float s = -0x1.0ed322p-10f;
@@ -89,8 +82,32 @@ __device__ __forceinline__ Gate gate_of(float g, const Span& w) {
   q.u = y < 0.6931f ? s * y : 1.f - e;
   q.a = e;
   const float r = __builtin_amdgcn_rcpf(1.f + t);
-  q.k = e * (pos ? r * w.dt : ts * r * w.part);
+  q.k = e * (pos ? r * dt : ts * r * part);
   return q;
+}
+// Gates side by side, without branches among them: their evaluations interleave.
+template <bool SPAN, int COUNT, int VE>
+__device__ __forceinline__ void gates_of(const float (&g)[COUNT][VE], const float (&dt)[COUNT], Gate (&k)[COUNT][VE]) {
+  bool far = false;
+  if constexpr (SPAN) {
+    float low = 0.f;
+#pragma unroll
+    for (int j = 0; j < COUNT; ++j)
+#pragma unroll
+      for (int q = 0; q < VE; ++q) low = fminf(low, g[j][q]);
+    far = __any(low < -69.f);
+  }
+  if (far) {
+#pragma unroll
+    for (int j = 0; j < COUNT; ++j)
+#pragma unroll
+      for (int q = 0; q < VE; ++q) k[j][q] = gate_of<SPAN, SPAN>(g[j][q], dt[j]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < COUNT; ++j)
+#pragma unroll
+      for (int q = 0; q < VE; ++q) k[j][q] = gate_of<SPAN, false>(g[j][q], dt[j]);
+  }
 }
 
 // ------------------------------------------------------------------ rows
@@ -203,7 +220,12 @@ struct Rows {
       const uint32_t o = min(uint32_t(j) * ld, end);
       x[j].load(reinterpret_cast<const T*>(px + o));
       g[j].load(reinterpret_cast<const T*>(pg + o));
-      dt[j] = SPAN ? a.dt[e + min(j, m - 1)] : 1.f;
+      if constexpr (SPAN) {
+        const float d = a.dt[e + min(j, m - 1)];
+        dt[j] = d < 0.f ? 0.f : d;
+      } else {
+        dt[j] = 1.f;
+      }
     }
   }
 };
@@ -223,16 +245,14 @@ __device__ __forceinline__ void fwd_range(const GsArgs& a, int64_t b, int64_t p,
     for (int i = 0; i < GS_AHEAD; i += GS_SIDE) {
       if (!__any(i < m)) break;
       Gate k[GS_SIDE][VE];
-      float xv[GS_SIDE][VE];
+      float xv[GS_SIDE][VE], gv[GS_SIDE][VE], dt[GS_SIDE];
 #pragma unroll
       for (int j = 0; j < GS_SIDE; ++j) {
-        float gv[VE];
         r.x[i + j].get(xv[j]);
-        r.g[i + j].get(gv);
-        const Span w = span_of(r.dt[i + j]);
-#pragma unroll
-        for (int q = 0; q < VE; ++q) k[j][q] = gate_of<SPAN>(gv[q], w);
+        r.g[i + j].get(gv[j]);
+        dt[j] = r.dt[i + j];
       }
+      gates_of<SPAN>(gv, dt, k);
 #pragma unroll
       for (int j = 0; j < GS_SIDE; ++j)
         if (i + j < m) {
@@ -271,15 +291,21 @@ __device__ __forceinline__ void bwd_range(const GsArgs& a, int64_t v, int64_t b,
 #pragma unroll
     for (int i = 0; i < GS_WIN; i += GS_SIDE)
       if (__any(i < m)) {
+        Gate ys[GS_SIDE][VE];
+        float gv[GS_SIDE][VE], dt[GS_SIDE];
+#pragma unroll
+        for (int j = 0; j < GS_SIDE; ++j) {
+          r.g[i + j].get(gv[j]);
+          dt[j] = r.dt[i + j];
+        }
+        gates_of<SPAN>(gv, dt, ys);
 #pragma unroll
         for (int j = i; j < i + GS_SIDE; ++j) {
-          float xv[VE], gv[VE];
+          float xv[VE];
           r.x[j].get(xv);
-          r.g[j].get(gv);
-          const Span span = span_of(r.dt[j]);
 #pragma unroll
           for (int q = 0; q < VE; ++q) {
-            const Gate y = gate_of<SPAN>(gv[q], span);
+            const Gate y = ys[j - i][q];
             k[j][q] = y.k * (xv[q] - s[q]);
             s[q] = fmaf(y.a, s[q], y.u * xv[q]);           // (past the end: used no more)
             u[j][q] = y.u;
@@ -388,25 +414,29 @@ __device__ __forceinline__ void piece_sums(const GsArgs& a, int64_t k, int first
           for (int j = 0; j < GS_AHEAD; ++j) w.x[j].load(dh + min(j, m - 1) * a.D);
         }
       }
-      Gate y[GS_AHEAD][VE];
 #pragma unroll
-      for (int j = 0; j < GS_AHEAD; ++j) {
-        float gv[VE];
-        w.g[j].get(gv);
-        const Span span = span_of(w.dt[j]);
+      for (int ii = 0; ii < GS_AHEAD; ii += GS_SIDE) {
+        const int i = BACK ? GS_AHEAD - GS_SIDE - ii : ii;
+        Gate y[GS_SIDE][VE];
+        float gv[GS_SIDE][VE], dt[GS_SIDE];
 #pragma unroll
-        for (int q = 0; q < VE; ++q) y[j][q] = gate_of<SPAN>(gv[q], span);
-      }
+        for (int j = 0; j < GS_SIDE; ++j) {
+          w.g[i + j].get(gv[j]);
+          dt[j] = w.dt[i + j];
+        }
+        gates_of<SPAN>(gv, dt, y);
 #pragma unroll
-      for (int jj = 0; jj < GS_AHEAD; ++jj) {
-        const int j = BACK ? GS_AHEAD - 1 - jj : jj;
-        float xv[VE];
-        w.x[j].get(xv);
+        for (int jj = 0; jj < GS_SIDE; ++jj) {
+          const int j = BACK ? GS_SIDE - 1 - jj : jj;
+          float xv[VE];
+          w.x[i + j].get(xv);
 #pragma unroll
-        for (int q = 0; q < VE; ++q) {
-          const float in = BACK ? y[j][q].a * (pb[q] + (a.dh ? xv[q] : 0.f)) : fmaf(y[j][q].a, pb[q], y[j][q].u * xv[q]);
-          pb[q] = j < m ? in : pb[q];
-          pa[q] = j < m ? pa[q] * y[j][q].a : pa[q];
+          for (int q = 0; q < VE; ++q) {
+            const float in =
+                BACK ? y[j][q].a * (pb[q] + (a.dh ? xv[q] : 0.f)) : fmaf(y[j][q].a, pb[q], y[j][q].u * xv[q]);
+            pb[q] = i + j < m ? in : pb[q];
+            pa[q] = i + j < m ? pa[q] * y[j][q].a : pa[q];
+          }
         }
       }
     }

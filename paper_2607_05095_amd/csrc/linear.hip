@@ -115,19 +115,49 @@ __device__ __forceinline__ LinParts lin_split(const float* x, float& cut) {
 template <typename T> constexpr int LIN_PARTS = sizeof(T) == 4 ? 3 : 1;
 
 // ------------------------------------------------------------------ activations
+__device__ __forceinline__ float exp_down(float h) {       // e^-h, h >= 0
+  return __builtin_amdgcn_exp2f(h * -0x1.715476p+0f);
+}
+// Phi(-|z|) and phi(z) sqrt(2 pi): e^(-z^2 / 2) times half of e^(x^2) erfc(x) at x = |z| / sqrt 2, which is
+// t times a polynomial in t = 1 / (1 + 0.48 x), within 2^-21.5 (a weighted least-squares fit).
+__device__ __forceinline__ float2 gauss(float z) {
+  const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(z), 0x1.5b8ea0p-2f, 1.f)), e = exp_down(0.5f * z * z);
+  float p = -0x1.908a46p-5f;
+  p = fmaf(p, t, 0x1.0ed562p-2f);
+  p = fmaf(p, t, -0x1.0aae58p-1f);
+  p = fmaf(p, t, 0x1.853468p-2f);
+  p = fmaf(p, t, -0x1.2be910p-4f);
+  p = fmaf(p, t, 0x1.cbc510p-3f);
+  p = fmaf(p, t, 0x1.da3e00p-3f);
+  p = fmaf(p, t, 0x1.16153cp-2f);
+  p = fmaf(p, t, 0x1.1547b2p-2f);
+  return make_float2(0.5f * p * t * e, e);
+}
 __device__ __forceinline__ float act_of(int act, float z) {
   if (act == FAST_ACT_RELU) return z > 0.f ? z : (z == z ? 0.f : z);
-  if (act == FAST_ACT_GELU) return 0.5f * z * erfcf(z * -0x1.6a09e6p-1f);
-  if (act == FAST_ACT_SILU) return z / (1.f + expf(-z));
+  if (act == FAST_ACT_GELU) {
+    const float q = gauss(z).x;
+    return z * (z > 0.f ? 1.f - q : q);
+  }
+  if (act == FAST_ACT_SILU) {
+    const float r = __builtin_amdgcn_rcpf(1.f + exp_down(fabsf(z)));
+    // (far out e^z lies below the normal numbers, z e^z not yet: 2^100 times as much of it)
+    const float h = z * 0x1.715476p+0f;
+    const bool far = h < -100.f;
+    const float t = __builtin_amdgcn_exp2f(far ? h + 100.f : h);
+    return z > 0.f ? z * r : z * r * t * (far ? 0x1p-100f : 1.f);
+  }
   return z;
 }
 __device__ __forceinline__ float slope_of(int act, float z) {
   if (act == FAST_ACT_RELU) return z > 0.f ? 1.f : (z == z ? 0.f : z);
-  if (act == FAST_ACT_GELU)
-    return fmaf(0.5f, erfcf(z * -0x1.6a09e6p-1f), z * expf(-0.5f * z * z) * 0x1.988454p-2f);
+  if (act == FAST_ACT_GELU) {
+    const float2 g = gauss(z);
+    return fmaf(z * 0x1.988454p-2f, g.y, z > 0.f ? 1.f - g.x : g.x);
+  }
   if (act == FAST_ACT_SILU) {
-    const float p = 1.f / (1.f + expf(-z));
-    return p * fmaf(z, 1.f - p, 1.f);
+    const float t = exp_down(fabsf(z)), r = __builtin_amdgcn_rcpf(1.f + t), p = z > 0.f ? r : t * r;
+    return fmaf(z * p, z > 0.f ? t * r : r, p);            // p (1 + z (1 - p))
   }
   return 1.f;
 }
@@ -168,6 +198,7 @@ __device__ __forceinline__ void lin_each(F f) {
 // The epilogue of a lane: VE neighbouring columns, the same in every row that it finishes.
 template <typename T, int VE>
 struct LinEnd {
+  static constexpr bool CHUNKS = VE == CHUNK<T>;
   const LinArgs& p;
   int c, n;                          // first column, columns in the row
   float bias[VE];
@@ -175,14 +206,22 @@ struct LinEnd {
 #pragma unroll
     for (int j = 0; j < VE; ++j) bias[j] = p.bias && j < n ? p.bias[c + j] : 0.f;
   }
-  __device__ void finish(int64_t r, float* z) const {
+  // row r's chunk of res, ahead of its use (the row's last chunk, if it is not whole, and rows past
+  // the end load something else)
+  __device__ u32x4 ahead(int64_t r) const {
+    static_assert(CHUNKS, "whole chunks");
+    if (!p.res || p.M < VE) return u32x4{0u, 0u, 0u, 0u};
+    return lin_load(static_cast<const T*>(p.res) + min(r, p.n - 1) * p.ldres + (n >= VE ? c : 0));
+  }
+  __device__ void finish(int64_t r, float* z, u32x4 raw = u32x4{0u, 0u, 0u, 0u}) const {
     if (r >= p.n || n <= 0) return;
     float t[VE];
     const T* res = p.res ? static_cast<const T*>(p.res) + r * p.ldres + c : nullptr;
     T* pre = p.pre ? static_cast<T*>(p.pre) + r * p.M + c : nullptr;
     T* y = static_cast<T*>(p.y) + r * p.ldy + c;
-    if constexpr (VE == CHUNK<T>) {
-      if (res) load_chunk(res, n, t);
+    if constexpr (CHUNKS) {
+      if (n >= VE) lin_unpack(T(), raw, t);
+      else if (res) load_chunk(res, n, t);
     } else {
 #pragma unroll
       for (int j = 0; j < VE; ++j) {
@@ -204,7 +243,7 @@ struct LinEnd {
     put(y, z);
   }
   __device__ void put(T* o, const float* z) const {
-    if constexpr (VE == CHUNK<T>) {
+    if constexpr (CHUNKS) {
       store_chunk(o, n, z);
     } else {
 #pragma unroll
@@ -225,7 +264,7 @@ struct LinTile {
   // (the epilogue takes 32 rows of every wave's block through it)
   static constexpr int LDS = 2 * BUF > WR * WC * 32 * (TC * 32 + 4) * 4 ? 2 * BUF : WR * WC * 32 * (TC * 32 + 4) * 4;
 };
-typedef LinTile<2, 4, 4, 2, 128> LinBig;   // 256 x 256
+typedef LinTile<4, 2, 2, 2, 64> LinBig;    // 256 x 128
 typedef LinTile<2, 2, 2, 2, 64> LinMid;    // 128 x 128
 typedef LinTile<2, 2, 2, 2, 128> LinGrad;  // 128 x 128 of weight gradients
 typedef LinTile<2, 4, 2, 2, 64> LinWide;   // 128 x 256
@@ -294,14 +333,18 @@ __device__ __forceinline__ void lin_clear(f32x16_t (&acc)[TR][TC]) {
 }
 
 // The wave's block through LDS, 32 rows at a time, so that rows leave in whole chunks.
-// out(row of the wave's block, values): of VE columns from (lane % (TC * 32 / VE)) * VE on.
-template <int VE, int TR, int TC, typename F>
-__device__ __forceinline__ void lin_out(char* lds, const f32x16_t (&acc)[TR][TC], F out) {
-  constexpr int W = TC * 32, LD = W + 4, PER = W / VE, ROWS = 64 / PER;
+// ahead(row of the wave's block): what out will want, on its way before the block is turned;
+// out(row, values, that): of VE columns from (lane % (TC * 32 / VE)) * VE on.
+template <int VE, int TR, int TC, typename G, typename F>
+__device__ __forceinline__ void lin_out(char* lds, const f32x16_t (&acc)[TR][TC], G ahead, F out) {
+  constexpr int W = TC * 32, LD = W + 4, PER = W / VE, ROWS = 64 / PER, COUNT = 32 / ROWS;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   float* buf = reinterpret_cast<float*>(lds) + wave * 32 * LD;
   lin_each<TR>([&](auto I) {
     constexpr int i = decltype(I)::value;
+    u32x4 raw[COUNT];
+#pragma unroll
+    for (int q = 0; q < COUNT; ++q) raw[q] = ahead(i * 32 + q * ROWS + lane / PER);
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < TC; ++j)
@@ -310,8 +353,8 @@ __device__ __forceinline__ void lin_out(char* lds, const f32x16_t (&acc)[TR][TC]
         *reinterpret_cast<f32x4*>(buf + (lane & 31) * LD + j * 32 + q * 8 + (lane >> 5) * 4) =
             f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
     __syncthreads();
-#pragma unroll 2
-    for (int q = 0; q < 32 / ROWS; ++q) {
+#pragma unroll
+    for (int q = 0; q < COUNT; ++q) {
       const int r = q * ROWS + lane / PER, c = lane % PER * VE;
       float z[VE];
 #pragma unroll
@@ -319,7 +362,7 @@ __device__ __forceinline__ void lin_out(char* lds, const f32x16_t (&acc)[TR][TC]
         const f32x4 w = *reinterpret_cast<const f32x4*>(buf + r * LD + c + v);
         z[v] = w.x; z[v + 1] = w.y; z[v + 2] = w.z; z[v + 3] = w.w;
       }
-      out(i * 32 + r, z);
+      out(i * 32 + r, z, raw[q]);
     }
   });
 }
@@ -401,7 +444,9 @@ __global__ void __launch_bounds__(Tile::THREADS) k_linear(LinArgs p) {
     __syncthreads();
   }
   const LinEnd<T, VE> end(p, c0 + wc * TC * 32 + (threadIdx.x & 63) % (TC * 32 / VE) * VE);
-  lin_out<VE>(lds, acc, [&](int r, float* z) { end.finish(r0 + wr * TR * 32 + r, z); });
+  const int64_t rw = r0 + wr * TR * 32;
+  lin_out<VE>(lds, acc, [&](int r) { return end.ahead(rw + r); },
+              [&](int r, float* z, u32x4 raw) { end.finish(rw + r, z, raw); });
 }
 
 // k_linear of fp32 rows in parts; K >= 8.  One buffer in LDS, so that two workgroups share a CU:
@@ -497,7 +542,9 @@ __global__ void __launch_bounds__(Tile::THREADS) k_linear_parts(LinArgs p) {
     }
   }
   const LinEnd<float, 4> end(p, c0 + wc * TC * 32 + lane % (TC * 8) * 4);
-  lin_out<4>(lds, acc, [&](int r, float* z) { end.finish(r0 + wr * TR * 32 + r, z); });
+  const int64_t rw = r0 + wr * TR * 32;
+  lin_out<4>(lds, acc, [&](int r) { return end.ahead(rw + r); },
+             [&](int r, float* z, u32x4 raw) { end.finish(rw + r, z, raw); });
 }
 
 // Few rows: 32 x 32 results a workgroup, its waves share k, each feeding the matrix unit from
@@ -513,6 +560,11 @@ __global__ void __launch_bounds__(64 * WAVES) k_linear_few(LinArgs p) {
   const int c = min(c0 + (lane & 31), p.M - 1);
   const T* ga = static_cast<const T*>(p.a) + r * p.lda;
   const T* gb = static_cast<const T*>(p.b) + int64_t(c) * p.ldb;
+  constexpr int VO = 16 / WAVES;                          // results of a thread
+  const int t = threadIdx.x * VO;
+  const LinEnd<T, VO> end(p, c0 + t % 32);
+  u32x4 raw = {0u, 0u, 0u, 0u};
+  if constexpr (LinEnd<T, VO>::CHUNKS) raw = end.ahead(r0 + t / 32);
   f32x16_t acc;
 #pragma unroll
   for (int q = 0; q < 16; ++q) acc[q] = 0.f;
@@ -544,8 +596,6 @@ __global__ void __launch_bounds__(64 * WAVES) k_linear_few(LinArgs p) {
     *reinterpret_cast<f32x4*>(&buf[wave][(lane & 31) * LD + q * 8 + half * 4]) =
         f32x4{acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]};
   __syncthreads();
-  constexpr int VO = 16 / WAVES;
-  const int t = threadIdx.x * VO;
   float z[VO];
 #pragma unroll
   for (int v = 0; v < VO; ++v) z[v] = 0.f;
@@ -553,8 +603,7 @@ __global__ void __launch_bounds__(64 * WAVES) k_linear_few(LinArgs p) {
   for (int w = 0; w < WAVES; ++w)
 #pragma unroll
     for (int v = 0; v < VO; ++v) z[v] += buf[w][t / 32 * LD + t % 32 + v];
-  const LinEnd<T, VO> end(p, c0 + t % 32);
-  end.finish(r0 + t / 32, z);
+  end.finish(r0 + t / 32, z, raw);
 }
 
 // ------------------------------------------------------------------ weight gradients
@@ -727,7 +776,7 @@ __global__ void __launch_bounds__(Tile::THREADS) k_linear_wgrad(LinArgs p) {
   if constexpr (PRODUCT) {
     float* part = p.part + int64_t(split) * p.n * p.M;
     const int col = c0 + wc * TC * 32 + (threadIdx.x & 63) % (TC * 8) * 4;
-    lin_out<4>(lds, acc, [&](int r, float* z) {
+    lin_out<4>(lds, acc, [](int) { return u32x4{0u, 0u, 0u, 0u}; }, [&](int r, float* z, u32x4) {
       const int64_t row = r0 + wr * TR * 32 + r;
       if (row < p.n && col < p.M) store_chunk_of(part + row * p.M + col, p.M - col, z);
     });
@@ -902,7 +951,7 @@ __global__ void __launch_bounds__(Tile::THREADS) k_linear_wgrad_parts(LinArgs p)
   if constexpr (PRODUCT) {
     float* part = p.part + int64_t(split) * p.n * p.M;
     const int col = c0 + wc * TC * 32 + lane % (TC * 8) * 4;
-    lin_out<4>(lds, acc, [&](int r, float* z) {
+    lin_out<4>(lds, acc, [](int) { return u32x4{0u, 0u, 0u, 0u}; }, [&](int r, float* z, u32x4) {
       const int64_t row = r0 + wr * TR * 32 + r;
       if (row < p.n && col < p.M) store_chunk_of(part + row * p.M + col, p.M - col, z);
     });
@@ -1035,10 +1084,10 @@ __global__ void __launch_bounds__(LIN_THREADS) k_linear_turn(const T* __restrict
 }
 
 // ------------------------------------------------------------------ host side
-// Long products into wide rows take 256 x 256: a tile of 128 x 128 reads twice the operands
-// from L2 (40,000 x 2048 x 2048 bf16 457 against 548 us, 8192^3 1068 / 1697; the library 349 / 728).
-// Otherwise several workgroups per CU count for more: 264,000 x 272 x 256 bf16 105 / 96,
-// x 256 x 272 146 / 93 (the library 148 / 155), x 372 x 200 fp32 538 / 469 (564).
+// Long products into wide rows take 256 x 128, which reads a quarter less from L2 than 128 x 128
+// (40,000 x 2048 x 2048 bf16 485 against 548 us, 8192^3 1178 / 1697; the library 349 / 728;
+// 256 x 256 leaves one workgroup per CU, whose epilogue nothing hides).  Otherwise more workgroups per
+// CU count for as much: 264,000 x 272 x 256 bf16 96, x 256 x 272 93 (the library 148, 155).
 static bool lin_big(int64_t n, int M, int64_t K) {
   return K >= 1024 && M >= 512 && ((n + 255) / 256) * ((M + 255) / 256) >= 256;
 }
