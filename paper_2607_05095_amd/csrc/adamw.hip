@@ -452,6 +452,7 @@ extern "C" fast_status_t fast_adamw(const fast_adamw_tensor_t* tensors, int coun
   int64_t blocks = 0;
   for (int j = 0; j < count; ++j) blocks += (tensors[j].n + chunk - 1) / chunk;
   if (!grid_fits(blocks, AW_THREADS)) return fail(FAST_ERR_UNSUPPORTED, "%s: 2^32 threads or more", fn);
+  if (blocks == 0) return ok();
   auto launch = [&] {
     if (a.count == 0) return;
     const dim3 grid(a.first[a.count]);
