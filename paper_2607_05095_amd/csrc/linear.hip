@@ -23,6 +23,7 @@ constexpr int64_t LIN_MAX_LD = 1 << 22;   // elements from row to row: a tile's 
 constexpr int LIN_THREADS = 256;
 
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 
 __device__ __forceinline__ void lin_mma(uint16_t, const u32x4& a, const u32x4& b, f32x16_t& c) {
@@ -72,6 +73,20 @@ __device__ __forceinline__ void lin_unpack(uint16_t, const u32x4& w, float* x) {
     x[2 * j] = bf16_lo(w[j]);
     x[2 * j + 1] = bf16_hi(w[j]);
   }
+}
+// bf16: elements skip, skip + 1, ... of a chunk moved to its start, zeros behind them (0 <= skip < 8)
+__device__ __forceinline__ u32x4 lin_shift(const u32x4& w, int skip) {
+  uint64_t lo = uint64_t(w[1]) << 32 | w[0], hi = uint64_t(w[3]) << 32 | w[2];
+  if (skip >= 4) {
+    lo = hi;
+    hi = 0;
+    skip -= 4;
+  }
+  if (skip > 0) {
+    lo = lo >> (16 * skip) | hi << (64 - 16 * skip);
+    hi >>= 16 * skip;
+  }
+  return u32x4{uint32_t(lo), uint32_t(lo >> 32), uint32_t(hi), uint32_t(hi >> 32)};
 }
 template <typename T>
 __device__ __forceinline__ u32x4 lin_mask(int skip) {
@@ -606,6 +621,93 @@ __global__ void __launch_bounds__(64 * WAVES) k_linear_few(LinArgs p) {
   end.finish(r0 + t / 32, z, raw);
 }
 
+// Many narrow bf16 rows: the weights stay in LDS, a wave holds 32 whole rows as the matrix unit's
+// operand in registers, loads the next 32 while it multiplies the last columns, and waits for no
+// other wave.  Columns lie in LDS in the order in which a lane's results are 8 neighbours of one
+// row: 16 bytes to store, 64 a row and instruction (8 bytes, 16 a row: 95 us for 77 at 264000 rows of
+// 272 x 256).  3.6 TB/s there, 5.1 at 100 x 64; 12 waves take 81 us, 16 spill.  STEPS: 32-element steps
+// of k.  C = A B^T + bias.
+constexpr int LS_WAVES = 8, LS_LDS = 156 * 1024, LS_STEPS = 9;
+template <int STEPS>
+__global__ void __launch_bounds__(64 * LS_WAVES) k_linear_stream(LinArgs p) {
+  constexpr int ROW = STEPS * 64 + 16, C = STEPS * 4;
+  __shared__ __attribute__((aligned(16))) char s_w[LS_LDS];    // [groups of 32][ROW], then the bias
+  const int K = int(p.K), groups = (p.M + 31) / 32;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, i = lane & 15;
+  const uint16_t* A = static_cast<const uint16_t*>(p.a);
+  const uint16_t* B = static_cast<const uint16_t*>(p.b);
+  float* s_bias = reinterpret_cast<float*>(s_w + groups * 32 * ROW);
+  for (int t = threadIdx.x; t < groups * 32 * C; t += 64 * LS_WAVES) {
+    const int m = t / C, c = t % C * 8, at = min(c, K - 8);
+    const int slot = (m & ~31) | (m & 4) << 2 | (m & 24) >> 1 | (m & 3);
+    u32x4 v = lin_load(B + int64_t(min(m, p.M - 1)) * p.ldb + at);
+    if (c != at) v = c < K ? lin_shift(v, c - at) : u32x4{0u, 0u, 0u, 0u};
+    *reinterpret_cast<u32x4*>(s_w + slot * ROW + c * 2) = v;
+  }
+  for (int t = threadIdx.x; t < groups * 32; t += 64 * LS_WAVES)
+    s_bias[t] = p.bias && t < p.M ? p.bias[t] : 0.f;
+  __syncthreads();
+  const uint32_t wg = xcd_tile(blockIdx.x, gridDim.x);
+  const int64_t tiles = (p.n + 31) / 32, t0 = tiles * wg / gridDim.x, t1 = tiles * (wg + 1) / gridDim.x;
+  u32x4 a[2][STEPS];
+  auto load = [&](int64_t tile) {
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      const uint16_t* x = A + min(tile * 32 + r * 16 + i, p.n - 1) * p.lda;
+#pragma unroll
+      for (int s = 0; s < STEPS; ++s) a[r][s] = lin_load(x + min(s * 32 + g * 8, K - 8));
+    }
+  };
+  // a chunk that passes K was loaded moved back to end there
+  const int last = K / 8, skip = K % 8 ? 8 - K % 8 : 0;
+  const char* wl = s_w + i * ROW + g * 16;
+  int64_t tile = t0 + wave;
+  if (tile < t1) load(tile);
+  for (; tile < t1; tile += LS_WAVES) {
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+      const int c = 4 * s + g;
+      if (c >= last)
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+          a[r][s] = c == last && skip ? lin_shift(a[r][s], skip) : u32x4{0u, 0u, 0u, 0u};
+    }
+    for (int b = 0; b < groups; ++b) {
+      f32x4_t acc[2][2];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) acc[q & 1][q >> 1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      const char* w = wl + b * 32 * ROW;
+#pragma unroll
+      for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const bf16x8_t wf = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4*>(w + h * 16 * ROW + s * 64));
+#pragma unroll
+          for (int r = 0; r < 2; ++r)
+            acc[r][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf, __builtin_bit_cast(bf16x8_t, a[r][s]), acc[r][h], 0, 0, 0);
+        }
+      if (b + 1 == groups && tile + LS_WAVES < t1) load(tile + LS_WAVES);
+      const int c = b * 32 + g * 8, left = p.M - c;
+      const f32x4 b0 = *reinterpret_cast<const f32x4*>(s_bias + c), b1 = *reinterpret_cast<const f32x4*>(s_bias + c + 4);
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const int64_t row = tile * 32 + r * 16 + i;
+        if (row >= p.n) continue;
+        uint16_t* y = static_cast<uint16_t*>(p.y) + row * p.ldy + c;
+        const u32x4 v{bf16_pack(acc[r][0][0] + b0.x, acc[r][0][1] + b0.y), bf16_pack(acc[r][0][2] + b0.z, acc[r][0][3] + b0.w),
+                      bf16_pack(acc[r][1][0] + b1.x, acc[r][1][1] + b1.y), bf16_pack(acc[r][1][2] + b1.z, acc[r][1][3] + b1.w)};
+        if (left >= 8) {
+          *reinterpret_cast<u32x4_e*>(y) = v;
+        } else {
+#pragma unroll
+          for (int e = 0; e < 7; ++e)
+            if (e < left) y[e] = uint16_t(v[e >> 1] >> (16 * (e & 1)));
+        }
+      }
+    }
+  }
+}
+
 // ------------------------------------------------------------------ weight gradients
 // Rows of A and B side by side in memory are k here: 64 rows of bf16 (32 of fp32) are read a
 // few columns per thread, turned in registers and put into LDS as in k_linear.
@@ -1091,6 +1193,17 @@ __global__ void __launch_bounds__(LIN_THREADS) k_linear_turn(const T* __restrict
 static bool lin_big(int64_t n, int M, int64_t K) {
   return K >= 1024 && M >= 512 && ((n + 255) / 256) * ((M + 255) / 256) >= 256;
 }
+constexpr int LS_GRID = 256;                // workgroups: one per CU
+// The streaming kernel's rule: rows that a wave's registers and weights that LDS hold, and enough of
+// them to pay for bringing the weights to every CU.  At 264000 rows, in x out, against 128 x 128 tiles:
+// 272 x 256 77 us and 111, 256 x 256 74 and 80, 200 x 200 49 and 73, 100 x 64 17 and 31; at 16384 rows
+// 12.6 and 12.2, 11.1 and 11.3, 100 x 64 6.6 and 6.9; at 4096 11.9 and 8.1.
+constexpr int64_t LS_ROWS = 16384;
+static int ls_steps(int64_t K) { return K <= 64 ? 2 : K <= 128 ? 4 : K <= 192 ? 6 : int((K + 31) / 32); }
+static bool ls_use(const LinArgs& a) {
+  return a.act == FAST_ACT_NONE && !a.res && a.K >= 8 && a.K <= 32 * LS_STEPS && a.n >= LS_ROWS &&
+         (a.M + 31) / 32 * 32 * (ls_steps(a.K) * 64 + 20) <= LS_LDS;
+}
 template <typename T, typename Tile>
 static void lin_tiled(LinArgs& a, hipStream_t st) {
   a.tiles_c = (a.M + Tile::BC - 1) / Tile::BC;
@@ -1115,6 +1228,17 @@ static void lin_product(LinArgs a, hipStream_t st) {
     }
   }
   if constexpr (sizeof(T) == 2) {
+    if (ls_use(a)) {
+      const dim3 grid(LS_GRID), block(64 * LS_WAVES);
+      const int steps = ls_steps(a.K);
+      if (steps == 2) hipLaunchKernelGGL((k_linear_stream<2>), grid, block, 0, st, a);
+      else if (steps == 4) hipLaunchKernelGGL((k_linear_stream<4>), grid, block, 0, st, a);
+      else if (steps == 6) hipLaunchKernelGGL((k_linear_stream<6>), grid, block, 0, st, a);
+      else if (steps == 7) hipLaunchKernelGGL((k_linear_stream<7>), grid, block, 0, st, a);
+      else if (steps == 8) hipLaunchKernelGGL((k_linear_stream<8>), grid, block, 0, st, a);
+      else hipLaunchKernelGGL((k_linear_stream<9>), grid, block, 0, st, a);
+      return;
+    }
     if (lin_big(a.n, a.M, a.K)) {
       lin_tiled<T, LinBig>(a, st);
       return;

@@ -85,6 +85,15 @@ def test_linear_fwd(n, K, M, dt, wide):
     check_fwd(n, K, M, dt, k, (n + M) % 2 == 0, wide)
 
 
+@pytest.mark.parametrize("K,M", [(8, 1), (9, 33), (15, 7), (31, 32), (63, 64), (65, 31), (100, 172), (129, 40), (187, 100),
+                                 (200, 200), (224, 9), (225, 250), (256, 288), (272, 256), (287, 225), (288, 3), (64, 960)])
+@pytest.mark.parametrize("wide", [False, True])
+def test_linear_narrow_long(K, M, wide):
+    """Many rows, a few columns: weights that a compute unit's memory just holds and just does not,
+    lengths on both sides of the matrix unit's steps, a last group of rows that is not whole."""
+    check_fwd(16384 + K, K, M, "bf16", "none", False, wide, seed=30)
+
+
 @pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 @pytest.mark.parametrize("n,K,M", [(70, 50, 90), (16500, 33, 300)])
