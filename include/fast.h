@@ -691,9 +691,11 @@ fast_status_t fast_edge_attention_fwd_cached(const fast_tcsr_t* g, int H, int dh
  * fp32, NULL for none; res, y: rows of `out` elements of dtype, ldres and ldy apart
  * (res NULL for none); pre: [n, out] of dtype, optional, only with an activation.
  * y may be res with ldy = ldres; y and pre lie apart from every other array
- * (spans of their rows that meet are refused).  Products of dtype's values are exact
- * or rounded to fp32, sums fp32.  Whatever n, ldx and the alignment, a row's result does
- * not depend on the other rows' values.
+ * (spans of their rows that meet are refused).  Sums are fp32.  bf16 products are exact in
+ * them; fp32 products are rounded, or, where rows are many, formed from three bf16 parts of each
+ * value and then within 2^-22 |x w| (2^-126 |x| or |w| where the other is smaller than 2^-100).
+ * How a row's sums are rounded may depend on n and on whether rows near it are finite;
+ * an infinity or a NaN reaches its own row (or, in w, its own column) alone.
  * Limits: in, out <= 16384, n < 2^31, strides < 2^22, and fewer than 2^32 threads.
  * ------------------------------------------------------------------------ */
 typedef enum {
@@ -715,8 +717,9 @@ fast_status_t fast_linear_fwd(int64_t n, int in, int out, fast_dtype_t dtype, co
  * pre: the forward's (needed with an activation, refused without).  dx: rows of `in`
  * elements of dtype, lddx apart, apart from every input; dw: [out, in] fp32, dbias:
  * [out] fp32, both overwritten (zeros when n = 0); each of the three may be NULL, w
- * where dx is, x where dw is.  Sums over rows: fp32 over a few thousand rows, fp64
- * beyond, in a fixed order (repeated calls give the same bits).
+ * where dx is, x where dw is.  dz is fp32; with an activation bf16 products read it rounded
+ * to bf16 for dx, and in three parts for dw.  Sums over rows: fp32 over at most 16384 rows,
+ * fp64 beyond, in a fixed order (repeated calls give the same bits).
  * Workspace: fast_linear_bwd_workspace(n, in, out, dtype, act) bytes, 256-byte aligned;
  * one for the largest n serves smaller ones. */
 size_t fast_linear_bwd_workspace(int64_t n, int in, int out, fast_dtype_t dtype, fast_act_t act);

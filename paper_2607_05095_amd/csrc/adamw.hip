@@ -2,7 +2,7 @@
 //   g = scale grad,  m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) g^2
 //   w = w - lr (decay w + (m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps))
 //
-// Bound by HBM: 28 bytes an element with fp32 states and gradients, 16 (and a 16th) with
+// Bound by HBM: 28 bytes an element with fp32 states and gradients, 16 (and an eighth) with
 // states in 8 bits.  A launch takes the descriptors of up to AW_TENSORS tensors as
 // arguments and cuts them into chunks of AW_UNIT elements, a workgroup each; a thread
 // moves 4 of them, so 8 neighbouring lanes hold the 32 elements that

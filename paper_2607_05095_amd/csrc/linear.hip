@@ -1189,7 +1189,7 @@ __global__ void __launch_bounds__(LIN_THREADS) k_linear_turn(const T* __restrict
 // Long products into wide rows take 256 x 128, which reads a quarter less from L2 than 128 x 128
 // (40,000 x 2048 x 2048 bf16 485 against 548 us, 8192^3 1178 / 1697; the library 349 / 728;
 // 256 x 256 leaves one workgroup per CU, whose epilogue nothing hides).  Otherwise more workgroups per
-// CU count for as much: 264,000 x 272 x 256 bf16 96, x 256 x 272 93 (the library 148, 155).
+// CU count for more: 128 x 128.
 static bool lin_big(int64_t n, int M, int64_t K) {
   return K >= 1024 && M >= 512 && ((n + 255) / 256) * ((M + 255) / 256) >= 256;
 }
@@ -1216,14 +1216,23 @@ static void lin_tiled(LinArgs& a, hipStream_t st) {
   }
   hipLaunchKernelGGL((k_linear<T, Tile, false>), grid, dim3(Tile::THREADS), 0, st, a);
 }
-constexpr int64_t LIN_PARTS_K = 64;       // products of fp32 rows in parts from this length on
+// Tiles of 128 x 128 from as many of them on (columns counted in 32s); below, 32 x 32 a workgroup
+// gives more workgroups and shorter walks.  Tiles against 32 x 32 at `tiles` x 256 columns, us: bf16,
+// k = 64 / 1024, 64 tiles 7.3 and 7.7 / 18.6 and 21.7, 32 tiles 7.4 and 5.6 / 18.4 and 11.3; fp32 128
+// tiles 13.5 and 14.0 / 69 and 82, 96 tiles 13.2 and 11.1 / 68 and 63.
+template <typename T>
+static bool lin_many(int64_t n, int M) {
+  return n * ((M + 31) / 32 * 32) >= (sizeof(T) == 4 ? 128 : 64) * 16384;
+}
+// Products of fp32 rows in parts from this length on: 264,000 rows into 200 columns in parts against
+// fp32 instructions, k = 200 252 us and 288, 100 183 / 187, 64 126 / 130, 48 119 / 109, 16 95 / 68.
+constexpr int64_t LIN_PARTS_K = 64;
 template <typename T>
 static void lin_product(LinArgs a, hipStream_t st) {
   if constexpr (sizeof(T) == 4) {
-    const int64_t tiles = (a.n + 127) / 128 * ((a.M + 127) / 128);
-    if (tiles >= 256 && a.K >= LIN_PARTS_K) {
+    if (lin_many<T>(a.n, a.M) && a.K >= LIN_PARTS_K) {
       a.tiles_c = (a.M + 127) / 128;
-      hipLaunchKernelGGL((k_linear_parts<LinMid>), dim3(uint32_t(tiles)), dim3(LinMid::THREADS), 0, st, a);
+      hipLaunchKernelGGL((k_linear_parts<LinMid>), dim3(uint32_t((a.n + 127) / 128 * a.tiles_c)), dim3(LinMid::THREADS), 0, st, a);
       return;
     }
   }
@@ -1244,10 +1253,12 @@ static void lin_product(LinArgs a, hipStream_t st) {
       return;
     }
   }
-  if ((a.n + 127) / 128 * ((a.M + 127) / 128) >= 256) {
+  if (lin_many<T>(a.n, a.M)) {
     lin_tiled<T, LinMid>(a, st);
     return;
   }
+  // (4 waves share k up to 1024 bytes of it, 16 beyond: 64 rows, 256 columns, bf16 k = 1024 6.5 and 6.1
+  // us; at k = 256 fp32 5.7 and 7.3)
   a.tiles_c = (a.M + 31) / 32;
   const dim3 grid(uint32_t((a.n + 31) / 32 * a.tiles_c));
   if (a.K < CHUNK<T>) hipLaunchKernelGGL((k_linear_few<T, 4, true>), grid, dim3(256), 0, st, a);
@@ -1492,7 +1503,8 @@ extern "C" fast_status_t fast_linear_bwd(int64_t n, int in, int out, fast_dtype_
   if (!ws || ws_bytes < need)
     return fail(FAST_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", fn, ws ? ws_bytes : 0, need);
   if (!aligned(ws, 256)) return fail(FAST_ERR_UNSUPPORTED, "%s: workspace not 256-byte aligned", fn);
-  if (!lin_fits(n, in) || !grid_fits((int64_t(in) * out + LJ_COLS - 1) / LJ_COLS, LIN_THREADS)) return fail(FAST_ERR_UNSUPPORTED, "%s: 2^32 threads or more", fn);
+  if (!lin_fits(n, in) || !grid_fits((int64_t(in) * out + LJ_COLS - 1) / LJ_COLS, LIN_THREADS))
+    return fail(FAST_ERR_UNSUPPORTED, "%s: 2^32 threads or more", fn);
   const int64_t sw = int64_t(in) * out;
   const struct { const void* p; int64_t n; } reads[] = {{dw ? x : nullptr, span(n, in, ldx, es)},
                                                         {dx ? w : nullptr, sw * es},

@@ -141,10 +141,10 @@ def check_bwd(n, K, M, dt, kind, wide, seed=40):
     low = dt == "bf16" and kind != "none"
     tdz = (np.abs(dy64) * slope_error(kind, pre64) + 2 * U * np.abs(dz)) if kind != "none" else 0 * dz
     a = np.abs(dz)
-    # dx: bf16 products read dz rounded; dw: in two parts, which leave a rounding of the rounding
+    # dx: bf16 products read dz rounded; dw: in three parts, which hold all of it
     tx = (tdz + (HALF[dt] * a if low else 0)) @ np.abs(w64) * 1.01 + 2 * (M + 3) * U * (a @ np.abs(w64))
     within(dx[:n, :K], rx, tx * (1 + HALF[dt]) + HALF[dt] * np.abs(rx), "dx")
-    tw = (tdz + (HALF[dt] ** 2 * a if low else 0)).T @ np.abs(x64) * 1.01
+    tw = tdz.T @ np.abs(x64) * 1.01
     tw = tw + 2 * (min(n, 16384) + 3) * U * (a.T @ np.abs(x64)) + U * np.abs(rw)
     within(dw[:M], rw, tw, "dw")
     within(db[:M], rb, tdz.sum(0) * 1.01 + 70 * U * a.sum(0) + U * np.abs(rb), "dbias")
