@@ -228,6 +228,8 @@ def _check(st: int):
 
 def _rows_as_said(t, F, ld):
     """A view's rows are F elements side by side, ld apart; raises otherwise."""
+    if t.dim() == 2 and t.shape[1] == F and t.stride() == (ld, 1):
+        return
     side = 1                             # elements side by side, from the last dimension on
     outer = []
     for size, step in zip(reversed(t.shape), reversed(t.stride())):
@@ -244,25 +246,25 @@ def _rows_as_said(t, F, ld):
                            f"are not {F} elements side by side, {ld} apart")
 
 
-def _resident(dense=(), rows=(), F=0):
-    """Tensors of a call live on the current device, and are contiguous or, as (tensor, stride) in
+def _resident(dense=(), rows=()):
+    """Tensors of a call live on the current device, and are contiguous or, as (tensor, stride, F) in
     `rows`, views of rows of F elements that far apart; raises otherwise."""
     import torch
-    dev = None
+    dev = None                           # (asked of the runtime directly: with a tensor there it is up)
     for t in dense:
         if t is None or isinstance(t, int):
             continue
         if dev is None and t.is_cuda:
-            dev = torch.cuda.current_device()
+            dev = torch._C._cuda_getDevice()
         if t.get_device() != dev:
             raise FastError(1, f"tensor on {t.device}, not on the current GPU")
         if not t.is_contiguous():
             raise FastError(1, f"tensor of shape {tuple(t.shape)} is not contiguous")
-    for t, ld in rows:
+    for t, ld, F in rows:
         if t is None or isinstance(t, int):
             continue
         if dev is None and t.is_cuda:
-            dev = torch.cuda.current_device()
+            dev = torch._C._cuda_getDevice()
         if t.get_device() != dev:
             raise FastError(1, f"tensor on {t.device}, not on the current GPU")
         if not t.is_contiguous():        # contiguous tensors hold rows of any stride
@@ -560,7 +562,7 @@ def fast_layer_norm_bwd(n, D, dtype, h, gamma, mean, rstd, dy, dsum, dx, dgamma,
 def fast_rotary_fwd(n, H, dh, dtype, x, ldx, pos, axes, axis, omega, pairs, interleaved, y, ldy,
                     stream=None):
     """x and y may be views whose rows are ldx and ldy elements apart."""
-    _resident((pos, axis, omega), ((x, ldx), (y, ldy)), H * dh)
+    _resident((pos, axis, omega), ((x, ldx, H * dh), (y, ldy, H * dh)))
     _check(lib().fast_rotary_fwd(n, H, dh, dtype, _ptr(x), ldx, _ptr(pos), axes, _ptr(axis),
                                  _ptr(omega), pairs, int(interleaved), _ptr(y), ldy,
                                  _stream(stream)))
@@ -568,7 +570,7 @@ def fast_rotary_fwd(n, H, dh, dtype, x, ldx, pos, axes, axis, omega, pairs, inte
 
 def fast_rotary_bwd(n, H, dh, dtype, dy, lddy, pos, axes, axis, omega, pairs, interleaved, dx, lddx,
                     stream=None):
-    _resident((pos, axis, omega), ((dy, lddy), (dx, lddx)), H * dh)
+    _resident((pos, axis, omega), ((dy, lddy, H * dh), (dx, lddx, H * dh)))
     _check(lib().fast_rotary_bwd(n, H, dh, dtype, _ptr(dy), lddy, _ptr(pos), axes, _ptr(axis),
                                  _ptr(omega), pairs, int(interleaved), _ptr(dx), lddx,
                                  _stream(stream)))
@@ -613,8 +615,7 @@ def fast_edge_attention_fwd_cached(g: TCSR, H, dh, dtype, Q, ids, id_bound, slot
 
 def fast_linear_fwd(n, in_, out, dtype, x, ldx, w, bias, act, res, ldres, y, ldy, pre=None, stream=None):
     """x, res and y may be views whose rows are ldx, ldres and ldy elements apart."""
-    _resident((w, bias, pre), ((x, ldx),), in_)
-    _resident((), ((res, ldres), (y, ldy)), out)
+    _resident((w, bias, pre), ((x, ldx, in_), (res, ldres, out), (y, ldy, out)))
     _check(lib().fast_linear_fwd(n, in_, out, dtype, _ptr(x), ldx, _ptr(w), _ptr(bias), act, _ptr(res),
                                  ldres, _ptr(y), ldy, _ptr(pre), _stream(stream)))
 
@@ -625,8 +626,7 @@ def fast_linear_bwd_workspace(n: int, in_: int, out: int, dtype: int, act: int) 
 
 def fast_linear_bwd(n, in_, out, dtype, x, ldx, w, act, pre, dy, lddy, dx, lddx, dw, dbias, ws,
                     ws_bytes, stream=None):
-    _resident((w, pre, dw, dbias, ws), ((x, ldx), (dx, lddx)), in_)
-    _resident((), ((dy, lddy),), out)
+    _resident((w, pre, dw, dbias, ws), ((x, ldx, in_), (dx, lddx, in_), (dy, lddy, out)))
     _check(lib().fast_linear_bwd(n, in_, out, dtype, _ptr(x), ldx, _ptr(w), act, _ptr(pre), _ptr(dy),
                                  lddy, _ptr(dx), lddx, _ptr(dw), _ptr(dbias), _ptr(ws), ws_bytes,
                                  _stream(stream)))
@@ -643,7 +643,7 @@ def fast_gated_scan_workspace(num_dst: int, num_edges: int, D: int) -> int:
 def fast_gated_scan_fwd(g: TCSR, D, dtype, x, gate, ldx, dt, h0, longest, h, h_last, states, ws,
                         ws_bytes, stream=None):
     """x and gate may be views whose rows are ldx elements apart."""
-    _resident((*getattr(g, "_keep", ())[:1], dt, h0, h, h_last, states, ws), ((x, ldx), (gate, ldx)), D)
+    _resident((*getattr(g, "_keep", ())[:1], dt, h0, h, h_last, states, ws), ((x, ldx, D), (gate, ldx, D)))
     _check(lib().fast_gated_scan_fwd(C.byref(g), D, dtype, _ptr(x), _ptr(gate), ldx, _ptr(dt),
                                      _ptr(h0), longest, _ptr(h), _ptr(h_last), _ptr(states), _ptr(ws),
                                      ws_bytes, _stream(stream)))
@@ -652,7 +652,7 @@ def fast_gated_scan_fwd(g: TCSR, D, dtype, x, gate, ldx, dt, h0, longest, h, h_l
 def fast_gated_scan_bwd(g: TCSR, D, dtype, x, gate, ldx, dt, h0, longest, states, dh, dh_last, dx,
                         dgate, lddx, dh0, ws, ws_bytes, stream=None):
     _resident((*getattr(g, "_keep", ())[:1], dt, h0, states, dh, dh_last, dh0, ws),
-              ((x, ldx), (gate, ldx), (dx, lddx), (dgate, lddx)), D)
+              ((x, ldx, D), (gate, ldx, D), (dx, lddx, D), (dgate, lddx, D)))
     _check(lib().fast_gated_scan_bwd(C.byref(g), D, dtype, _ptr(x), _ptr(gate), ldx, _ptr(dt),
                                      _ptr(h0), longest, _ptr(states), _ptr(dh), _ptr(dh_last),
                                      _ptr(dx), _ptr(dgate), lddx, _ptr(dh0), _ptr(ws), ws_bytes,

@@ -621,6 +621,65 @@ __global__ void __launch_bounds__(64 * WAVES) k_linear_few(LinArgs p) {
   end.finish(r0 + t / 32, z, raw);
 }
 
+// A handful of rows (a request's, one token's): a wave per column takes w's row and up to R rows of x
+// a chunk a lane, and adds up over its lanes.  K >= a chunk.  Bound by w's bytes,
+// below them by the launch: one row past 2048 x 8192 weights in fp32 11 us, past 100 x 272 3.8.
+template <typename T, int R>
+__global__ void __launch_bounds__(LIN_THREADS) k_linear_row(LinArgs p) {
+  constexpr int VE = CHUNK<T>, AHEAD = 4, STEP = 64 * VE;
+  const int lane = threadIdx.x & 63, c = int(blockIdx.x) * (LIN_THREADS / 64) + (threadIdx.x >> 6), K = int(p.K);
+  const int64_t r0 = int64_t(blockIdx.y) * R;
+  const T* w = static_cast<const T*>(p.b) + int64_t(min(c, p.M - 1)) * p.ldb;
+  const T* x[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) x[r] = static_cast<const T*>(p.a) + min(r0 + r, p.n - 1) * p.lda;
+  const LinEnd<T, 1> end(p, c);
+  float sum[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) sum[r] = 0.f;
+  auto add = [&](const u32x4& wv, const u32x4& xv, float& s) {
+    float a[VE], b[VE];
+    lin_unpack(T(), wv, a);
+    lin_unpack(T(), xv, b);
+#pragma unroll
+    for (int j = 0; j < VE; ++j) s = fmaf(a[j], b[j], s);
+  };
+  for (int k0 = 0; k0 < K; k0 += AHEAD * STEP) {
+    u32x4 wv[AHEAD], xv[R][AHEAD];
+#pragma unroll
+    for (int s = 0; s < AHEAD; ++s) {
+      const int at = min(k0 + s * STEP + lane * VE, K - VE);
+      wv[s] = lin_load(w + at);
+#pragma unroll
+      for (int r = 0; r < R; ++r) xv[r][s] = lin_load(x[r] + at);
+    }
+#pragma unroll
+    for (int s = 0; s < AHEAD; ++s) {
+      const int first = k0 + s * STEP, at = first + lane * VE;
+      if (first + STEP > K) {                            // (the same for the whole wave)
+        const u32x4 m = lin_mask<T>(at - min(at, K - VE));
+        wv[s] &= m;
+#pragma unroll
+        for (int r = 0; r < R; ++r) xv[r][s] &= m;
+      }
+#pragma unroll
+      for (int r = 0; r < R; ++r) add(wv[s], xv[r][s], sum[r]);
+    }
+  }
+  float z = 0.f;
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    float v = sum[r];
+    v += dpp_quad_xor1(v);
+    v += dpp_quad_xor2(v);
+    v += dpp_row_half_mirror(v);
+    v += dpp_row_mirror(v);
+    v = sum_halves32(sum_rows16(v));
+    z = lane == r ? v : z;
+  }
+  if (lane < R) end.finish(r0 + lane, &z);
+}
+
 // Many narrow bf16 rows: the weights stay in LDS, a wave holds 32 whole rows as the matrix unit's
 // operand in registers, loads the next 32 while it multiplies the last columns, and waits for no
 // other wave.  Columns lie in LDS in the order in which a lane's results are 8 neighbours of one
@@ -1227,6 +1286,15 @@ static bool lin_many(int64_t n, int M) {
 // Products of fp32 rows in parts from this length on: 264,000 rows into 200 columns in parts against
 // fp32 instructions, k = 200 252 us and 288, 100 183 / 187, 64 126 / 130, 48 119 / 109, 16 95 / 68.
 constexpr int64_t LIN_PARTS_K = 64;
+// A wave per column for a few rows, as long as waves are few for the bytes of a row: against 32 x 32 a
+// workgroup, one row into 2048 columns fp32 k = 272 4.2 us and 5.6, 2048 3.7 / 14.1, 8192 11 / 49; bf16
+// 1024 3.8 / 4.4, 8192 4.7 / 20; 16 rows bf16 1024 7.8 / 5.1, 2048 7.3 / 7.9; 32 rows into 256 fp32
+// 272 3.9 / 5.7, bf16 512 4.1 / 4.4.
+constexpr int64_t LR_ROWS = 32;
+static bool lr_use(int64_t n, int M, int64_t bytes) {
+  const int64_t waves = M * ((n + 3) / 4);
+  return n <= LR_ROWS && bytes >= 1024 && waves <= std::min<int64_t>(3 * bytes, 8192);
+}
 template <typename T>
 static void lin_product(LinArgs a, hipStream_t st) {
   if constexpr (sizeof(T) == 4) {
@@ -1257,13 +1325,20 @@ static void lin_product(LinArgs a, hipStream_t st) {
     lin_tiled<T, LinMid>(a, st);
     return;
   }
-  // (4 waves share k up to 1024 bytes of it, 16 beyond: 64 rows, 256 columns, bf16 k = 1024 6.5 and 6.1
-  // us; at k = 256 fp32 5.7 and 7.3)
+  if (lr_use(a.n, a.M, a.K * int64_t(sizeof(T)))) {
+    const uint32_t cols = uint32_t((a.M + 3) / 4);
+    if (a.n == 1) hipLaunchKernelGGL((k_linear_row<T, 1>), dim3(cols), dim3(LIN_THREADS), 0, st, a);
+    else if (a.n == 2) hipLaunchKernelGGL((k_linear_row<T, 2>), dim3(cols), dim3(LIN_THREADS), 0, st, a);
+    else hipLaunchKernelGGL((k_linear_row<T, 4>), dim3(cols, uint32_t((a.n + 3) / 4)), dim3(LIN_THREADS), 0, st, a);
+    return;
+  }
+  // (4 waves share k up to 1024 bytes of it, 8 beyond: 2000 rows, 256 columns fp32 k = 272 7.6 us and 8.3;
+  // 64 rows bf16 k = 1024 6.2 and 5.8; 16 waves 5.9, and 7.8 for 4.3 at 2000 rows of 272)
   a.tiles_c = (a.M + 31) / 32;
   const dim3 grid(uint32_t((a.n + 31) / 32 * a.tiles_c));
   if (a.K < CHUNK<T>) hipLaunchKernelGGL((k_linear_few<T, 4, true>), grid, dim3(256), 0, st, a);
   else if (a.K * int64_t(sizeof(T)) <= 1024) hipLaunchKernelGGL((k_linear_few<T, 4, false>), grid, dim3(256), 0, st, a);
-  else hipLaunchKernelGGL((k_linear_few<T, 16, false>), grid, dim3(1024), 0, st, a);
+  else hipLaunchKernelGGL((k_linear_few<T, 8, false>), grid, dim3(512), 0, st, a);
 }
 // Workgroups of lin_product times its threads, at most
 static bool lin_fits(int64_t n, int M) {

@@ -94,6 +94,15 @@ def test_linear_narrow_long(K, M, wide):
     check_fwd(16384 + K, K, M, "bf16", "none", False, wide, seed=30)
 
 
+@pytest.mark.parametrize("n", [1, 2, 3, 4, 9, 32, 33])
+@pytest.mark.parametrize("K,M", [(256, 5), (257, 300), (512, 1), (515, 130), (1025, 64), (2049, 7), (4100, 33)])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_linear_handful(n, K, M, dt):
+    """A request's rows: long products of few results, forward and as the rows' gradient."""
+    check_fwd(n, K, M, dt, KINDS[(n + K) % 4], M % 2 == 1, n % 2 == 0, seed=35)
+    check_bwd(n, M, K, dt, KINDS[(n + M) % 4], n % 2 == 1, seed=36)
+
+
 @pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 @pytest.mark.parametrize("n,K,M", [(70, 50, 90), (16500, 33, 300)])
