@@ -10,7 +10,9 @@
 // ends with 4 neighbouring columns of C in a row of its own.
 //
 // Bound by HBM for narrow rows (n (in + out) elements), by the matrix units from a few
-// hundred columns on.
+// hundred columns on.  264,000 rows bf16 272 -> 256: 77 us, dx 78, dw 94 + 20; fp32 372 -> 200 with
+// gelu and its pre 510, dx 370, dw 320, dz 122; 40,000 rows bf16 2048 -> 2048 with silu and
+// residual 495, dx 400 (840 TFLOP/s), dw in parts 1150 (900), dz 180.
 #include <algorithm>
 #include <type_traits>
 
