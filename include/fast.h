@@ -798,7 +798,8 @@ fast_status_t fast_gated_scan_bwd(const fast_tcsr_t* g, int D, fast_dtype_t dtyp
  * lr, t: *lr_dev and *step_dev (device) in place of lr and step where not NULL, for a
  * captured step.  scale: device, NULL for 1; where it is not finite the call leaves
  * weights and states as they are.  grad_scale [1] of fast_grad_norm is one.
- * Arrays that the call writes and that overlap each other or a grad are refused.
+ * Arrays that the call writes and that overlap each other, a grad, lr_dev, step_dev or scale
+ * are refused.
  * Limits: count <= 1024, n < 2^40 each, t >= 1; alignment: each array's element.
  * ------------------------------------------------------------------------ */
 typedef enum {
@@ -828,7 +829,7 @@ fast_status_t fast_adamw(const fast_adamw_tensor_t* tensors, int count, fast_dty
  * factor that clips them:
  *   norm = sqrt(sum grad^2) (squares and sums in fp64, in a fixed order)
  *   scale = max_norm / norm where norm > max_norm, else 1; NaN where norm is not finite
- * norm, scale: [1] fp32 device, scale optional.  max_norm > 0 (infinity: never clips).
+ * norm, scale: [1] fp32 device, apart from grads and workspace, scale optional.  max_norm > 0 (infinity: never clips).
  * Workspace: fast_grad_norm_workspace(total elements, count) bytes, 8-byte aligned; one
  * for the largest list serves smaller ones. */
 size_t fast_grad_norm_workspace(int64_t total, int count);

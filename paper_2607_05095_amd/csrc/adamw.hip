@@ -408,8 +408,10 @@ extern "C" fast_status_t fast_adamw(const fast_adamw_tensor_t* tensors, int coun
     return fail(FAST_ERR_UNSUPPORTED, "%s: lr_dev/step_dev/scale misaligned", fn);
   const bool low = format == FAST_STATE_MXFP8;
   const int64_t es = low ? 1 : 4, gs = elem_size(grad_dtype);
-  AwRange r[AW_COUNT * 7];
-  int k = 0;
+  AwRange r[AW_COUNT * 7 + 3];
+  int k = aw_add(r, 0, lr_dev, 4, false);
+  k = aw_add(r, k, step_dev, 8, false);
+  k = aw_add(r, k, scale, 4, false);
   int64_t total = 0;
   for (int j = 0; j < count; ++j) {
     const fast_adamw_tensor_t& t = tensors[j];
@@ -498,13 +500,20 @@ extern "C" fast_status_t fast_grad_norm(const fast_adamw_tensor_t* tensors, int 
   if (!aligned(norm, 4) || !aligned(scale, 4))
     return fail(FAST_ERR_UNSUPPORTED, "%s: norm/scale not 4-byte aligned", fn);
   int64_t total = 0, blocks = 0;
-  for (int j = 0; j < count; ++j) total += tensors[j].n;
+  for (int j = 0; j < count; ++j) {
+    const int64_t bytes = elem_size(grad_dtype) * tensors[j].n;
+    if (meet(norm, 4, tensors[j].grad, bytes) || meet(scale, 4, tensors[j].grad, bytes))
+      return fail(FAST_ERR_INVALID_ARG, "%s: tensor %d: norm or scale lies in grad", fn, j);
+    total += tensors[j].n;
+  }
   const int chunk = total <= GN_SHORT ? GN_CHUNK_SHORT : GN_CHUNK;
   for (int j = 0; j < count; ++j) blocks += (tensors[j].n + chunk - 1) / chunk;
   const size_t need = fast_grad_norm_workspace(total, count);
   if (!ws || ws_bytes < need)
     return fail(FAST_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", fn, ws ? ws_bytes : 0, need);
   if (!aligned(ws, 8)) return fail(FAST_ERR_UNSUPPORTED, "%s: workspace not 8-byte aligned", fn);
+  if (meet(norm, 4, ws, int64_t(need)) || meet(scale, 4, ws, int64_t(need)))
+    return fail(FAST_ERR_INVALID_ARG, "%s: norm or scale lies in the workspace", fn);
   if (!grid_fits(blocks, GN_THREADS)) return fail(FAST_ERR_UNSUPPORTED, "%s: 2^32 threads or more", fn);
   hipStream_t st = static_cast<hipStream_t>(stream);
   GnArgs a = {};

@@ -269,6 +269,18 @@ def test_grad_norm_refusals(row, kw, status):
     assert fast.lib().fast_grad_norm(*a.values()) == status
 
 
+@pytest.mark.parametrize("kw", [dict(lrd=at(1) + 8), dict(stepd=at(3) + 392), dict(scale=at(4)), dict(scale=at(5) + 196)])
+def test_adamw_refuses_a_step_s_numbers_among_what_it_writes(kw):
+    assert fast.lib().fast_adamw(*{**STEP, "t": tensors({}), **kw}.values()) == INVALID
+    assert "overlaps" in fast.fast_last_error()
+
+
+@pytest.mark.parametrize("kw", [dict(norm=at(2) + 396), dict(scale=at(2)), dict(norm=at(9)), dict(scale=at(9) + 8)])
+def test_grad_norm_refuses_results_in_grads_and_workspace(kw):
+    assert fast.lib().fast_grad_norm(*{**NORM, "t": tensors({}), **kw}.values()) == INVALID
+    assert "lies in" in fast.fast_last_error()
+
+
 def test_grad_norm_workspace():
     f = fast.fast_grad_norm_workspace
     assert f(-1, 1) == f(5, -1) == f(5, 1025) == 0
