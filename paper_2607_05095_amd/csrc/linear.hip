@@ -10,9 +10,9 @@
 // ends with 4 neighbouring columns of C in a row of its own.
 //
 // Bound by HBM for narrow rows (n (in + out) elements), by the matrix units from a few
-// hundred columns on.  264,000 rows bf16 272 -> 256: 77 us, dx 78, dw 94 + 20; fp32 372 -> 200 with
-// gelu and its pre 510, dx 370, dw 320, dz 122; 40,000 rows bf16 2048 -> 2048 with silu and
-// residual 495, dx 400 (840 TFLOP/s), dw in parts 1150 (900), dz 180.
+// hundred columns on.  264,000 rows bf16 272 -> 256: 77 us, dx 78, dw 94 + 10; fp32 372 -> 200 with
+// gelu and its pre 510, dx 370, dw 295, dz 122; 40,000 rows bf16 2048 -> 2048 with silu and
+// residual 495, dx 400 (840 TFLOP/s), dw in parts 1030 (980), dz 180.
 #include <algorithm>
 #include <type_traits>
 
@@ -995,8 +995,10 @@ __device__ __forceinline__ float lin_value(float x) { return x; }
 __device__ __forceinline__ float lin_value(uint16_t x) { return __uint_as_float(uint32_t(x) << 16); }
 
 // As k_linear_wgrad; ONE: p.M is 1.
+// Eight waves: 128 registers, so that two workgroups share a CU and one multiplies while the other cuts
+// up (144 and one workgroup: 1150 us for 1050 at 40,000 rows of 2048 x 2048 bf16).
 template <typename T, typename Tile, bool PRODUCT, bool ONE>
-__global__ void __launch_bounds__(Tile::THREADS) k_linear_wgrad_parts(LinArgs p) {
+__global__ void __launch_bounds__(Tile::THREADS, Tile::THREADS == 512 ? 4 : 1) k_linear_wgrad_parts(LinArgs p) {
   constexpr int TR = Tile::TR, TC = Tile::TC, BR = Tile::BR, BC = Tile::BC, ROW = Tile::ROW, PB = LIN_PARTS<T>;
   constexpr int BK = Tile::KB / 2;
   typedef LinCols<float> ColsA;
@@ -1214,22 +1216,26 @@ __global__ void __launch_bounds__(LIN_THREADS) k_linear_dz(DzArgs p) {
   }
 }
 
-// out[i] = the sum over the parts, in order, in fp64: 64 threads per 16 elements.
-constexpr int LJ_COLS = 16, LJ_PARTS = LIN_THREADS / LJ_COLS;
-__global__ void __launch_bounds__(LIN_THREADS) k_linear_join(const float* __restrict__ part, int64_t parts,
+// out[i] = the sum over the parts in fp64, in an order of their own: a workgroup takes COLS elements, its
+// THREADS / COLS groups every so many-th part.
+template <int COLS, int THREADS>
+__global__ void __launch_bounds__(THREADS) k_linear_join(const float* __restrict__ part, int64_t parts,
                                                              int64_t size, float* __restrict__ out) {
-  __shared__ double s[LJ_PARTS][LJ_COLS];
-  const int col = threadIdx.x % LJ_COLS, q = threadIdx.x / LJ_COLS;
-  const int64_t i = int64_t(blockIdx.x) * LJ_COLS + col;
+  constexpr int PARTS = THREADS / COLS;
+  __shared__ double s[PARTS][COLS];
+  const int col = threadIdx.x % COLS, q = threadIdx.x / COLS;
+  const int64_t i = int64_t(blockIdx.x) * COLS + col;
   double t = 0.0;
   if (i < size) {
-#pragma unroll 4
-    for (int64_t b = q; b < parts; b += LJ_PARTS) t += part[b * size + i];
+#pragma unroll 8
+    for (int64_t b = q; b < parts; b += PARTS) t += part[b * size + i];
   }
-  s[q][col] = t;
-  __syncthreads();
+  if constexpr (PARTS > 1) {
+    s[q][col] = t;
+    __syncthreads();
+  }
   if (q == 0 && i < size) {
-    for (int k = 1; k < LJ_PARTS; ++k) t += s[k][col];
+    for (int k = 1; k < PARTS; ++k) t += s[k][col];
     out[i] = float(t);
   }
 }
@@ -1342,6 +1348,17 @@ static void lin_product(LinArgs a, hipStream_t st) {
   else if (a.K * int64_t(sizeof(T)) <= 1024) hipLaunchKernelGGL((k_linear_few<T, 4, false>), grid, dim3(256), 0, st, a);
   else hipLaunchKernelGGL((k_linear_few<T, 8, false>), grid, dim3(512), 0, st, a);
 }
+// Few elements: many groups share their parts (4125 parts of 200 13 us, with 256 threads 21); few parts: a
+// thread takes all of an element's (4 of 2048 x 2048 19 us, 64-byte pieces 110).
+constexpr int64_t LJ_MANY = 16384, LJ_PARTS = 16;
+static void lin_join(const float* part, int64_t parts, int64_t size, float* out, hipStream_t st) {
+  auto launch = [&](auto kernel, int cols, int threads) {
+    hipLaunchKernelGGL(kernel, dim3(uint32_t((size + cols - 1) / cols)), dim3(threads), 0, st, part, parts, size, out);
+  };
+  if (size < LJ_MANY) launch(k_linear_join<16, 1024>, 16, 1024);
+  else if (parts > LJ_PARTS) launch(k_linear_join<64, 256>, 64, 256);
+  else launch(k_linear_join<256, 256>, 256, 256);
+}
 // Workgroups of lin_product times its threads, at most
 static bool lin_fits(int64_t n, int M) {
   return grid_fits((n + 127) / 128 * ((M + 127) / 128), LIN_THREADS);
@@ -1452,9 +1469,7 @@ static void lin_bwd(int64_t n, int K, int M, fast_dtype_t dtype, const void* x, 
     lin_product<T>(a, st);
   }
   auto join = [&](const float* part, int64_t parts, int64_t size, float* out) {
-    if (parts != 1)
-      hipLaunchKernelGGL(k_linear_join, dim3(uint32_t((size + LJ_COLS - 1) / LJ_COLS)), dim3(LIN_THREADS), 0, st, part,
-                         parts, size, out);
+    if (parts != 1) lin_join(part, parts, size, out, st);
   };
   const int64_t parts = n > 0 ? int64_t(p.splits) : 0;
   if (n > 0 && (dw || (dbias && !acts))) {
@@ -1497,8 +1512,7 @@ static void lin_bwd(int64_t n, int K, int M, fast_dtype_t dtype, const void* x, 
   }
   if (dw) join(m.part, parts, int64_t(M) * K, dw);
   if (dbias && acts) {                                  // a part per block of rows
-    hipLaunchKernelGGL(k_linear_join, dim3(uint32_t((M + LJ_COLS - 1) / LJ_COLS)), dim3(LIN_THREADS), 0, st, m.sums,
-                       p.dz_blocks, int64_t(M), dbias);
+    lin_join(m.sums, p.dz_blocks, M, dbias, st);
   } else if (dbias) {
     join(m.sums, parts, M, dbias);
   }
@@ -1580,7 +1594,7 @@ extern "C" fast_status_t fast_linear_bwd(int64_t n, int in, int out, fast_dtype_
   if (!ws || ws_bytes < need)
     return fail(FAST_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", fn, ws ? ws_bytes : 0, need);
   if (!aligned(ws, 256)) return fail(FAST_ERR_UNSUPPORTED, "%s: workspace not 256-byte aligned", fn);
-  if (!lin_fits(n, in) || !grid_fits((int64_t(in) * out + LJ_COLS - 1) / LJ_COLS, LIN_THREADS))
+  if (!lin_fits(n, in) || !grid_fits((int64_t(in) * out + 63) / 64, LIN_THREADS))
     return fail(FAST_ERR_UNSUPPORTED, "%s: 2^32 threads or more", fn);
   const int64_t sw = int64_t(in) * out;
   const struct { const void* p; int64_t n; } reads[] = {{dw ? x : nullptr, span(n, in, ldx, es)},
