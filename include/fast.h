@@ -717,8 +717,9 @@ fast_status_t fast_linear_fwd(int64_t n, int in, int out, fast_dtype_t dtype, co
  * pre: the forward's (needed with an activation, refused without).  dx: rows of `in`
  * elements of dtype, lddx apart, apart from every input; dw: [out, in] fp32, dbias:
  * [out] fp32, both overwritten (zeros when n = 0); each of the three may be NULL, w
- * where dx is, x where dw is.  dz is fp32; with an activation bf16 products read it rounded
- * to bf16 for dx, and in three parts for dw.  Sums over rows: fp32 over at most 16384 rows,
+ * where dx is, x where dw is.  dz is fp32; with an activation bf16 products read it in bf16 parts, two
+ * for dx (within 2^-16 |dz|, 2^-126 where that is more; exact with FAST_ACT_RELU) and three for dw.
+ * Sums over rows: fp32 over at most 16384 rows,
  * fp64 beyond, in a fixed order (repeated calls give the same bits).
  * Workspace: fast_linear_bwd_workspace(n, in, out, dtype, act) bytes, 256-byte aligned;
  * one for the largest n serves smaller ones. */

@@ -1134,7 +1134,18 @@ __global__ void __launch_bounds__(Tile::THREADS, Tile::THREADS == 512 ? 4 : 1) k
   }
 }
 
-// dz = dy act'(pre) in fp32 (and, for dx of bf16 rows, rounded to that) and its columns' sums: a workgroup takes DZ_ROWS rows and up to 256 chunks of columns, a thread one chunk
+// A value as two bf16 parts, each rounded to nearest: together within 2^-16 of it.  What the first would
+// round to an infinity is cut off instead; an infinity and what is no number have no second part.
+__device__ __forceinline__ void lin_two(float x, float& hi, float& lo) {
+  const bool finite = fabsf(x) < INFINITY;
+  hi = __uint_as_float(bf16_rne(x) << 16);
+  if (finite && fabsf(hi) == INFINITY) hi = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
+  lo = finite ? x - hi : 0.f;
+}
+
+// dz = dy act'(pre) in fp32 (and, for dx of bf16 rows, in two bf16 parts side by side: rounded to one it would
+// move dx by as much as dx's own rounding does; a slope of 0 or 1 leaves a bf16 number, one part) and its
+// columns' sums: a workgroup takes DZ_ROWS rows and up to 256 chunks of columns, a thread one chunk
 // of every `groups`-th row, DZ_AHEAD of them loaded together.  A row's last chunk starts early
 // enough to end with it (both writers of an element write the same value; one counts it).
 // SHORT: rows of less than a chunk.
@@ -1147,6 +1158,7 @@ struct DzArgs {
   const void* pre;
   float* dz;                                            // NULL where only near is needed
   uint16_t* near;                                       // NULL: none
+  int parts;                                            // of near: M of them in a row, or M and M
   float* sums;                                          // [row blocks][M], or NULL
 };
 template <typename T, bool SHORT>
@@ -1196,7 +1208,15 @@ __global__ void __launch_bounds__(LIN_THREADS) k_linear_dz(DzArgs p) {
             for (int j = 0; j < VE; j += 4) store_chunk(p.dz + o + j, SHORT ? n - j : 4, x + j);
           }
           if constexpr (sizeof(T) == 2) {
-            if (p.near) store_chunk(p.near + o, n, x);
+            if (p.near && p.parts == 1) {
+              store_chunk(p.near + o, n, x);
+            } else if (p.near) {
+              uint16_t* q = p.near + 2 * (o - c) + c;
+#pragma unroll
+              for (int j = 0; j < VE; ++j) lin_two(x[j], x[j], y[j]);
+              store_chunk(q, n, x);
+              store_chunk(q + p.M, n, y);
+            }
           }
         }
     }
@@ -1240,13 +1260,22 @@ __global__ void __launch_bounds__(THREADS) k_linear_join(const float* __restrict
   }
 }
 
-// w [M, K] -> wt [K, ld], its columns from M on zeros
-template <typename T>
+// w [M, K] -> wt [K, ld], zeros behind its M columns; PARTS 2: its M columns twice, for dz in two parts.  In the
+// second ones what is not finite is 0: the first part has carried it, and the second, of either sign or 0,
+// would make it no number.
+template <typename T, int PARTS>
 __global__ void __launch_bounds__(LIN_THREADS) k_linear_turn(const T* __restrict__ w, int M, int K, T* __restrict__ wt,
                                                              int ld) {
   __shared__ T s[32][33];
   const int k0 = blockIdx.x * 32, m0 = blockIdx.y * 32, x = threadIdx.x & 31, y = threadIdx.x >> 5;
-  for (int i = y; i < 32; i += 8) s[i][x] = m0 + i < M && k0 + x < K ? w[int64_t(m0 + i) * K + k0 + x] : T(0);
+  for (int i = y; i < 32; i += 8) {
+    const int c = m0 + i, m = PARTS == 2 && c >= M ? c - M : c;
+    T v = m < M && k0 + x < K ? w[int64_t(m) * K + k0 + x] : T(0);
+    if constexpr (PARTS == 2) {
+      if (c >= M && (v & 0x7f80) == 0x7f80) v = T(0);
+    }
+    s[i][x] = v;
+  }
   __syncthreads();
   for (int i = y; i < 32; i += 8)
     if (k0 + i < K && m0 + x < ld) wt[int64_t(k0 + i) * ld + m0 + x] = s[x][i];
@@ -1393,6 +1422,10 @@ struct LinWork {
   float* part;
   float* sums;
 };
+// bf16 parts that dx reads dz in: with a slope other than 0 and 1 dz is no bf16 number
+static int lin_dx_parts(fast_dtype_t dtype, fast_act_t act) {
+  return dtype == FAST_BF16 && act != FAST_ACT_NONE && act != FAST_ACT_RELU ? 2 : 1;
+}
 static int lin_wt_ld(int M, int64_t es) { return int((M * es + 15) / 16 * 16 / es); }
 static size_t lin_layout(int64_t n, int K, int M, fast_dtype_t dtype, fast_act_t act, char* ws, LinWork* w) {
   const LinPlan p = lin_plan(n, K, M, dtype, act);
@@ -1404,10 +1437,10 @@ static size_t lin_layout(int64_t n, int K, int M, fast_dtype_t dtype, fast_act_t
     return q;
   };
   LinWork t;
-  t.wt = take(int64_t(K) * lin_wt_ld(M, es) * es);
+  t.wt = take(int64_t(K) * lin_wt_ld(lin_dx_parts(dtype, act) * M, es) * es);
   const bool acts = act != FAST_ACT_NONE;
   t.dz = acts ? reinterpret_cast<float*>(take(n * M * 4)) : nullptr;
-  t.near = acts && dtype == FAST_BF16 ? reinterpret_cast<uint16_t*>(take(n * M * 2)) : nullptr;
+  t.near = acts && dtype == FAST_BF16 ? reinterpret_cast<uint16_t*>(take(lin_dx_parts(dtype, act) * n * M * 2)) : nullptr;
   t.part = reinterpret_cast<float*>(take(int64_t(p.splits) * M * K * 4));
   t.sums = reinterpret_cast<float*>(take((act != FAST_ACT_NONE ? p.dz_blocks : p.splits) * M * 4));
   if (w) *w = t;
@@ -1444,26 +1477,32 @@ static void lin_bwd(int64_t n, int K, int M, fast_dtype_t dtype, const void* x, 
   const bool acts = act != FAST_ACT_NONE;
   if (n > 0 && acts) {
     DzArgs d = {n, lddy, M, act, (M + CHUNK<T> - 1) / CHUNK<T>, 0, dy, pre, dw || sizeof(T) == 4 ? m.dz : nullptr,
-                dx ? m.near : nullptr, dbias ? m.sums : nullptr};
+                dx ? m.near : nullptr, lin_dx_parts(dtype, act), dbias ? m.sums : nullptr};
     d.lanes = std::min(d.chunks, LIN_THREADS);
     const dim3 grid(uint32_t(p.dz_blocks), uint32_t((d.chunks + d.lanes - 1) / d.lanes));
     if (M < CHUNK<T>) hipLaunchKernelGGL((k_linear_dz<T, true>), grid, dim3(LIN_THREADS), 0, st, d);
     else hipLaunchKernelGGL((k_linear_dz<T, false>), grid, dim3(LIN_THREADS), 0, st, d);
   }
-  const void* dz = !acts ? dy : (sizeof(T) == 4 ? static_cast<const void*>(m.dz) : m.near);   // of dx
   const int64_t lddz = acts ? M : lddy;
   if (dx && n > 0) {
-    const int ld = lin_wt_ld(M, sizeof(T));
-    hipLaunchKernelGGL(k_linear_turn<T>, dim3(uint32_t((K + 31) / 32), uint32_t((ld + 31) / 32)), dim3(LIN_THREADS), 0,
-                       st, static_cast<const T*>(w), M, K, reinterpret_cast<T*>(m.wt), ld);
+    // dz in two parts is one product of twice the length, so all its kernels serve it
+    const int parts = lin_dx_parts(dtype, act), ld = lin_wt_ld(parts * M, sizeof(T));
+    const dim3 grid(uint32_t((K + 31) / 32), uint32_t((ld + 31) / 32));
+    auto turn = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, grid, dim3(LIN_THREADS), 0, st, static_cast<const T*>(w), M, K, reinterpret_cast<T*>(m.wt), ld);
+    };
+    if constexpr (sizeof(T) == 2) {
+      if (parts == 2) turn(k_linear_turn<T, 2>);
+    }
+    if (parts == 1) turn(k_linear_turn<T, 1>);
     LinArgs a = {};
-    a.a = dz;
-    a.lda = lddz;
+    a.a = !acts ? dy : (sizeof(T) == 4 ? static_cast<const void*>(m.dz) : m.near);
+    a.lda = parts * lddz;
     a.b = m.wt;
     a.ldb = ld;
     a.n = n;
     a.M = K;
-    a.K = M;
+    a.K = parts * M;
     a.y = dx;
     a.ldy = lddx;
     lin_product<T>(a, st);
