@@ -662,7 +662,10 @@ def fast_gated_scan_bwd(g: TCSR, D, dtype, x, gate, ldx, dt, h0, longest, states
 def adamw_tensors(w, grad, m, v, m_scale=None, v_scale=None, copy=None, decay=None):
     """Builds the host array of fast_adamw_tensor_t over lists of device tensors, one entry per
     tensor (m_scale, v_scale, copy: None, or lists; decay: a number, a list, or None for 0).  Built once
-    and passed to every step; it keeps a reference to each tensor."""
+    and passed to every step; it holds addresses and keeps a reference to each tensor, so a program whose
+    gradients move builds it anew.  w fp32; all grads fp32 or all bf16; m and v fp32, or all of them codes
+    of a byte (uint8, float8_e4m3fn) with scales of a byte (uint8, float8_e8m0fnu); copy bf16."""
+    import torch
     n = len(w)
     lists = [w, grad, m, v, m_scale, v_scale, copy]
     for k, x in enumerate(lists):
@@ -675,21 +678,37 @@ def adamw_tensors(w, grad, m, v, m_scale=None, v_scale=None, copy=None, decay=No
     elif len(decay) != n:
         raise ValueError("one decay per tensor")
     a = (AdamWTensor * max(n, 1))()
+    f32, bf16 = torch.float32, torch.bfloat16
+    code, power = (torch.uint8, torch.float8_e4m3fn), (torch.uint8, torch.float8_e8m0fnu)
+    half = any(t is not None and t.dtype == bf16 for t in lists[1])
+    low = any(t is not None and t.dtype in code for t in lists[2])
+    types = ((f32,), (bf16,) if half else (f32,), *2 * [code if low else (f32,)], power, power, (bf16,))
     for j, ts in enumerate(zip(*lists)):
         size = ts[0].numel()
         for t, want in zip(ts, (size, size, size, size, (size + 31) // 32, (size + 31) // 32, size)):
             if t is not None and t.numel() != want:
                 raise FastError(1, f"tensor {j}: an array of {t.numel()} elements, {want} wanted")
+        for t, want, name in zip(ts, types, ("w", "grad", "m", "v", "m_scale", "v_scale", "copy")):
+            if t is not None and t.dtype not in want:
+                raise FastError(1, f"tensor {j}: {name} of {t.dtype}, {' or '.join(map(str, want))} wanted")
         a[j] = AdamWTensor(*[_ptr(t) for t in ts], size, decay[j])
+    a._count, a._grad, a._format = n, BF16 if half else F32, STATE_MXFP8 if low else STATE_F32
     a._keep = tuple(t for x in lists for t in x if t is not None)
-    a._count = n
     _resident(a._keep)
     return a
+
+
+def _listed(tensors, grad_dtype, format):
+    """A list's types are those that a call names; raises otherwise."""
+    if tensors._count and (tensors._grad != grad_dtype or tensors._format != format):
+        raise FastError(1, f"grad_dtype {grad_dtype}, format {format}: the list holds grads of dtype "
+                           f"{tensors._grad}, states of format {tensors._format}")
 
 
 def fast_adamw(tensors, grad_dtype, format, lr, beta1, beta2, eps, step, seed=0, lr_dev=None,
                step_dev=None, scale=None, stream=None):
     """tensors: from adamw_tensors."""
+    _listed(tensors, grad_dtype, format)
     _resident((*tensors._keep[:1], lr_dev, step_dev, scale))
     _check(lib().fast_adamw(tensors, tensors._count, grad_dtype, format, lr, beta1, beta2, eps, step,
                             seed, _ptr(lr_dev), _ptr(step_dev), _ptr(scale), _stream(stream)))
@@ -701,6 +720,7 @@ def fast_grad_norm_workspace(total: int, count: int) -> int:
 
 def fast_grad_norm(tensors, grad_dtype, max_norm, norm, scale, ws, ws_bytes, stream=None):
     """tensors: from adamw_tensors."""
+    _listed(tensors, grad_dtype, tensors._format)
     _resident((*tensors._keep[:1], norm, scale, ws))
     _check(lib().fast_grad_norm(tensors, tensors._count, grad_dtype, max_norm, _ptr(norm), _ptr(scale),
                                 _ptr(ws), ws_bytes, _stream(stream)))

@@ -1,0 +1,59 @@
+"""Calls of the products, the recurrence and the AdamW step that are refused before any launch: sizes whose launches do
+not fit, workspaces among a call's arrays, lists of tensors of other types than the step takes.  Without a GPU."""
+import pytest
+import torch
+
+import paper_2607_05095_amd as fast
+from tests.test_train_abi import at
+
+
+# ------------------------------------------------------------------ lists of tensors
+F32, BF16, U8 = torch.float32, torch.bfloat16, torch.uint8
+LISTS = dict(w=[F32, F32], grad=[F32, F32], m=[F32, F32], v=[F32, F32])
+LOW = dict(w=[F32, F32], grad=[BF16, BF16], m=[U8, U8], v=[U8, U8], m_scale=[U8, U8], v_scale=[U8, U8], copy=[BF16, BF16])
+
+
+def lists(types, n=96, **kw):
+    d = {k: [torch.zeros((n + 31) // 32 if "scale" in k else n, dtype=t) for t in ts] for k, ts in dict(types, **kw).items()}
+    return lambda: fast.adamw_tensors(**d)
+
+
+@pytest.mark.parametrize("types,kw,name", [
+    (LISTS, dict(w=[F32, BF16]), "tensor 1: w of torch.bfloat16"), (LISTS, dict(w=[torch.float64, F32]), "tensor 0: w of"),
+    (LISTS, dict(grad=[F32, BF16]), "tensor 0: grad of torch.float32"), (LISTS, dict(grad=[torch.float16, F32]), "tensor 0: grad of"),
+    (LISTS, dict(grad=[BF16, torch.float64]), "tensor 1: grad of"), (LISTS, dict(m=[F32, U8]), "tensor 0: m of torch.float32"),
+    (LISTS, dict(m=[BF16, BF16]), "tensor 0: m of"), (LISTS, dict(v=[F32, BF16]), "tensor 1: v of"),
+    (LISTS, dict(v=[U8, U8]), "tensor 0: v of"), (LOW, dict(v=[F32, F32]), "tensor 0: v of"), (LOW, dict(m=[U8, F32]), "tensor 1: m of"),
+    (LOW, dict(m_scale=[F32, U8]), "tensor 0: m_scale of"), (LOW, dict(v_scale=[U8, torch.int32]), "tensor 1: v_scale of"),
+    (LISTS, dict(copy=[F32, BF16]), "tensor 0: copy of"), (LISTS, dict(copy=[BF16, torch.float16]), "tensor 1: copy of")])
+def test_adamw_tensors_of_other_types_are_refused(types, kw, name):
+    """A step reads and writes each array at its own type's size: one of a smaller type would be passed by."""
+    with pytest.raises(fast.FastError) as e:
+        lists(types, **kw)()
+    assert name in str(e.value)
+
+
+def test_adamw_tensors_of_the_types_named_are_taken():
+    """What is left to refuse here is that there is no GPU."""
+    for types, kw in ((LISTS, {}), (LOW, {}), (LISTS, dict(grad=[BF16, BF16], copy=[BF16, BF16])),
+                      (LOW, dict(m=2 * [torch.float8_e4m3fn], v_scale=2 * [torch.float8_e8m0fnu]))):
+        with pytest.raises(fast.FastError) as e:
+            lists(types, **kw)()
+        assert "not on the current GPU" in str(e.value)
+    assert fast.adamw_tensors([], [], [], [])._count == 0
+
+
+def test_adamw_and_norm_refuse_a_list_of_other_types(monkeypatch):
+    """A call names the types of grads and states; they are those that its list was built of."""
+    monkeypatch.setattr(fast, "_resident", lambda *a: None)
+    wide, low = lists(LISTS)(), lists(LOW)()
+    step = dict(lr=1e-3, beta1=.9, beta2=.999, eps=1e-8, step=1)
+    for ts, grad, form in ((wide, fast.BF16, fast.STATE_F32), (wide, fast.F32, fast.STATE_MXFP8),
+                           (low, fast.F32, fast.STATE_MXFP8), (low, fast.BF16, fast.STATE_F32)):
+        with pytest.raises(fast.FastError) as e:
+            fast.fast_adamw(ts, grad, form, **step)
+        assert "the list holds" in str(e.value)
+    for ts, grad in ((wide, fast.BF16), (low, fast.F32)):
+        with pytest.raises(fast.FastError) as e:
+            fast.fast_grad_norm(ts, grad, 1.0, at(1), at(2), at(3), 1 << 20)
+        assert "the list holds" in str(e.value)
