@@ -1397,6 +1397,7 @@ struct LinPlan {
   int64_t rows;                      // k of a split
   int splits;
   bool parts, wide;                  // fp32 operands in parts; tiles of 128 x 256
+  int64_t tiles;                     // of a split's result
   int64_t dz_blocks;
 };
 constexpr int64_t LIN_SPLIT_MAX = 16384;     // rows whose products are added in fp32, at most
@@ -1406,8 +1407,8 @@ static LinPlan lin_plan(int64_t n, int K, int M, fast_dtype_t dtype, fast_act_t 
   p.parts = dtype == FAST_F32 || acts;
   p.dz_blocks = (n + DZ_ROWS - 1) / DZ_ROWS;
   p.wide = acts && dtype == FAST_BF16 && K >= 512;
-  const int64_t tiles = int64_t((M + 127) / 128) * (p.wide ? (K + 255) / 256 : (K + 127) / 128);
-  int64_t s = std::max<int64_t>(1, 512 / tiles);
+  p.tiles = int64_t((M + 127) / 128) * (p.wide ? (K + 255) / 256 : (K + 127) / 128);
+  int64_t s = std::max<int64_t>(1, 512 / p.tiles);
   s = std::min<int64_t>(s, (n + 255) / 256);
   s = std::max<int64_t>({s, (n + LIN_SPLIT_MAX - 1) / LIN_SPLIT_MAX, 1});
   p.rows = ((n + s - 1) / s + 63) / 64 * 64;
@@ -1633,7 +1634,10 @@ extern "C" fast_status_t fast_linear_bwd(int64_t n, int in, int out, fast_dtype_
   if (!ws || ws_bytes < need)
     return fail(FAST_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", fn, ws ? ws_bytes : 0, need);
   if (!aligned(ws, 256)) return fail(FAST_ERR_UNSUPPORTED, "%s: workspace not 256-byte aligned", fn);
-  if (!lin_fits(n, in) || !grid_fits((int64_t(in) * out + 63) / 64, LIN_THREADS))
+  const LinPlan plan = lin_plan(n, in, out, dtype, act);
+  if (!lin_fits(n, in) || !grid_fits((int64_t(in) * out + 63) / 64, LIN_THREADS) ||
+      (act != FAST_ACT_NONE && !grid_fits(plan.dz_blocks, LIN_THREADS)) ||
+      ((dw || dbias) && !grid_fits(plan.splits * plan.tiles, plan.wide ? LinWide::THREADS : LIN_THREADS)))
     return fail(FAST_ERR_UNSUPPORTED, "%s: 2^32 threads or more", fn);
   const int64_t sw = int64_t(in) * out;
   const struct { const void* p; int64_t n; } reads[] = {{dw ? x : nullptr, span(n, in, ldx, es)},

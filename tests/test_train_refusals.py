@@ -4,7 +4,9 @@ import pytest
 import torch
 
 import paper_2607_05095_amd as fast
-from tests.test_train_abi import at
+from tests.test_train_abi import BWD, UNSUPPORTED, at, call
+
+FAR = 1 << 48                            # from one array to the next, where a case's arrays are large
 
 
 # ------------------------------------------------------------------ lists of tensors
@@ -57,3 +59,18 @@ def test_adamw_and_norm_refuse_a_list_of_other_types(monkeypatch):
         with pytest.raises(fast.FastError) as e:
             fast.fast_grad_norm(ts, grad, 1.0, at(1), at(2), at(3), 1 << 20)
         assert "the list holds" in str(e.value)
+
+
+# ------------------------------------------------------------------ launches
+@pytest.mark.parametrize("kw", [
+    # dz: 64 rows a workgroup of 256 threads
+    dict(n=(1 << 30) - 63, K=1, M=1, act=3), dict(n=1 << 30, K=1, M=1, act=2, dw=None), dict(n=1 << 30, K=1, M=1, act=1, dx=None),
+    dict(n=(1 << 31) - 1, K=1, M=1, act=1, dx=None, dw=None),
+    # the weight gradient: 2^17 splits of 128 tiles, 256 threads each
+    dict(n=(1 << 31) - 16383, K=1, M=16384, act=0, pre=None, dx=None), dict(n=(1 << 31) - 16383, K=1, M=16384, act=0, pre=None, dw=None)])
+def test_linear_bwd_refuses_launches_of_2_32_threads(kw):
+    a = {k: FAR * (j + 1) for j, k in enumerate(("x", "w", "pre", "dy", "dx", "dw", "db", "ws"))}
+    a.update(dt=1, ldx=kw["K"], lddx=kw["K"], lddy=kw["M"], wsb=1 << 62)
+    a.update(kw)
+    assert call("fast_linear_bwd", BWD, a) == UNSUPPORTED
+    assert "2^32 threads" in fast.fast_last_error()
