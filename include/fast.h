@@ -721,8 +721,8 @@ fast_status_t fast_linear_fwd(int64_t n, int in, int out, fast_dtype_t dtype, co
  * for dx (within 2^-16 |dz|, 2^-126 where that is more; exact with FAST_ACT_RELU) and three for dw.
  * Sums over rows: fp32 over at most 16384 rows,
  * fp64 beyond, in a fixed order (repeated calls give the same bits).
- * Workspace: fast_linear_bwd_workspace(n, in, out, dtype, act) bytes, 256-byte aligned;
- * one for the largest n serves smaller ones. */
+ * Workspace: fast_linear_bwd_workspace(n, in, out, dtype, act) bytes, 256-byte aligned, apart from
+ * every array; one for the largest n serves smaller ones. */
 size_t fast_linear_bwd_workspace(int64_t n, int in, int out, fast_dtype_t dtype, fast_act_t act);
 fast_status_t fast_linear_bwd(int64_t n, int in, int out, fast_dtype_t dtype, const void* x,
                               int64_t ldx, const void* w, fast_act_t act, const void* pre,
@@ -749,7 +749,7 @@ fast_status_t fast_linear_bwd(int64_t n, int in, int out, fast_dtype_t dtype, co
  * Outputs lie apart from the inputs and each other (but h_last and h0).
  * Limits: D <= 8192, ldx < 2^26, N, E < 2^31,
  * fewer than 2^32 threads.  Repeated calls give the same bits.
- * Workspace: fast_gated_scan_workspace(N, E, D) bytes, 256-byte aligned; one for the
+ * Workspace: fast_gated_scan_workspace(N, E, D) bytes, 256-byte aligned, apart from every array; one for the
  * largest N, E serves smaller blocks of the same D.
  * ------------------------------------------------------------------------ */
 int64_t fast_gated_scan_state_rows(int64_t num_edges);
@@ -831,7 +831,7 @@ fast_status_t fast_adamw(const fast_adamw_tensor_t* tensors, int count, fast_dty
  *   norm = sqrt(sum grad^2) (squares and sums in fp64, in a fixed order)
  *   scale = max_norm / norm where norm > max_norm, else 1; NaN where norm is not finite
  * norm, scale: [1] fp32 device, apart from grads and workspace, scale optional.  max_norm > 0 (infinity: never clips).
- * Workspace: fast_grad_norm_workspace(total elements, count) bytes, 8-byte aligned; one
+ * Workspace: fast_grad_norm_workspace(total elements, count) bytes, 8-byte aligned, apart from grads; one
  * for the largest list serves smaller ones. */
 size_t fast_grad_norm_workspace(int64_t total, int count);
 fast_status_t fast_grad_norm(const fast_adamw_tensor_t* tensors, int count,

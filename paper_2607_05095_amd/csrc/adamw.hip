@@ -514,6 +514,9 @@ extern "C" fast_status_t fast_grad_norm(const fast_adamw_tensor_t* tensors, int 
   if (!aligned(ws, 8)) return fail(FAST_ERR_UNSUPPORTED, "%s: workspace not 8-byte aligned", fn);
   if (meet(norm, 4, ws, int64_t(need)) || meet(scale, 4, ws, int64_t(need)))
     return fail(FAST_ERR_INVALID_ARG, "%s: norm or scale lies in the workspace", fn);
+  for (int j = 0; j < count; ++j)
+    if (meet(ws, int64_t(need), tensors[j].grad, elem_size(grad_dtype) * tensors[j].n))
+      return fail(FAST_ERR_INVALID_ARG, "%s: tensor %d: the workspace overlaps grad", fn, j);
   if (!grid_fits(blocks, GN_THREADS)) return fail(FAST_ERR_UNSUPPORTED, "%s: 2^32 threads or more", fn);
   hipStream_t st = static_cast<hipStream_t>(stream);
   GnArgs a = {};

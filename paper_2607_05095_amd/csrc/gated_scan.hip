@@ -699,11 +699,21 @@ static fast_status_t gs_run(const char* fn, GsArgs& a, fast_dtype_t dtype, int64
   return check_launch(fn);
 }
 
-static fast_status_t gs_workspace(const char* fn, int64_t N, int64_t E, int D, void* ws, size_t ws_bytes) {
+struct GsSpan {
+  const void* p;
+  int64_t n;
+};
+template <int R, int W>
+static fast_status_t gs_workspace(const char* fn, int64_t N, int64_t E, int D, void* ws, size_t ws_bytes,
+                                  const GsSpan (&reads)[R], const GsSpan (&writes)[W]) {
   const size_t need = fast_gated_scan_workspace(N, E, D);
   if (need > 0 && (!ws || ws_bytes < need))
     return fail(FAST_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", fn, ws ? ws_bytes : 0, need);
   if (!aligned(ws, 256)) return fail(FAST_ERR_UNSUPPORTED, "%s: workspace not 256-byte aligned", fn);
+  bool on = false;
+  for (int j = 0; j < R; ++j) on |= meet(ws, int64_t(need), reads[j].p, reads[j].n);
+  for (int j = 0; j < W; ++j) on |= meet(ws, int64_t(need), writes[j].p, writes[j].n);
+  if (on) return fail(FAST_ERR_INVALID_ARG, "%s: the workspace overlaps another array", fn);
   return FAST_OK;
 }
 
@@ -740,7 +750,7 @@ extern "C" fast_status_t fast_gated_scan_fwd(const fast_tcsr_t* g, int D, fast_d
     return fail(FAST_ERR_UNSUPPORTED, "%s: dt/h0/h_last/states not 4-byte aligned", fn);
   const int64_t in = span(E, D, ldx, es), rows = N * D * 4, out = E * D * es,
                 keep = fast_gated_scan_state_rows(E) * D * 4;
-  const struct { const void* p; int64_t n; } reads[] = {{x, in}, {gate, in}, {dt, 4 * E}, {h0, rows},
+  const GsSpan reads[] = {{x, in}, {gate, in}, {dt, 4 * E}, {h0, rows},
                                                         {g->dst_offsets, 4 * (N + 1)}},
                                              writes[] = {{h, out}, {h_last, rows}, {states, keep}};
   for (int i = 0; i < 3; ++i) {
@@ -751,7 +761,7 @@ extern "C" fast_status_t fast_gated_scan_fwd(const fast_tcsr_t* g, int D, fast_d
       if (meet(writes[i].p, writes[i].n, writes[j].p, writes[j].n))
         return fail(FAST_ERR_INVALID_ARG, "%s: h, h_last and states overlap", fn);
   }
-  if ((s = gs_workspace(fn, N, E, D, ws, ws_bytes)) != FAST_OK) return s;
+  if ((s = gs_workspace(fn, N, E, D, ws, ws_bytes, reads, writes)) != FAST_OK) return s;
   GsArgs a = {};
   a.off = g->dst_offsets;
   a.N = N;
@@ -787,7 +797,7 @@ extern "C" fast_status_t fast_gated_scan_bwd(const fast_tcsr_t* g, int D, fast_d
   if (!aligned(dt, 4) || !aligned(h0, 4) || !aligned(states, 4) || !aligned(dh_last, 4) || !aligned(dh0, 4))
     return fail(FAST_ERR_UNSUPPORTED, "%s: dt/h0/states/dh_last/dh0 not 4-byte aligned", fn);
   const int64_t in = span(E, D, ldx, es), rows = N * D * 4, out = span(E, D, lddx, es);
-  const struct { const void* p; int64_t n; } reads[] = {
+  const GsSpan reads[] = {
       {x, in}, {gate, in}, {dt, 4 * E}, {h0, rows}, {g->dst_offsets, 4 * (N + 1)},
       {states, fast_gated_scan_state_rows(E) * D * 4}, {dh, E * D * es}, {dh_last, rows}},
       writes[] = {{dx, out}, {dgate, out}, {dh0, rows}};
@@ -798,7 +808,7 @@ extern "C" fast_status_t fast_gated_scan_bwd(const fast_tcsr_t* g, int D, fast_d
   if (meet(dx, out, dh0, rows) || meet(dgate, out, dh0, rows) || (E > 0 && dx == dgate) ||
       (E > 0 && rows_collide(static_cast<const char*>(dx), lddx, static_cast<const char*>(dgate), lddx, E, D, es)))
     return fail(FAST_ERR_INVALID_ARG, "%s: dx, dgate and dh0 overlap", fn);
-  if ((s = gs_workspace(fn, N, E, D, ws, ws_bytes)) != FAST_OK) return s;
+  if ((s = gs_workspace(fn, N, E, D, ws, ws_bytes, reads, writes)) != FAST_OK) return s;
   GsArgs a = {};
   a.off = g->dst_offsets;
   a.N = N;

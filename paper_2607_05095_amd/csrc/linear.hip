@@ -1653,7 +1653,12 @@ extern "C" fast_status_t fast_linear_bwd(int64_t n, int in, int out, fast_dtype_
     for (int j = 0; j < i; ++j)
       if (meet(writes[i].p, writes[i].n, writes[j].p, writes[j].n))
         return fail(FAST_ERR_INVALID_ARG, "%s: dx, dw and dbias overlap", fn);
+    if (meet(ws, int64_t(need), writes[i].p, writes[i].n))
+      return fail(FAST_ERR_INVALID_ARG, "%s: the workspace overlaps dx, dw or dbias", fn);
   }
+  for (int j = 0; j < 4; ++j)
+    if (meet(ws, int64_t(need), reads[j].p, reads[j].n))
+      return fail(FAST_ERR_INVALID_ARG, "%s: the workspace overlaps an input", fn);
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (dtype == FAST_F32)
     lin_bwd<float>(n, in, out, dtype, x, ldx, w, act, pre, dy, lddy, dx, lddx, dw, dbias, static_cast<char*>(ws), st);

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import paper_2607_05095_amd as fast
-from tests.test_train_abi import BWD, UNSUPPORTED, at, call
+from tests.test_train_abi import BWD, INVALID, NORM, SB, SF, UNSUPPORTED, at, call, scan_call, tensors
 
 FAR = 1 << 48                            # from one array to the next, where a case's arrays are large
 
@@ -74,3 +74,30 @@ def test_linear_bwd_refuses_launches_of_2_32_threads(kw):
     a.update(kw)
     assert call("fast_linear_bwd", BWD, a) == UNSUPPORTED
     assert "2^32 threads" in fast.fast_last_error()
+
+
+# ------------------------------------------------------------------ workspaces
+def test_linear_bwd_refuses_a_workspace_among_its_arrays():
+    """On each array, and one whose end reaches into the next."""
+    need = fast.fast_linear_bwd_workspace(5, 10, 6, 0, 1)
+    for kw in ([dict(ws=at(k)) for k in (1, 2, 3, 4, 5, 6, 7)] + [dict(ws=at(k) - need // 256 * 256 + 256) for k in (1, 4, 6)] +
+               [dict(dw=at(8) + need - 4), dict(dx=at(8) + need - 4), dict(db=at(8) + 512)]):
+        assert call("fast_linear_bwd", BWD, kw) == INVALID, kw
+        assert "the workspace overlaps" in fast.fast_last_error()
+
+
+@pytest.mark.parametrize("name,defaults,arrays", [("fast_gated_scan_fwd", SF, (1, 2, 3, 4, 5, 6, 7, 20)),
+                                                  ("fast_gated_scan_bwd", SB, (1, 2, 3, 4, 7, 9, 10, 11, 12, 13, 20))])
+def test_gated_scan_refuses_a_workspace_among_its_arrays(name, defaults, arrays):
+    need = fast.fast_gated_scan_workspace(4, 200, 10)
+    for kw in [dict(ws=at(k)) for k in arrays] + [dict(ws=at(k) - need // 256 * 256 + 256) for k in arrays[:3]]:
+        assert scan_call(name, defaults, kw) == INVALID, kw
+        assert "the workspace overlaps" in fast.fast_last_error()
+
+
+def test_grad_norm_refuses_a_workspace_among_grads():
+    other = dict(grad=at(12))
+    for ws in (at(2), at(2) + 392, at(12) + 8):
+        a = dict(NORM, t=tensors({}, other), count=2, ws=ws)
+        assert fast.lib().fast_grad_norm(*a.values()) == INVALID
+        assert "the workspace overlaps" in fast.fast_last_error()
