@@ -19,6 +19,8 @@
 // (two launches, 4.5 TB/s) and the norm of them 32 + 5; 400,000 elements in 24 tensors 6, 5 and 2.
 #include <algorithm>
 #include <cmath>
+#include <memory>
+#include <new>
 
 #include "mx.h"
 #include "rows.h"
@@ -408,7 +410,10 @@ extern "C" fast_status_t fast_adamw(const fast_adamw_tensor_t* tensors, int coun
     return fail(FAST_ERR_UNSUPPORTED, "%s: lr_dev/step_dev/scale misaligned", fn);
   const bool low = format == FAST_STATE_MXFP8;
   const int64_t es = low ? 1 : 4, gs = elem_size(grad_dtype);
-  AwRange r[AW_COUNT * 7 + 3];
+  // (on the heap: 115 KB of them are too much for the stack of a small thread)
+  const std::unique_ptr<AwRange[]> ranges(new (std::nothrow) AwRange[count * 7 + 3]);
+  if (!ranges) return fail(FAST_ERR_WORKSPACE, "%s: no host memory for %d tensors", fn, count);
+  AwRange* r = ranges.get();
   int k = aw_add(r, 0, lr_dev, 4, false);
   k = aw_add(r, k, step_dev, 8, false);
   k = aw_add(r, k, scale, 4, false);

@@ -1,11 +1,16 @@
 """Calls of the products, the recurrence and the AdamW step that are refused before any launch: sizes whose launches do
 not fit, workspaces among a call's arrays, lists of tensors of other types than the step takes.  Without a GPU."""
+import os
+import subprocess
+import sys
+
 import pytest
 import torch
 
 import paper_2607_05095_amd as fast
 from tests.test_train_abi import BWD, INVALID, NORM, SB, SF, UNSUPPORTED, at, call, scan_call, tensors
 
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 FAR = 1 << 48                            # from one array to the next, where a case's arrays are large
 
 
@@ -101,3 +106,26 @@ def test_grad_norm_refuses_a_workspace_among_grads():
         a = dict(NORM, t=tensors({}, other), count=2, ws=ws)
         assert fast.lib().fast_grad_norm(*a.values()) == INVALID
         assert "the workspace overlaps" in fast.fast_last_error()
+
+
+# ------------------------------------------------------------------ small threads
+SMALL = """
+import ctypes, threading
+import paper_2607_05095_amd as fast
+from tests.test_train_abi import STEP, tensors
+f = fast.lib().fast_adamw
+a = list(dict(STEP, t=tensors({}, {}), count=2).values())
+f(*a)                                    # (refused: one tensor twice)
+got = []
+threading.stack_size(96 << 10)
+t = threading.Thread(target=lambda: got.append(f(*a)))
+t.start()
+t.join()
+print("status", got)
+"""
+
+
+def test_adamw_runs_on_a_small_stack():
+    """A thread of 96 KB; the call's list of ranges, 115 KB at its longest, is elsewhere."""
+    r = subprocess.run([sys.executable, "-c", SMALL], cwd=ROOT, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "status [1]" in r.stdout, (r.returncode, r.stdout, r.stderr[-500:])
