@@ -692,8 +692,8 @@ fast_status_t fast_edge_attention_fwd_cached(const fast_tcsr_t* g, int H, int dh
  * (res NULL for none); pre: [n, out] of dtype, optional, only with an activation.
  * y may be res with ldy = ldres; y and pre lie apart from every other array
  * (spans of their rows that meet are refused).  Sums are fp32.  bf16 products are exact in
- * them; fp32 products are rounded, or, where rows are many, formed from three bf16 parts of each
- * value and then within 2^-22 |x w| (2^-126 |x| or |w| where the other is smaller than 2^-100).
+ * them; fp32 products are rounded, or, where rows are many and in every weight gradient, formed from three
+ * bf16 parts of each value and then within 2^-22 |x w| (2^-126 |x| or |w| where the other is smaller than 2^-100).
  * How a row's sums are rounded may depend on n and on whether rows near it are finite;
  * an infinity or a NaN reaches its own row (or, in w, its own column) alone.
  * Limits: in, out <= 16384, n < 2^31, strides < 2^22, and fewer than 2^32 threads.

@@ -102,30 +102,31 @@ __device__ __forceinline__ u32x4 lin_mask(int skip) {
 }
 
 // ------------------------------------------------------------------ fp32 in three parts
-// An fp32 value is the sum of three bf16 values, 8 bits of its mantissa each: cut off, subtracted
-// (exactly), cut off again.  A product of two is then six products of parts; the three that are
-// left out are below 2^-22 of it together, 2^-24 in the mean.  Six bf16 instructions take 2.7
+// An fp32 value is the sum of three bf16 values: rounded to nearest, subtracted (exactly), rounded again; the
+// rest has 8 bits or fewer.  The second is at most 2^-8 of the value, the third 2^-16.  A product of two is then
+// six products of parts; the three that are left out are at most 2^-23 of it together, of either sign (cut off
+// instead of rounded, the parts would all have the value's sign and twice the size: 2^-21, and sums of products
+// short by the mean of it).  Six bf16 instructions take 2.7
 // times less than the fp32 ones of the same product.  An infinity has no such parts (and a part
-// of 0 times an infinity is no number): a workgroup that meets a value that is not finite does
+// of 0 times an infinity is no number), and what rounds to one neither: a workgroup that meets such a value does
 // its tile again with fp32 instructions.
 struct LinParts {
   u32x4 p[3];                        // 8 values: their first, second and third parts
 };
-// cut: accumulates what is not a number once a value was not finite.
+// cut: accumulates what is not a number once a value was not finite, or rounded to an infinity.
 __device__ __forceinline__ LinParts lin_split(const float* x, float& cut) {
   LinParts r;
-  float y[8], z[8];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    y[j] = x[j] - __uint_as_float(__float_as_uint(x[j]) & 0xffff0000u);
-    z[j] = y[j] - __uint_as_float(__float_as_uint(y[j]) & 0xffff0000u);
-    cut = fmaf(y[j], 0.f, cut);
-  }
 #pragma unroll
   for (int d = 0; d < 4; ++d) {
-    r.p[0][d] = __builtin_amdgcn_perm(__float_as_uint(x[2 * d + 1]), __float_as_uint(x[2 * d]), 0x07060302u);
-    r.p[1][d] = __builtin_amdgcn_perm(__float_as_uint(y[2 * d + 1]), __float_as_uint(y[2 * d]), 0x07060302u);
-    r.p[2][d] = __builtin_amdgcn_perm(__float_as_uint(z[2 * d + 1]), __float_as_uint(z[2 * d]), 0x07060302u);
+    float y[2], z[2];
+    r.p[0][d] = bf16_pack(x[2 * d], x[2 * d + 1]);
+    y[0] = x[2 * d] - bf16_lo(r.p[0][d]);
+    y[1] = x[2 * d + 1] - bf16_hi(r.p[0][d]);
+    r.p[1][d] = bf16_pack(y[0], y[1]);
+    z[0] = y[0] - bf16_lo(r.p[1][d]);
+    z[1] = y[1] - bf16_hi(r.p[1][d]);
+    cut = fmaf(y[0], 0.f, fmaf(y[1], 0.f, cut));
+    r.p[2][d] = __builtin_amdgcn_perm(__float_as_uint(z[1]), __float_as_uint(z[0]), 0x07060302u);
   }
   return r;
 }
