@@ -61,6 +61,30 @@ def test_linear_parts_hold_a_product(n, K, M):
     alone(dw, xv[:M, None], wv, "dw")
 
 
+def test_linear_parts_next_to_the_largest_number():
+    """Two values whose first parts, rounded up, have a product past the largest number: their own is 3.39e38."""
+    n, K, M = 16500, 64, 128
+    v = np.array([0x3fff7fff], np.uint32).view(np.float32)[0] * np.float32(2.0 ** 63)
+    big = np.full(n, v, np.float32)
+    x = np.zeros((n, K), np.float32)
+    x[np.arange(n), np.arange(n) % K] = v
+    X = torch.from_numpy(x).cuda()
+    w = torch.full((M, K), float(v), device="cuda")
+    w[1::2] = 2.0 ** -40
+    y = torch.empty(n, M, device="cuda")
+    fast.fast_linear_fwd(n, K, M, 0, X, K, w, None, 0, None, M, y, M)
+    alone(y[:, ::2], big[:, None], np.full((1, M // 2), v), "y")
+    alone(y[:, 1::2], big[:, None], np.full((1, M // 2), 2.0 ** -40, np.float32), "y beside it")
+    dw = torch.empty(M, K, device="cuda")
+    wsb = fast.fast_linear_bwd_workspace(n, K, M, 0, 0)
+    ws = torch.empty(wsb, dtype=torch.uint8, device="cuda")
+    dy = torch.zeros(n, M, device="cuda")
+    dy[torch.arange(K), torch.arange(K)] = float(v)
+    fast.fast_linear_bwd(n, K, M, 0, X, K, None, 0, None, dy, M, None, K, dw, None, ws, wsb)
+    assert (dw[:K] == torch.diag(torch.diagonal(dw))).all()
+    alone(torch.diagonal(dw), big[:K], big[:K], "dw")
+
+
 def test_linear_weight_gradients_always_in_parts():
     """One row: fp32 weight gradients are formed from parts at any n, and held to the same."""
     K, M = 37, 53
