@@ -44,6 +44,8 @@ struct Gate {
 // evaluations of several events and columns interleave.
 // FAR: some gate is so low that e^gate, at most 2^-100 then, may lie below what fp32 holds; over a
 // long time it counts all the same, so it is formed 2^100 times as large and the time as much smaller.
+// Which lanes share a wave decides which version runs: both give the same bits for every gate but those so low,
+// and these always run the scaled one.
 template <bool SPAN, bool FAR>
 __device__ __forceinline__ Gate gate_of(float g, float dt) {
   Gate q;
@@ -52,7 +54,7 @@ __device__ __forceinline__ Gate gate_of(float g, float dt) {
   const float x = fabsf(g), h = -x * 0x1.715476p+0f;
   float l = fmaf(-x, 0x1.715476p+0f, -h);
   l = __builtin_amdgcn_fmed3f(fmaf(-x, 0x1.4ae0cp-26f, l), -1.f, 1.f);
-  const bool far = FAR && h < -100.f;
+  const bool far = FAR && g < 0.f && h < -100.f;
   float ts = __builtin_amdgcn_exp2f(far ? h + 100.f : h);
   ts = fmaf(ts, l * 0x1.62e43p-1f, ts);
   const bool pos = g >= 0.f;
@@ -76,7 +78,7 @@ __device__ __forceinline__ Gate gate_of(float g, float dt) {
   p = fmaf(p, t, -0x1.ffffbep-2f);
   p = fmaf(p, t, 1.f);
   // rate dt
-  const float y = FAR ? fmaf(p * ts, part, fmaxf(g, 0.f) * dt) : fmaf(p, t, fmaxf(g, 0.f)) * dt;
+  const float y = far ? p * ts * part : fmaf(p, t, fmaxf(g, 0.f)) * dt;
   // (1 - e^-y) / y below log 2, within 2^-26; the difference above
   const float e = __builtin_amdgcn_exp2f(y * -0x1.715476p+0f);
   float s = -0x1.0ed322p-10f;
