@@ -390,6 +390,11 @@ __device__ __forceinline__ int64_t find_owner(const GsArgs& a, int64_t k) {
   return -1;
 }
 
+// The product p a of factors a >= 0: 0 only of a factor that is 0.  Where fp32 holds it no more it is the least number
+// that fp32 holds, so that an infinite state passes a piece as it passes its events one by one (times 0 it would
+// be no number); what that adds to a finite state lies where the product's own last bits would have.
+__device__ __forceinline__ float shrink(float p, float a) { return fmaxf(p * a, fminf(fminf(p, a), 0x1p-149f)); }
+
 // A slot's piece: waves over its columns, `first` of them this wave's, `step` from one to its next.
 template <typename T, int VE, bool SPAN, bool BACK>
 __device__ __forceinline__ void piece_sums(const GsArgs& a, int64_t k, int first, int step) {
@@ -443,7 +448,7 @@ __device__ __forceinline__ void piece_sums(const GsArgs& a, int64_t k, int first
             const float in =
                 BACK ? y[j][q].a * (pb[q] + (a.dh ? xv[q] : 0.f)) : fmaf(y[j][q].a, pb[q], y[j][q].u * xv[q]);
             pb[q] = i + j < m ? in : pb[q];
-            pa[q] = i + j < m ? pa[q] * y[j][q].a : pa[q];
+            pa[q] = i + j < m ? shrink(pa[q], y[j][q].a) : pa[q];
           }
         }
       }
@@ -521,7 +526,7 @@ struct Chain {
         if (j + q < j1) {
           if (WRITE && write) a.pa[at(j + q)] = s;
           s = fmaf(xa[q], s, xb[q]);
-          pa *= xa[q];
+          pa = shrink(pa, xa[q]);
         }
     }
   }
