@@ -1286,7 +1286,9 @@ __global__ void __launch_bounds__(LIN_THREADS) k_linear_turn(const T* __restrict
 // Long products into wide rows take 256 x 128, which reads a quarter less from L2 than 128 x 128
 // (40,000 x 2048 x 2048 bf16 485 against 548 us, 8192^3 1178 / 1697; the library 349 / 728;
 // 256 x 256 leaves one workgroup per CU, whose epilogue nothing hides).  Otherwise more workgroups per
-// CU count for more: 128 x 128.
+// CU count for more: 128 x 128.  Both at 40,000 rows, k x columns: 1024 x 1024 107 / 124, 2048 x 512 119 / 120,
+// 1024 x 512 67 / 65, 2048 x 256 68 / 64, 512 x 512 42 / 41 (512 x 2048 126 / 139: left to 128 x 128); 16,384 rows
+// (256 tiles of 256 x 256) 1024 x 1024 46 / 57; 8192 (128 of them) 2048 x 1024 53 / 49.
 static bool lin_big(int64_t n, int M, int64_t K) {
   return K >= 1024 && M >= 512 && ((n + 255) / 256) * ((M + 255) / 256) >= 256;
 }
@@ -1294,7 +1296,9 @@ constexpr int LS_GRID = 256;                // workgroups: one per CU
 // The streaming kernel's rule: rows that a wave's registers and weights that LDS hold, and enough of
 // them to pay for bringing the weights to every CU.  At 264000 rows, in x out, against 128 x 128 tiles:
 // 272 x 256 77 us and 111, 256 x 256 74 and 80, 200 x 200 49 and 73, 100 x 64 17 and 31; at 16384 rows
-// 12.6 and 12.2, 11.1 and 11.3, 100 x 64 6.6 and 6.9; at 4096 11.9 and 8.1.
+// 12.6 and 12.2, 11.1 and 11.3, 100 x 64 6.6 and 6.9; at 4096 11.9 and 8.1.  As wide as LDS holds, 264000 rows: 64 x 960
+// 145 and 189, 128 x 480 91 and 131; 16384: 20.5 and 18.2, 13.6 and 12.6.  LS_STEPS covers k <= 288; a step
+// more would take 320 x 200 from 93 to 79, two 352 x 200 nowhere (117).
 constexpr int64_t LS_ROWS = 16384;
 static int ls_steps(int64_t K) { return K <= 64 ? 2 : K <= 128 ? 4 : K <= 192 ? 6 : int((K + 31) / 32); }
 static bool ls_use(const LinArgs& a) {
@@ -1370,12 +1374,15 @@ static void lin_product(LinArgs a, hipStream_t st) {
     else hipLaunchKernelGGL((k_linear_row<T, 4>), dim3(cols, uint32_t((a.n + 3) / 4)), dim3(LIN_THREADS), 0, st, a);
     return;
   }
-  // (4 waves share k up to 1024 bytes of it, 8 beyond: 2000 rows, 256 columns fp32 k = 272 7.6 us and 8.3;
-  // 64 rows bf16 k = 1024 6.2 and 5.8; 16 waves 5.9, and 7.8 for 4.3 at 2000 rows of 272)
+  // Waves that share k: 4 up to 1024 bytes of it, and where there are more workgroups than CUs; 8 otherwise.  4 / 8
+  // waves into 256 columns, us: 504 workgroups, fp32 k = 256 6.6 / 8.1, 272 7.6 / 8.3, 384 8.7 / 11.9, 512 10.9 / 11.9,
+  // 1024 21.2 / 21.4; 152, fp32 256 5.1 / 4.6, 272 5.4 / 4.8, 384 6.1 / 6.7, 512 6.9 / 6.4, 1024 10.4 / 10.1; 16, bf16
+  // 272 3.7 / 3.4, 544 4.4 / 3.8, 768 5.4 / 6.0, 1024 6.2 / 5.9.
   a.tiles_c = (a.M + 31) / 32;
   const dim3 grid(uint32_t((a.n + 31) / 32 * a.tiles_c));
   if (a.K < CHUNK<T>) hipLaunchKernelGGL((k_linear_few<T, 4, true>), grid, dim3(256), 0, st, a);
-  else if (a.K * int64_t(sizeof(T)) <= 1024) hipLaunchKernelGGL((k_linear_few<T, 4, false>), grid, dim3(256), 0, st, a);
+  else if (a.K * int64_t(sizeof(T)) <= 1024 || grid.x > 256)
+    hipLaunchKernelGGL((k_linear_few<T, 4, false>), grid, dim3(256), 0, st, a);
   else hipLaunchKernelGGL((k_linear_few<T, 8, false>), grid, dim3(512), 0, st, a);
 }
 // Few elements: many groups share their parts (4125 parts of 200 13 us, with 256 threads 21); few parts: a
@@ -1407,8 +1414,12 @@ static LinPlan lin_plan(int64_t n, int K, int M, fast_dtype_t dtype, fast_act_t 
   const bool acts = act != FAST_ACT_NONE;
   p.parts = dtype == FAST_F32 || acts;
   p.dz_blocks = (n + DZ_ROWS - 1) / DZ_ROWS;
+  // 128 x 256 / 128 x 128 at 40,000 rows, columns of x x of dz, us: 372 x 200 61 / 59, 512 x 512 120 / 120, 768 x 768
+  // 224 / 236, 1024 x 1024 328 / 368
   p.wide = acts && dtype == FAST_BF16 && K >= 512;
   p.tiles = int64_t((M + 127) / 128) * (p.wide ? (K + 255) / 256 : (K + 127) / 128);
+  // 512 workgroups, two a CU (256 / 512 / 1024, us: 264,000 rows 272 x 256 bf16 117 / 93 / 103, 372 x 200 fp32 391 / 304 /
+  // 334; 40,000 rows 2048 x 2048 bf16 with silu 1234 / 1090 / 1124)
   int64_t s = std::max<int64_t>(1, 512 / p.tiles);
   s = std::min<int64_t>(s, (n + 255) / 256);
   s = std::max<int64_t>({s, (n + LIN_SPLIT_MAX - 1) / LIN_SPLIT_MAX, 1});

@@ -33,6 +33,15 @@ def test_linear_many_short_rows(n, K, M, dt, wide):
     check_bwd(n, M, K, dt, KINDS[(n + M) % 4], wide, seed=8)
 
 
+# 32 x 32 results a workgroup: up to 256 of them and more, k of up to 1024 bytes and more
+@pytest.mark.parametrize("n", [800, 830, 2000])
+@pytest.mark.parametrize("K,M", [(250, 300), (600, 300), (1030, 310)])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_linear_few_results(n, K, M, dt):
+    check_fwd(n, K, M, dt, KINDS[(n + K) % 4], K > 300, n == 830, seed=9)
+    check_bwd(n, M, K, dt, KINDS[(n + M + K) % 4], n == 800, seed=10)
+
+
 def small(n, F, dt, seed, ld=None):
     """whole numbers of -3 .. 3"""
     g = torch.Generator(device="cuda").manual_seed(seed)
