@@ -444,7 +444,7 @@ extern "C" fast_status_t fast_adamw(const fast_adamw_tensor_t* tensors, int coun
   AwArgs a = {};
   a.b1 = beta1;
   a.b2 = beta2;
-  a.eps = eps;
+  a.eps = eps > 0.0 ? std::max(eps, 0x1p-149) : 0.0;   // (an fp32 number: above 0 where eps is, so that 0 / eps is 0)
   a.lr = lr;
   a.step = step;
   if (!step_dev) {
