@@ -18,11 +18,13 @@
 // starts of two pieces never share a slot of `piece` positions, so slot = start / piece
 // numbers them.
 //
-// 264,000 segments, 2.4 M events of 100 fp32: forward 630 us (4.8 TB/s, 400-byte rows),
-// backward 1300 (3.8: 188 registers, two waves a SIMD; three or four by spilling 1690 and 3421).
-// bf16 is bound by the gates' instructions, 55 forward and 72 back: 900,001 events of 256,
-// three hubs among 6000 segments, 306 + 72 and 596 + 117 us.  Four segments of 100,003 events
-// of 128 in all: sums 26, chains 17, pieces 39 (forward), 28, 17, 56 (backward).
+// 264,000 segments, 2.4 M events of 100 fp32: forward 620 us (4.8 TB/s, 400-byte rows),
+// backward 1300-1380 (3.7: 186 registers, two waves a SIMD; three or four by spilling 1690 and 3421).
+// bf16, 900,001 events of 256, three hubs among 6000 segments: 308 + 70 and 595 + 120 us.  Forward two halves of the
+// same size: its bytes would take 225 us, its instructions about 180 (25 vector instructions a gate and
+// column without times, 16 of them the gate's, the rest addresses, conversions and two-column stores); backward
+// 37 of them, and three waves a SIMD to hide the loads of a window behind.  Four segments of 100,003 events
+// of 128 in all: sums 27, chains 18, pieces 38 (forward), 29, 19, 53 (backward).
 #include <algorithm>
 
 #include "rows.h"

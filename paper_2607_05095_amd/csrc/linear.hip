@@ -10,9 +10,10 @@
 // ends with 4 neighbouring columns of C in a row of its own.
 //
 // Bound by HBM for narrow rows (n (in + out) elements), by the matrix units from a few
-// hundred columns on.  264,000 rows bf16 272 -> 256: 77 us, dx 78, dw 94 + 10; fp32 372 -> 200 with
-// gelu and its pre 510, dx 370, dw 295, dz 122; 40,000 rows bf16 2048 -> 2048 with silu and
-// residual 495, dx 400 (840 TFLOP/s), dw in parts 1030 (980), dz 180.
+// hundred columns on.  264,000 rows bf16 272 -> 256: 76 us, dx 78-88, dw 96 + 11; fp32 372 -> 200 with
+// gelu and its pre 470-550, dx 380-475, dw 310-375 (the clock falls over repeated passes), dz 122; 40,000 rows bf16
+// 2048 -> 2048 with silu and residual 480-560, dx of dz in two parts 780-880 (850 TFLOP/s; of one part, as
+// without an activation or with relu, 400), dw in three parts 1040-1240 (970), dz 220.
 #include <algorithm>
 #include <type_traits>
 
@@ -997,7 +998,8 @@ __device__ __forceinline__ float lin_value(uint16_t x) { return __uint_as_float(
 
 // As k_linear_wgrad; ONE: p.M is 1.
 // Eight waves: 128 registers, so that two workgroups share a CU and one multiplies while the other cuts
-// up (144 and one workgroup: 1150 us for 1050 at 40,000 rows of 2048 x 2048 bf16).
+// up (144 and one workgroup: 1150 us for 1050 at 40,000 rows of 2048 x 2048 bf16).  The bound spills 6 registers
+// there (28 bytes of scratch a lane, bf16 rows).
 template <typename T, typename Tile, bool PRODUCT, bool ONE>
 __global__ void __launch_bounds__(Tile::THREADS, Tile::THREADS == 512 ? 4 : 1) k_linear_wgrad_parts(LinArgs p) {
   constexpr int TR = Tile::TR, TC = Tile::TC, BR = Tile::BR, BC = Tile::BC, ROW = Tile::ROW, PB = LIN_PARTS<T>;
